@@ -19,16 +19,20 @@
  *                     in a single call.
  *
  * Beside them: flowkv_decode_attention*, the paged decode attention that
- * reads either layout (the PagedAttention kernel section 3.3 adapts), and
- * flowkv_sched*, the load-aware scheduler of section 3.4 (Algorithm 1),
- * host only.
+ * reads either layout (the PagedAttention kernel section 3.3 adapts);
+ * flowkv_append and flowkv_chunk_attention, which fill the pool and read it
+ * for a chunk of new tokens (prefill, several tokens of a decode step);
+ * flowkv_copy_blocks with flowkv_share, flowkv_fork and flowkv_compact, pages
+ * copied within a pool, shared and moved together; and flowkv_sched*, the
+ * load-aware scheduler of section 3.4 (Algorithm 1), host only.
  *
  * Conventions for every entry point:
  *   - Functions return FLOWKV_OK (0) or a negative FLOWKV_E* code; nothing
  *     throws across the ABI.  flowkv_strerror() names a code;
  *     flowkv_last_error() gives the calling thread's last detailed message.
  *   - On error, output arguments are left untouched, except *n_out of the
- *     planners and *n_runs of flowkv_transfer_request on FLOWKV_ECAP.
+ *     planners, *n_runs of flowkv_transfer_request and *n_moves of
+ *     flowkv_compact on FLOWKV_ECAP.
  *   - The caller owns every buffer.  The library allocates no device memory and
  *     keeps no pointer after a call returns, except inside an allocator or a
  *     scheduler handle, and except the fixed scratch array of
@@ -180,15 +184,53 @@ void flowkv_allocator_destroy(flowkv_allocator* a);
    n_blocks < 0. */
 int flowkv_alloc(flowkv_allocator* a, int32_t n_blocks, int32_t* out_ids);
 
-/* Return ids[0 .. n) to the free pool, merging with free neighbours.
-   ERANGE: an ID out of range; EDUP: an ID repeated or already free.  Checked
-   before any change: on error nothing is freed. */
+/* Return ids[0 .. n) to the free pool, merging with free neighbours.  A block
+   with several owners (flowkv_share) loses one, and is free when the last one
+   frees it.  ERANGE: an ID out of range; EDUP: an ID repeated or already free.
+   Checked before any change: on error nothing is freed. */
 int flowkv_free(flowkv_allocator* a, const int32_t* ids, int32_t n);
 
 /* Mark ids[0 .. n) in use without allocating them (blocks already held by
    resident requests).  ERANGE / EDUP as for flowkv_free, EDUP also for a block
    already in use.  On error nothing changes. */
 int flowkv_mark_used(flowkv_allocator* a, const int32_t* ids, int32_t n);
+
+/* One more owner for each of ids[0 .. n), blocks in use: requests whose first
+   tokens agree list the same blocks, and each frees its list as it would its
+   own.  ERANGE: an ID out of range; EDUP: an ID repeated or free; EINVAL: a
+   block with 2^31 - 1 owners.  On error nothing changes. */
+int flowkv_share(flowkv_allocator* a, const int32_t* ids, int32_t n);
+
+/* counts[0 .. n): the owners of ids[0 .. n), 0 for a free block, 1 for a block
+   that was allocated or marked used and never shared.  IDs may repeat.
+   ERANGE: an ID out of range. */
+int flowkv_owners(const flowkv_allocator* a, const int32_t* ids, int32_t n, int32_t* counts);
+
+/* The block list of a second continuation of a request with n_tokens tokens in
+   ids[0 .. n_blocks), block_size a block: it shares the full blocks, and has a
+   block of its own, newly allocated, in the place of a part-filled last one.
+   Writes ceil(n_tokens / block_size) IDs to out_ids and to *copy_tokens how
+   many tokens that block has to receive (0: there is none).  The caller copies
+   them, with k = n_tokens / block_size:
+   flowkv_copy_blocks(pool, ids + k, out_ids + k, copy_tokens, 1, ...).
+   EINVAL: NULL pointers, negative sizes, block_size < 1, more tokens than
+   n_blocks hold; ERANGE / EDUP as for flowkv_share, over the blocks that the
+   tokens lie in; ENOSPC: no free block.  On error nothing changes. */
+int flowkv_fork(flowkv_allocator* a, const int32_t* ids, int32_t n_blocks, int64_t n_tokens,
+                int32_t block_size, int32_t* out_ids, int32_t* copy_tokens);
+
+/* Move the blocks in use together: with U of them, those at U and above go to
+   the free IDs below U, in ascending order on both sides, so that one run
+   [U, num_blocks) is left free and the fewest blocks move.  Writes the moves to
+   src_ids and dst_ids [0 .. *n_moves); from then on the allocator counts the
+   destinations as in use (with the sources' owners) and the sources as free
+   (a FIFO policy appends them in this order).  The caller copies the blocks
+   (flowkv_copy_blocks) before anything writes to a source, and renames them in
+   its block lists.  *n_moves is 0 where the blocks in use lie together already.
+   ECAP: more than `cap` moves (*n_moves = moves needed, nothing changed);
+   EINVAL: NULL pointers (the lists may be NULL when cap is 0), cap < 0. */
+int flowkv_compact(flowkv_allocator* a, int32_t cap, int32_t* src_ids, int32_t* dst_ids,
+                   int32_t* n_moves);
 
 /* Current free-space summary. */
 int flowkv_allocator_stats(const flowkv_allocator* a, flowkv_alloc_stats* out);
@@ -397,6 +439,93 @@ int flowkv_decode_attention_noalloc(const flowkv_pool* pool, int32_t layer, cons
                                     const int32_t* seq_lens_host, int32_t max_seq_len,
                                     float scale, int32_t split_tokens, float* out_dev,
                                     void* hip_stream);
+
+/* ---- new tokens: written into the pool, and attending over it -----------------
+   A call takes a ragged batch: n_tokens new tokens, one request after another,
+   request r's at offsets[r] .. offsets[r + 1] (n_req + 1 non-decreasing int32
+   in device memory, offsets[0] >= 0 and offsets[n_req] <= n_tokens; a request
+   may have none).  seq_lens[r] is the request's length with its new tokens, so
+   new token i of r is at position seq_lens[r] - (offsets[r + 1] - offsets[r]) +
+   i.  block_tables (n_req, max_blocks) as for flowkv_decode_attention.  Lengths
+   and offsets are read from device memory only, so a captured call may be
+   replayed with others.  Rows of the batch that belong to no request (before
+   offsets[0], from offsets[n_req] on: padding) are neither read into the pool
+   nor written. */
+
+/* Write new tokens' K and V of layer `layer` into their requests' blocks, one
+   launch on hip_stream.  Byte-exact for any element type.  k_dev, v_dev: each
+   token's slot_bytes = kv_heads x head_dim x element size bytes, 16-byte
+   aligned, tokens k_stride and v_stride BYTES apart (columns of a joint
+   projection need no copy first).  The pool's chunk_bytes is block_size x
+   slot_bytes.  A token at a negative position, past max_blocks x block_size, or
+   whose block ID is outside the pool is not written.  Two new tokens in one
+   slot (a block that two requests of the batch both write) leave either's
+   bytes.  Nothing is read from the pool and no other byte of it is written.
+   EINVAL: NULL pointers, negative sizes, bad pool (as for flowkv_transfer),
+   layer outside it, slot_bytes not a multiple of 16 that divides chunk_bytes,
+   misaligned k, v or strides, strides below slot_bytes. */
+int flowkv_append(const flowkv_pool* pool, int32_t layer, const void* k_dev, int64_t k_stride,
+                  const void* v_dev, int64_t v_stride, int64_t slot_bytes, int32_t n_tokens,
+                  int32_t n_req, const int32_t* offsets_dev, const int32_t* block_tables_dev,
+                  int32_t max_blocks, const int32_t* seq_lens_dev, void* hip_stream);
+
+/* Attention of new tokens over the pool: prefill in chunks, a prompt behind a
+   cached prefix, or the several tokens of a speculative decode step.  The new
+   tokens' own K and V are in the pool already (flowkv_append).  For new token i
+   of request r at position p and query head h (KV head g = h / (q_heads /
+   kv_heads)), over layer `layer` of a bf16 pool of either layout:
+       out[i][h] = sum_{t <= p} softmax_t(scale * q[i][h] . K[t][g]) * V[t][g]
+   q_dev: bf16, 16-byte aligned, a token's (q_heads, head_dim) values together
+   and tokens q_stride ELEMENTS apart (a multiple of 8).  out_dev: (n_tokens,
+   q_heads, head_dim) bf16, 8-byte aligned; scores, weights' sums and the output
+   are formed in float32, the weights enter the matrix product rounded to bf16,
+   and the output is rounded once.  Tokens beyond max_blocks x block_size or
+   beyond max_seq_len are not read; a block ID outside the pool contributes
+   nothing; a new token that sees nothing (a negative position among them) gets
+   zeros.  A score that is NaN or +inf makes its row's output NaN; one of -inf
+   weighs nothing.  K and V of tokens that a row does not see, infinities and
+   NaN among them, do not reach it.
+   max_new: the most new tokens of a request, and max_seq_len the longest
+   length; both size the launch, and rows past max_new are computed all the
+   same.  head_dim 64 or 128; any whole number of query heads per KV head.
+   split_tokens: cached tokens per workgroup, a multiple of 64; 0 takes the
+   library's rule.  One launch on hip_stream, two where max_seq_len is more than
+   split_tokens; then workspace_dev holds at least
+   flowkv_chunk_attention_workspace(...) bytes, owned by the caller and busy
+   until the stream passes the call (NULL when that is 0; calls that may overlap
+   need one each).  EINVAL for bad shapes or pointers, ECAP for a short
+   workspace. */
+int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, const void* q_dev,
+                           int64_t q_stride, int32_t n_tokens, int32_t n_req, int32_t q_heads,
+                           int32_t kv_heads, int32_t head_dim, const int32_t* offsets_dev,
+                           const int32_t* block_tables_dev, int32_t max_blocks,
+                           const int32_t* seq_lens_dev, int32_t max_new, int32_t max_seq_len,
+                           float scale, int32_t split_tokens, void* out_dev, void* workspace_dev,
+                           int64_t workspace_bytes, void* hip_stream);
+
+/* Workspace bytes of flowkv_chunk_attention for these arguments: 0 where one
+   split covers max_seq_len, else n_tokens x q_heads x ceil(max_seq_len /
+   split_tokens) x (head_dim + 2) floats. */
+int flowkv_chunk_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q_heads,
+                                     int32_t kv_heads, int32_t head_dim, int32_t max_new,
+                                     int32_t max_seq_len, int32_t split_tokens, int64_t* bytes);
+
+/* ---- copies of blocks within a pool --------------------------------------------- */
+
+/* Copy block src_ids[i] to block dst_ids[i], every layer's K and V, for i in
+   [0, n_blocks): lists in host memory, read before the call returns.  With
+   `tokens` (host, NULL = whole blocks) only the first tokens[i] slots of each
+   chunk, slot_bytes apart (ignored without `tokens`), are copied, the rest of
+   the destination stays.  A source may go to several destinations.  The lists
+   travel in the kernel arguments; long ones take several launches on
+   hip_stream.  Byte-exact for any element type.
+   ERANGE: an ID outside the pool; EDUP: a destination listed twice, or also
+   among the sources; EINVAL: NULL pointers, negative sizes, bad pool (as for
+   flowkv_transfer), a token count outside 0 .. block_size, slot_bytes not a
+   multiple of 16 that divides chunk_bytes.  Checked before any launch. */
+int flowkv_copy_blocks(const flowkv_pool* pool, const int32_t* src_ids, const int32_t* dst_ids,
+                       const int32_t* tokens, int32_t n_blocks, int64_t slot_bytes,
+                       void* hip_stream);
 
 /* ---- load-aware scheduler (section 3.4; Appendix A, Algorithm 1) ------------
    Host only.  Each node reports a status vector S_i of 12 indicators, in

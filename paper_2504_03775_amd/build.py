@@ -1,7 +1,7 @@
 """Build the native library ``libflowkv.so`` in-tree for gfx950.
 
 ``python -m paper_2504_03775_amd.build`` compiles the host C++ (allocator,
-planner, scheduler, status) with g++ and the HIP translation unit (kernel + launcher)
+planner, scheduler, status) with g++ and the HIP translation units (kernels + launchers)
 with hipcc, then links them into ``paper_2504_03775_amd/libflowkv.so``.  In a
 checkout with ``tests/native/abi_transfer.cpp`` it also builds that program,
 which drives the library through the C ABI alone (no Python), next to its
@@ -24,7 +24,8 @@ LIB = os.path.join(PKG, "libflowkv.so")
 
 HOST_SOURCES = ["flowkv_status.cpp", "flowkv_alloc.cpp", "flowkv_plan.cpp", "flowkv_sched.cpp",
                 "flowkv_request.cpp"]
-HIP_SOURCES = ["flowkv_transfer.hip", "flowkv_attention.hip"]
+HIP_SOURCES = ["flowkv_transfer.hip", "flowkv_attention.hip", "flowkv_chunk.hip",
+               "flowkv_pages.hip"]
 
 ARCH = "gfx950"
 # packed-fp32 instructions are disabled for every HIP translation unit

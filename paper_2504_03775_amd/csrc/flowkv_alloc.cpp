@@ -30,6 +30,8 @@ struct flowkv_allocator {
   int32_t policy = FLOWKV_POLICY_SEGMENT;
   int64_t free_blocks = 0;
   std::vector<uint8_t> used;  // 1 = in use (2: seen while a list is being checked)
+  // owners of a block in use beyond the first; empty until a block is shared
+  std::vector<int32_t> extra;
 
   // FLOWKV_POLICY_SEGMENT
   std::map<int32_t, int32_t> by_start;            // start -> length
@@ -218,6 +220,16 @@ int free_impl(flowkv_allocator* a, const int32_t* ids, int32_t n) {
   if (!a) return fail(FLOWKV_EINVAL, "NULL allocator");
   int rc = check_ids(a, ids, n, /*want_used=*/true);
   if (rc) return rc;
+  std::vector<int32_t> last;  // the blocks that lose their last owner
+  if (!a->extra.empty()) {
+    last.reserve(size_t(n));
+    for (int32_t i = 0; i < n; ++i) {
+      if (a->extra[ids[i]] > 0) --a->extra[ids[i]];
+      else last.push_back(ids[i]);
+    }
+    ids = last.data();
+    n = int32_t(last.size());
+  }
   for (int32_t i = 0; i < n; ++i) a->used[ids[i]] = 0;
   a->free_blocks += n;
   if (a->policy == FLOWKV_POLICY_SEGMENT)
@@ -246,7 +258,115 @@ int mark_used_impl(flowkv_allocator* a, const int32_t* ids, int32_t n) {
   return ok();
 }
 
+int share_impl(flowkv_allocator* a, const int32_t* ids, int32_t n) {
+  if (!a) return fail(FLOWKV_EINVAL, "NULL allocator");
+  int rc = check_ids(a, ids, n, /*want_used=*/true);
+  if (rc) return rc;
+  if (n == 0) return ok();
+  if (a->extra.empty()) a->extra.assign(size_t(a->num_blocks), 0);
+  for (int32_t i = 0; i < n; ++i)
+    if (a->extra[ids[i]] >= INT32_MAX - 1)
+      return fail(FLOWKV_EINVAL, "block %d has 2^31 - 1 owners", ids[i]);
+  for (int32_t i = 0; i < n; ++i) ++a->extra[ids[i]];
+  return ok();
+}
+
+int fork_impl(flowkv_allocator* a, const int32_t* ids, int32_t n_blocks, int64_t n_tokens,
+              int32_t block_size, int32_t* out_ids, int32_t* copy_tokens) {
+  if (!a || !copy_tokens) return fail(FLOWKV_EINVAL, "NULL allocator or output");
+  if (n_blocks < 0 || n_tokens < 0 || block_size < 1)
+    return fail(FLOWKV_EINVAL, "%d blocks of %d tokens, %lld tokens", n_blocks, block_size,
+                (long long)n_tokens);
+  if (n_tokens > int64_t(n_blocks) * block_size)
+    return fail(FLOWKV_EINVAL, "%lld tokens in %d blocks of %d", (long long)n_tokens, n_blocks,
+                block_size);
+  const int32_t full = int32_t(n_tokens / block_size), rest = int32_t(n_tokens % block_size);
+  const int32_t all = full + (rest > 0);
+  if (all > 0 && (!ids || !out_ids)) return fail(FLOWKV_EINVAL, "NULL block list");
+  int rc = check_ids(a, ids, all, /*want_used=*/true);
+  if (rc) return rc;
+  if (rest > 0 && a->free_blocks < 1) return fail(FLOWKV_ENOSPC, "no free block");
+  rc = share_impl(a, ids, full);
+  if (rc) return rc;
+  int32_t own = 0;
+  if (rest > 0) {
+    rc = alloc_impl(a, 1, &own);
+    if (rc) return rc;
+  }
+  std::copy(ids, ids + full, out_ids);
+  if (rest > 0) out_ids[full] = own;
+  *copy_tokens = rest;
+  return ok();
+}
+
+int compact_impl(flowkv_allocator* a, int32_t cap, int32_t* src_ids, int32_t* dst_ids,
+                 int32_t* n_moves) {
+  if (!a || !n_moves) return fail(FLOWKV_EINVAL, "NULL allocator or n_moves");
+  if (cap < 0) return fail(FLOWKV_EINVAL, "negative capacity %d", cap);
+  if (cap > 0 && (!src_ids || !dst_ids)) return fail(FLOWKV_EINVAL, "NULL move list");
+  const int32_t live = int32_t(a->num_blocks - a->free_blocks);
+  int32_t need = 0;  // holes below `live`: as many as blocks in use from there on
+  for (int32_t b = 0; b < live; ++b) need += !a->used[b];
+  if (need > cap) {
+    *n_moves = need;
+    return fail(FLOWKV_ECAP, "%d moves, room for %d", need, cap);
+  }
+  if (need > 0) {
+    for (int32_t b = 0, i = 0; b < live; ++b)
+      if (!a->used[b]) dst_ids[i++] = b;
+    for (int32_t b = live, i = 0; i < need; ++b)
+      if (a->used[b]) src_ids[i++] = b;
+    for (int32_t i = 0; i < need; ++i) {
+      a->used[dst_ids[i]] = 1;
+      a->used[src_ids[i]] = 0;
+      if (!a->extra.empty()) std::swap(a->extra[dst_ids[i]], a->extra[src_ids[i]]);
+    }
+    if (a->policy == FLOWKV_POLICY_SEGMENT) {
+      a->by_start.clear();
+      a->by_len.clear();
+      a->insert_run(live, a->num_blocks - live);
+    } else {
+      std::deque<int32_t> kept;
+      for (int32_t b : a->fifo)
+        if (!a->used[b]) kept.push_back(b);
+      kept.insert(kept.end(), src_ids, src_ids + need);
+      a->fifo.swap(kept);
+    }
+  }
+  *n_moves = need;
+  return ok();
+}
+
 }  // namespace
+
+extern "C" int flowkv_share(flowkv_allocator* a, const int32_t* ids, int32_t n) {
+  return flowkv::guarded([&] { return share_impl(a, ids, n); });
+}
+
+extern "C" int flowkv_owners(const flowkv_allocator* a, const int32_t* ids, int32_t n,
+                             int32_t* counts) {
+  if (!a) return fail(FLOWKV_EINVAL, "NULL allocator");
+  if (n < 0) return fail(FLOWKV_EINVAL, "negative block count %d", n);
+  if (n > 0 && (!ids || !counts)) return fail(FLOWKV_EINVAL, "NULL block or count list");
+  for (int32_t i = 0; i < n; ++i)
+    if (ids[i] < 0 || ids[i] >= a->num_blocks)
+      return fail(FLOWKV_ERANGE, "block %d outside [0, %d)", ids[i], a->num_blocks);
+  for (int32_t i = 0; i < n; ++i)
+    counts[i] = !a->used[ids[i]] ? 0 : 1 + (a->extra.empty() ? 0 : a->extra[ids[i]]);
+  return ok();
+}
+
+extern "C" int flowkv_fork(flowkv_allocator* a, const int32_t* ids, int32_t n_blocks,
+                           int64_t n_tokens, int32_t block_size, int32_t* out_ids,
+                           int32_t* copy_tokens) {
+  return flowkv::guarded(
+      [&] { return fork_impl(a, ids, n_blocks, n_tokens, block_size, out_ids, copy_tokens); });
+}
+
+extern "C" int flowkv_compact(flowkv_allocator* a, int32_t cap, int32_t* src_ids,
+                              int32_t* dst_ids, int32_t* n_moves) {
+  return flowkv::guarded([&] { return compact_impl(a, cap, src_ids, dst_ids, n_moves); });
+}
 
 extern "C" int flowkv_alloc(flowkv_allocator* a, int32_t n, int32_t* out_ids) {
   return flowkv::guarded([&] { return alloc_impl(a, n, out_ids); });

@@ -1,0 +1,377 @@
+// Writing into the pages of a pool, for gfx950 (MI355X): new tokens' K and V
+// appended to their requests' blocks, and blocks copied within one pool.
+//
+// Both move bytes and interpret none.  The pool is either layout of FlowKV's
+// Eq. 5 (arXiv 2504.03775, section 3.3).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <vector>
+
+#include "flowkv.h"
+#include "flowkv_device.h"
+#include "flowkv_ragged.h"
+#include "flowkv_status.h"
+
+using flowkv::fail;
+using flowkv::ok;
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(1))) u32x4 gvec;
+typedef __attribute__((address_space(1))) const u32x4 cgvec;
+
+// ---- append --------------------------------------------------------------------
+
+struct AppendArgs {
+  char* kbase;              // the layer's K of block 0
+  int64_t voff;             // V from K
+  int64_t bstride;          // bytes between blocks
+  const char* k;
+  const char* v;
+  int64_t k_stride, v_stride;   // bytes between tokens
+  const int32_t* offsets;
+  const int32_t* seq_lens;
+  const int32_t* tables;
+  int32_t n_tokens, n_req, max_blocks, pool_blocks, block_size;
+  int32_t pieces;           // 16-byte pieces of a slot
+};
+
+// Token i of request r goes to position p = seq_lens[r] - new[r] + (i - offsets[r]),
+// new[r] = offsets[r + 1] - offsets[r]: slot p % bs of block tables[r][p / bs].
+// A token outside every request or with a negative position, past its block list
+// or with a block outside the pool is dropped.
+//
+// Work: the 16-byte pieces of all tokens' K and V, in order; a wave takes 64
+// consecutive ones kAppendUnroll times.  What bounds it: up to a few thousand
+// tokens a launch and three dependent loads (the offsets, the length, the table
+// entry); the data's own loads are under way meanwhile.
+constexpr int kAppendThreads = 256;
+constexpr int kAppendUnroll = 4;
+
+__global__ __launch_bounds__(kAppendThreads) void kv_append(const AppendArgs a) {
+  const int ln = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t first =
+      (int64_t(blockIdx.x) * (kAppendThreads / 64) + wave) * (64 * kAppendUnroll);
+  const uint32_t per = 2 * uint32_t(a.pieces);       // pieces of a token
+  const int64_t items = int64_t(a.n_tokens) * per;
+  if (first >= items) return;
+  const int64_t last = std::min<int64_t>(first + 64 * kAppendUnroll, items) - 1;
+  const int32_t t0 = int32_t(first / per), t1 = int32_t(last / per);
+  const uint32_t rem0 = uint32_t(first - int64_t(t0) * per);
+
+  u32x4 x[kAppendUnroll];
+  int32_t token[kAppendUnroll];
+  uint32_t piece[kAppendUnroll];                     // of K, then of V
+#pragma unroll
+  for (int u = 0; u < kAppendUnroll; ++u) {
+    const int64_t i = first + u * 64 + ln;
+    const uint32_t d = rem0 + u * 64 + ln;
+    token[u] = i < items ? t0 + int32_t(d / per) : t1;
+    piece[u] = i < items ? d % per : 0;
+    const bool v = piece[u] >= uint32_t(a.pieces);
+    const char* src = v ? a.v + token[u] * a.v_stride + int64_t(piece[u] - a.pieces) * 16
+                        : a.k + token[u] * a.k_stride + int64_t(piece[u]) * 16;
+    x[u] = *(cgvec*)src;
+  }
+  const int32_t r0 = flowkv::last_at_most(a.n_req, t0, [&](int32_t r) { return a.offsets[r]; });
+  const int32_t r1 =
+      t1 == t0 ? r0
+               : flowkv::last_at_most(a.n_req, t1, [&](int32_t r) { return a.offsets[r]; });
+#pragma unroll
+  for (int u = 0; u < kAppendUnroll; ++u) {
+    int32_t r = r0;
+    if (r1 != r0) {                                  // uniform
+      int32_t hi = r1 + 1;                           // the last in [r0, r1] at most token
+      while (hi - r > 1) {
+        const int32_t mid = r + (hi - r) / 2;
+        if (a.offsets[mid] <= token[u]) r = mid;
+        else hi = mid;
+      }
+    }
+    const int32_t begin = a.offsets[r], end = a.offsets[r + 1];
+    const int64_t p = int64_t(a.seq_lens[r]) - (int64_t(end) - begin) + (token[u] - begin);
+    const uint64_t b = uint64_t(p) / uint32_t(a.block_size);
+    const bool in = first + u * 64 + ln < items && token[u] >= begin && token[u] < end && p >= 0 &&
+                    b < uint64_t(a.max_blocks);
+    const int32_t id = in ? a.tables[int64_t(r) * a.max_blocks + int64_t(b)] : -1;
+    if (id < 0 || id >= a.pool_blocks) continue;
+    const bool v = piece[u] >= uint32_t(a.pieces);
+    const int64_t slot = p - int64_t(b) * a.block_size;
+    char* dst = a.kbase + (v ? a.voff : 0) + id * a.bstride +
+                (slot * a.pieces + (v ? piece[u] - a.pieces : piece[u])) * 16;
+    *(gvec*)dst = x[u];
+  }
+}
+
+// ---- copies within a pool --------------------------------------------------------
+
+struct PairOf {
+  int32_t src, dst;
+};
+struct PairTokens {
+  int32_t src, dst, tokens;
+};
+
+template <class Rec, int kBases, int kRecs>
+struct CopyArgs {
+  typedef Rec Record;
+  static constexpr int kMaxBases = kBases;
+  static constexpr int kMaxRecs = kRecs;
+  int64_t chunk_bytes, block_bytes;   // H, 2 L H
+  int64_t num_blocks;
+  int32_t n;                          // records
+  int32_t num_layers;
+  int32_t slot_pieces;                // 16-byte pieces of a slot (token counts only)
+  int32_t tiles;                      // of a whole block
+  int64_t perm_mul;
+  char* base[kBases];
+  Rec rec[kRecs];
+};
+// The records travel in the kernel arguments, as many as a 4 KiB segment holds
+// beside the base pointers; a longer list takes several launches.
+using CopyBM = CopyArgs<PairOf, 1, 460>;
+using CopyLM = CopyArgs<PairOf, FLOWKV_MAX_LAYERS, 330>;
+using CopyTokensBM = CopyArgs<PairTokens, 1, 300>;
+using CopyTokensLM = CopyArgs<PairTokens, FLOWKV_MAX_LAYERS, 220>;
+constexpr size_t kImplicitArgBytes = 256;
+static_assert(sizeof(CopyBM) + kImplicitArgBytes <= 4096, "kernel arguments");
+static_assert(sizeof(CopyLM) + kImplicitArgBytes <= 4096, "kernel arguments");
+static_assert(sizeof(CopyTokensBM) + kImplicitArgBytes <= 4096, "kernel arguments");
+static_assert(sizeof(CopyTokensLM) + kImplicitArgBytes <= 4096, "kernel arguments");
+
+constexpr int kCopyUnroll = 4;
+
+// A record's bytes: the first `tokens` slots (all of them without token counts)
+// of each of its 2 L chunks, taken as one span of 16-byte pieces, tile by tile.
+template <class A, bool kLM>
+__global__ __launch_bounds__(1024) void kv_block_copy(const A a) {
+  constexpr bool kTokens = sizeof(typename A::Record) == sizeof(PairTokens);
+  __shared__ char* s_base[kLM ? FLOWKV_MAX_LAYERS : 1];
+  const uint32_t line = blockDim.x;
+  // blocks scattered (x -> x m mod n, m coprime to n): tile-major in a block-major
+  // pool, a block's tiles together in a layer-major one
+  const uint32_t u = blockIdx.x;
+  const uint32_t t = kLM ? u % uint32_t(a.tiles) : u / uint32_t(a.n);
+  const uint32_t i0 = kLM ? u / uint32_t(a.tiles) : u % uint32_t(a.n);
+  const uint32_t i = uint32_t(uint64_t(i0) * uint64_t(a.perm_mul) % uint32_t(a.n));
+  const int64_t src = a.rec[i].src, dst = a.rec[i].dst;
+  uint32_t chunk = uint32_t(a.chunk_bytes / 16);     // pieces moved of a chunk
+  if constexpr (kTokens) chunk = uint32_t(a.rec[i].tokens) * uint32_t(a.slot_pieces);
+  const uint32_t span = chunk * 2u * uint32_t(a.num_layers);
+  const uint32_t o0 = t * (line * kCopyUnroll);
+  if (o0 >= span) return;
+  if constexpr (kLM) {
+    for (uint32_t l = threadIdx.x; l < uint32_t(a.num_layers); l += blockDim.x)
+      s_base[l] = a.base[l];
+    __syncthreads();
+  }
+  auto at = [&](int64_t block, uint32_t o) -> char* {
+    if constexpr (!kLM && !kTokens) {
+      return a.base[0] + block * a.block_bytes + int64_t(o) * 16;
+    } else {
+      const uint32_t c = o / chunk, w = o - c * chunk;
+      if constexpr (kLM)
+        return s_base[c >> 1] + (int64_t(c & 1) * a.num_blocks + block) * a.chunk_bytes +
+               int64_t(w) * 16;
+      else
+        return a.base[0] + block * a.block_bytes + int64_t(c) * a.chunk_bytes + int64_t(w) * 16;
+    }
+  };
+  u32x4 x[kCopyUnroll];
+#pragma unroll
+  for (int k = 0; k < kCopyUnroll; ++k) {
+    const uint32_t o = o0 + k * line + threadIdx.x;
+    if (o < span) x[k] = __builtin_nontemporal_load((cgvec*)at(src, o));
+  }
+#pragma unroll
+  for (int k = 0; k < kCopyUnroll; ++k) {
+    const uint32_t o = o0 + k * line + threadIdx.x;
+    if (o < span) __builtin_nontemporal_store(x[k], (gvec*)at(dst, o));
+  }
+}
+
+// The pool's descriptor, as every call here checks it.
+int check_pool(const flowkv_pool* p) {
+  if (!p) return fail(FLOWKV_EINVAL, "NULL pool");
+  if (p->layout != FLOWKV_LAYOUT_LAYER_MAJOR && p->layout != FLOWKV_LAYOUT_BLOCK_MAJOR)
+    return fail(FLOWKV_EINVAL, "unknown layout %d", p->layout);
+  if (p->num_layers < 1 || p->num_layers > FLOWKV_MAX_LAYERS)
+    return fail(FLOWKV_EINVAL, "%d layers, need 1..%d", p->num_layers, FLOWKV_MAX_LAYERS);
+  if (p->num_blocks < 1) return fail(FLOWKV_EINVAL, "%d blocks", p->num_blocks);
+  if (p->reserved != 0) return fail(FLOWKV_EINVAL, "reserved field not 0");
+  if (p->chunk_bytes <= 0 || p->chunk_bytes % 16)
+    return fail(FLOWKV_EINVAL, "chunk_bytes %lld not a positive multiple of 16",
+                (long long)p->chunk_bytes);
+  if (p->chunk_bytes >= (int64_t(1) << 31) / (2 * int64_t(p->num_layers)))
+    return fail(FLOWKV_EINVAL, "block of %d x 2 chunks of %lld bytes, limit 2 GiB", p->num_layers,
+                (long long)p->chunk_bytes);
+  if (!p->layer_base) return fail(FLOWKV_EINVAL, "NULL layer_base");
+  const int nb = p->layout == FLOWKV_LAYOUT_LAYER_MAJOR ? p->num_layers : 1;
+  for (int i = 0; i < nb; ++i)
+    if (!p->layer_base[i] || reinterpret_cast<uintptr_t>(p->layer_base[i]) % 16)
+      return fail(FLOWKV_EINVAL, "pool base pointer %d NULL or not 16-byte aligned", i);
+  return FLOWKV_OK;
+}
+
+}  // namespace
+
+extern "C" int flowkv_append(const flowkv_pool* pool, int32_t layer, const void* k_dev,
+                             int64_t k_stride, const void* v_dev, int64_t v_stride,
+                             int64_t slot_bytes, int32_t n_tokens, int32_t n_req,
+                             const int32_t* offsets_dev, const int32_t* block_tables_dev,
+                             int32_t max_blocks, const int32_t* seq_lens_dev, void* hip_stream) {
+  int rc = check_pool(pool);
+  if (rc) return rc;
+  if (layer < 0 || layer >= pool->num_layers)
+    return fail(FLOWKV_EINVAL, "layer %d outside the pool's %d layers", layer, pool->num_layers);
+  if (slot_bytes <= 0 || slot_bytes % 16 || pool->chunk_bytes % slot_bytes)
+    return fail(FLOWKV_EINVAL,
+                "slot of %lld bytes: need a multiple of 16 that divides chunk_bytes %lld",
+                (long long)slot_bytes, (long long)pool->chunk_bytes);
+  if (n_tokens < 0 || n_req < 0 || max_blocks < 0) return fail(FLOWKV_EINVAL, "negative sizes");
+  if (n_tokens == 0 || n_req == 0) return ok();
+  if (!k_dev || !v_dev || !offsets_dev || !seq_lens_dev || (max_blocks > 0 && !block_tables_dev))
+    return fail(FLOWKV_EINVAL, "NULL device pointer");
+  if (reinterpret_cast<uintptr_t>(k_dev) % 16 || reinterpret_cast<uintptr_t>(v_dev) % 16 ||
+      k_stride % 16 || v_stride % 16)
+    return fail(FLOWKV_EINVAL, "K and V need 16-byte alignment and strides of whole 16 bytes");
+  if (n_tokens > 1 && (k_stride < slot_bytes || v_stride < slot_bytes))
+    return fail(FLOWKV_EINVAL, "token strides of %lld and %lld bytes, a token has %lld",
+                (long long)k_stride, (long long)v_stride, (long long)slot_bytes);
+  const bool lm = pool->layout == FLOWKV_LAYOUT_LAYER_MAJOR;
+  AppendArgs a{};
+  a.kbase = static_cast<char*>(pool->layer_base[lm ? layer : 0]) +
+            (lm ? 0 : int64_t(layer) * 2 * pool->chunk_bytes);
+  a.voff = lm ? int64_t(pool->num_blocks) * pool->chunk_bytes : pool->chunk_bytes;
+  a.bstride = lm ? pool->chunk_bytes : 2 * int64_t(pool->num_layers) * pool->chunk_bytes;
+  a.k = static_cast<const char*>(k_dev);
+  a.v = static_cast<const char*>(v_dev);
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.offsets = offsets_dev;
+  a.seq_lens = seq_lens_dev;
+  a.tables = block_tables_dev;
+  a.n_tokens = n_tokens;
+  a.n_req = n_req;
+  a.max_blocks = max_blocks;
+  a.pool_blocks = pool->num_blocks;
+  a.block_size = int32_t(pool->chunk_bytes / slot_bytes);
+  a.pieces = int32_t(slot_bytes / 16);
+  const int64_t per_group = int64_t(kAppendThreads) * kAppendUnroll;
+  const int64_t groups = (int64_t(n_tokens) * 2 * a.pieces + per_group - 1) / per_group;
+  if (groups > INT32_MAX)
+    return fail(FLOWKV_EINVAL, "%d tokens of %lld bytes: too many for one call", n_tokens,
+                (long long)slot_bytes);
+  void* args[] = {&a};
+  hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kv_append), dim3(unsigned(groups)),
+                                 dim3(kAppendThreads), args, 0,
+                                 static_cast<hipStream_t>(hip_stream));
+  if (e == hipSuccess) e = hipGetLastError();
+  if (e != hipSuccess) return fail(FLOWKV_EHIP, "append launch: %s", hipGetErrorString(e));
+  return ok();
+}
+
+namespace {
+
+// Every destination once, and no destination among the sources: the pairs can
+// then be copied in any order, in any number of launches.
+int check_pairs(const int32_t* src, const int32_t* dst, int32_t n, int32_t blocks) {
+  std::vector<uint8_t> is_dst(size_t(blocks), 0);
+  for (int32_t i = 0; i < n; ++i) {
+    for (const int32_t* ids : {src, dst})
+      if (ids[i] < 0 || ids[i] >= blocks)
+        return fail(FLOWKV_ERANGE, "block %d at position %d outside [0, %d)", ids[i], i, blocks);
+    if (is_dst[size_t(dst[i])])
+      return fail(FLOWKV_EDUP, "block %d is a destination twice (position %d)", dst[i], i);
+    is_dst[size_t(dst[i])] = 1;
+  }
+  for (int32_t i = 0; i < n; ++i)
+    if (is_dst[size_t(src[i])])
+      return fail(FLOWKV_EDUP, "block %d at position %d is a source and a destination", src[i], i);
+  return FLOWKV_OK;
+}
+
+template <class A, bool kLM>
+int launch_copy(const flowkv_pool* p, const int32_t* src, const int32_t* dst,
+                const int32_t* tokens, int32_t n, int64_t slot_bytes, void* stream) {
+  constexpr bool kTokens = sizeof(typename A::Record) == sizeof(PairTokens);
+  const int64_t span = 2 * int64_t(p->num_layers) * p->chunk_bytes;
+  A a{};
+  a.chunk_bytes = p->chunk_bytes;
+  a.block_bytes = span;
+  a.num_blocks = p->num_blocks;
+  a.num_layers = p->num_layers;
+  a.slot_pieces = int32_t(slot_bytes / 16);
+  for (int i = 0; i < (kLM ? p->num_layers : 1); ++i)
+    a.base[i] = static_cast<char*>(p->layer_base[i]);
+  const int threads = 1024;
+  for (int32_t at = 0; at < n; at += A::kMaxRecs) {
+    const int32_t m = std::min<int32_t>(n - at, A::kMaxRecs);
+    int64_t most = span;
+    if constexpr (kTokens) most = 0;
+    for (int32_t i = 0; i < m; ++i) {
+      a.rec[i].src = src[at + i];
+      a.rec[i].dst = dst[at + i];
+      if constexpr (kTokens) {
+        a.rec[i].tokens = tokens[at + i];
+        most = std::max(most, 2 * int64_t(p->num_layers) * tokens[at + i] * slot_bytes);
+      }
+    }
+    if (most == 0) continue;
+    const int64_t tile = int64_t(threads) * kCopyUnroll * 16;
+    a.n = m;
+    a.tiles = int32_t((most + tile - 1) / tile);
+    a.perm_mul = int64_t(2654435761ull % uint64_t(m));   // a prime above m: a bijection mod m
+    void* args[] = {&a};
+    hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kv_block_copy<A, kLM>),
+                                   dim3(unsigned(a.tiles) * unsigned(m)), dim3(threads), args, 0,
+                                   static_cast<hipStream_t>(stream));
+    if (e == hipSuccess) e = hipGetLastError();
+    if (e != hipSuccess) return fail(FLOWKV_EHIP, "block copy launch: %s", hipGetErrorString(e));
+  }
+  return ok();
+}
+
+int copy_impl(const flowkv_pool* pool, const int32_t* src_ids, const int32_t* dst_ids,
+              const int32_t* tokens, int32_t n_blocks, int64_t slot_bytes, void* stream) {
+  int rc = check_pool(pool);
+  if (rc) return rc;
+  if (n_blocks < 0) return fail(FLOWKV_EINVAL, "negative block count %d", n_blocks);
+  if (tokens) {
+    if (slot_bytes <= 0 || slot_bytes % 16 || pool->chunk_bytes % slot_bytes)
+      return fail(FLOWKV_EINVAL,
+                  "slot of %lld bytes: need a multiple of 16 that divides chunk_bytes %lld",
+                  (long long)slot_bytes, (long long)pool->chunk_bytes);
+    const int64_t bs = pool->chunk_bytes / slot_bytes;
+    for (int32_t i = 0; i < n_blocks; ++i)
+      if (tokens[i] < 0 || tokens[i] > bs)
+        return fail(FLOWKV_EINVAL, "%d tokens at position %d, a block holds %lld", tokens[i], i,
+                    (long long)bs);
+  }
+  if (n_blocks == 0) return ok();
+  if (!src_ids || !dst_ids) return fail(FLOWKV_EINVAL, "NULL block list");
+  rc = check_pairs(src_ids, dst_ids, n_blocks, pool->num_blocks);
+  if (rc) return rc;
+  const bool lm = pool->layout == FLOWKV_LAYOUT_LAYER_MAJOR;
+  if (tokens)
+    return lm ? launch_copy<CopyTokensLM, true>(pool, src_ids, dst_ids, tokens, n_blocks,
+                                                slot_bytes, stream)
+              : launch_copy<CopyTokensBM, false>(pool, src_ids, dst_ids, tokens, n_blocks,
+                                                 slot_bytes, stream);
+  return lm ? launch_copy<CopyLM, true>(pool, src_ids, dst_ids, nullptr, n_blocks, 16, stream)
+            : launch_copy<CopyBM, false>(pool, src_ids, dst_ids, nullptr, n_blocks, 16, stream);
+}
+
+}  // namespace
+
+extern "C" int flowkv_copy_blocks(const flowkv_pool* pool, const int32_t* src_ids,
+                                  const int32_t* dst_ids, const int32_t* tokens,
+                                  int32_t n_blocks, int64_t slot_bytes, void* hip_stream) {
+  return flowkv::guarded([&] {
+    return copy_impl(pool, src_ids, dst_ids, tokens, n_blocks, slot_bytes, hip_stream);
+  });
+}

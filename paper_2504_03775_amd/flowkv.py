@@ -134,6 +134,30 @@ SIGNATURES = {
                                                        ctypes.c_int32,
                                                        ctypes.c_float, ctypes.c_int32,
                                                        ctypes.c_void_p, ctypes.c_void_p]),
+    "flowkv_share": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32]),
+    "flowkv_owners": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                     ctypes.c_void_p]),
+    "flowkv_fork": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                   ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, _I32P]),
+    "flowkv_compact": (ctypes.c_int, [ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+                                      ctypes.c_void_p, _I32P]),
+    "flowkv_append": (ctypes.c_int, [_POOLP, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64,
+                                     ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64,
+                                     ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                                     ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+                                     ctypes.c_void_p]),
+    "flowkv_chunk_attention": (ctypes.c_int, [_POOLP, ctypes.c_int32, ctypes.c_void_p,
+                                              ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                                              ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                              ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32,
+                                              ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32,
+                                              ctypes.c_float, ctypes.c_int32, ctypes.c_void_p,
+                                              ctypes.c_void_p, ctypes.c_int64,
+                                              ctypes.c_void_p]),
+    "flowkv_chunk_attention_workspace": (ctypes.c_int, [ctypes.c_int32] * 8 + [_I64P]),
+    "flowkv_copy_blocks": (ctypes.c_int, [_POOLP, ctypes.c_void_p, ctypes.c_void_p,
+                                          ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
+                                          ctypes.c_void_p]),
     "flowkv_sched_create": (ctypes.c_int, [ctypes.POINTER(flowkv_sched_params), ctypes.c_int32,
                                            ctypes.c_void_p, ctypes.POINTER(ctypes.c_void_p)]),
     "flowkv_sched_destroy": (None, [ctypes.c_void_p]),
@@ -263,6 +287,42 @@ def flowkv_allocator_stats(h) -> dict:
             "largest_free": st.largest_free}
 
 
+def flowkv_share(h, ids) -> None:
+    """One more owner for each block of the list (``flowkv_free`` takes one off)."""
+    ids = _i32(ids)
+    _check(_lib.flowkv_share(h, _ptr(ids), ids.size), "flowkv_share")
+
+
+def flowkv_owners(h, ids) -> np.ndarray:
+    ids = _i32(ids)
+    out = np.zeros(ids.size, dtype=np.int32)
+    _check(_lib.flowkv_owners(h, _ptr(ids), ids.size, _ptr(out)), "flowkv_owners")
+    return out
+
+
+def flowkv_fork(h, ids, n_tokens: int, block_size: int):
+    """(block list, tokens to copy) of a second continuation of a request with
+    n_tokens tokens in ``ids``: with k = n_tokens // block_size full blocks
+    shared, ``flowkv_copy_blocks(pool, ids[k:k + 1], list[k:], [tokens])`` fills
+    its part-filled last one (no copy where tokens is 0)."""
+    ids = _i32(ids)
+    out = np.empty(ids.size, dtype=np.int32)
+    tokens = ctypes.c_int32()
+    _check(_lib.flowkv_fork(h, _ptr(ids), ids.size, n_tokens, block_size, _ptr(out),
+                            ctypes.byref(tokens)), "flowkv_fork")
+    return out[: -(-n_tokens // block_size)], tokens.value
+
+
+def flowkv_compact(h, cap: int):
+    """(sources, destinations) of the moves that leave one free run at the
+    pool's end; the allocator counts them as made, the caller copies the blocks
+    (``flowkv_copy_blocks``) and renames them in its lists."""
+    src, dst = np.empty(max(cap, 0), dtype=np.int32), np.empty(max(cap, 0), dtype=np.int32)
+    n = ctypes.c_int32()
+    _check(_lib.flowkv_compact(h, cap, _ptr(src), _ptr(dst), ctypes.byref(n)), "flowkv_compact")
+    return src[: n.value], dst[: n.value]
+
+
 class Allocator:
     """Owner of one allocator handle."""
 
@@ -285,6 +345,18 @@ class Allocator:
 
     def mark_used(self, ids) -> None:
         flowkv_mark_used(self._h, ids)
+
+    def share(self, ids) -> None:
+        flowkv_share(self._h, ids)
+
+    def owners(self, ids) -> np.ndarray:
+        return flowkv_owners(self._h, ids)
+
+    def fork(self, ids, n_tokens: int, block_size: int):
+        return flowkv_fork(self._h, ids, n_tokens, block_size)
+
+    def compact(self):
+        return flowkv_compact(self._h, self.num_blocks)
 
     def stats(self) -> dict:
         return flowkv_allocator_stats(self._h)
@@ -646,6 +718,132 @@ def flowkv_decode_attention(pool: KVPool, layer: int, q, block_tables, seq_lens,
         ctypes.c_void_p(out.data_ptr()), ctypes.c_void_p(workspace.data_ptr()),
         workspace.numel() * workspace.element_size(), ctypes.c_void_p(_stream_handle(stream))),
         "flowkv_decode_attention")
+
+
+def _on_pool_device(pool: KVPool, stream, call, where: str) -> None:
+    """``call(stream handle)`` with the pool's device current."""
+    import torch
+
+    if stream is not None and stream.device != pool.device:
+        raise ValueError(f"{where}: the stream is on {stream.device}, the pool on {pool.device}")
+    if pool.device.index == torch.cuda.current_device():
+        _check(call(ctypes.c_void_p(_stream_handle(stream))), where)
+    else:
+        with torch.cuda.device(pool.device):
+            _check(call(ctypes.c_void_p(_stream_handle(stream))), where)
+
+
+def _check_ragged(pool: KVPool, q_offsets, block_tables, seq_lens) -> int:
+    """The batch arrays of flowkv_append and flowkv_chunk_attention; the requests' count."""
+    import torch
+
+    n = seq_lens.numel()
+    for t, dims in ((q_offsets, 1), (block_tables, 2), (seq_lens, 1)):
+        if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() \
+                or t.device != pool.device:
+            raise ValueError(f"q_offsets, block_tables and seq_lens: need contiguous int32 tensors "
+                             f"of 1, 2 and 1 dimensions on {pool.device}, got {t.dtype} "
+                             f"{tuple(t.shape)} on {t.device}")
+    if q_offsets.numel() != n + 1 or block_tables.shape[0] != n:
+        raise ValueError(f"{n} lengths, {q_offsets.numel()} offsets (one more is needed) and "
+                         f"{block_tables.shape[0]} block lists")
+    return n
+
+
+def _token_stride(t, name: str, shape, dtype, device) -> int:
+    """Elements between the tokens of a (n, heads, head_dim) tensor whose tokens
+    are each in one piece."""
+    if t.dim() != 3 or tuple(t.shape[1:]) != tuple(shape) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name}: need (tokens, {shape[0]}, {shape[1]}) {dtype} on {device}, got "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.numel() and (t.stride(2) != 1 or (shape[0] > 1 and t.stride(1) != shape[1])):
+        raise ValueError(f"{name}: a token's heads must lie together, strides are {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else shape[0] * shape[1]
+
+
+def flowkv_append(pool: KVPool, layer: int, k, v, q_offsets, block_tables, seq_lens,
+                  stream=None) -> None:
+    """Write new tokens' K and V of layer `layer` into the pool.  k, v: (n, Hkv,
+    Dh) of the pool's element type, the tokens of one request after another at
+    any stride of whole 16 bytes (columns of a joint projection, say);
+    q_offsets (n_req + 1,), block_tables (n_req, max_blocks) and seq_lens
+    (n_req,) int32 on the pool's device, the lengths counted with the new
+    tokens."""
+    n_req = _check_ragged(pool, q_offsets, block_tables, seq_lens)
+    shape, dtype = (pool.kv_heads, pool.head_dim), pool.tensors[0].dtype
+    ks = _token_stride(k, "k", shape, dtype, pool.device)
+    vs = _token_stride(v, "v", shape, dtype, pool.device)
+    if k.shape[0] != v.shape[0]:
+        raise ValueError(f"{k.shape[0]} tokens of K and {v.shape[0]} of V")
+    e = pool.elem_bytes
+    _on_pool_device(pool, stream, lambda s: _lib.flowkv_append(
+        ctypes.byref(pool.desc), layer, ctypes.c_void_p(k.data_ptr()), ks * e,
+        ctypes.c_void_p(v.data_ptr()), vs * e, pool.kv_heads * pool.head_dim * e, k.shape[0], n_req,
+        ctypes.c_void_p(q_offsets.data_ptr()), ctypes.c_void_p(block_tables.data_ptr()),
+        block_tables.shape[1], ctypes.c_void_p(seq_lens.data_ptr()), s), "flowkv_append")
+
+
+def flowkv_chunk_attention_workspace(n_tokens: int, n_req: int, q_heads: int, kv_heads: int,
+                                     head_dim: int, max_new: int, max_seq_len: int,
+                                     split_tokens: int = 0) -> int:
+    b = ctypes.c_int64()
+    _check(_lib.flowkv_chunk_attention_workspace(n_tokens, n_req, q_heads, kv_heads, head_dim,
+                                                 max_new, max_seq_len, split_tokens,
+                                                 ctypes.byref(b)),
+           "flowkv_chunk_attention_workspace")
+    return b.value
+
+
+def flowkv_chunk_attention(pool: KVPool, layer: int, q, q_offsets, block_tables, seq_lens,
+                           max_new: int, max_seq_len: int, scale: float, out, workspace=None,
+                           split_tokens: int = 0, stream=None) -> None:
+    """Attention of new tokens over layer `layer` of a bfloat16 pool that holds
+    their K and V already (``flowkv_append``), each up to its own position.  q:
+    (n, Hq, Dh) bf16, laid out and strided as ``flowkv_append``'s k; q_offsets,
+    block_tables and seq_lens as there; out: (n, Hq, Dh) bf16, contiguous;
+    workspace: uint8, ``flowkv_chunk_attention_workspace`` bytes (None where
+    that is 0)."""
+    import torch
+
+    n_req = _check_ragged(pool, q_offsets, block_tables, seq_lens)
+    if any(t.dtype != torch.bfloat16 for t in pool.tensors):
+        raise ValueError(f"attention reads bfloat16 K/V: the pool holds {pool.tensors[0].dtype}")
+    if q.dim() != 3:
+        raise ValueError(f"q: need (tokens, heads, head_dim), got {tuple(q.shape)}")
+    n, hq, dh = q.shape
+    if dh != pool.head_dim:
+        raise ValueError(f"q has a head_dim of {dh}, the pool of {pool.head_dim}")
+    qs = _token_stride(q, "q", (hq, dh), torch.bfloat16, pool.device)
+    if tuple(out.shape) != (n, hq, dh) or out.dtype != torch.bfloat16 or not out.is_contiguous() \
+            or out.device != pool.device:
+        raise ValueError(f"out: need contiguous {(n, hq, dh)} bfloat16 on {pool.device}, got "
+                         f"{tuple(out.shape)} {out.dtype} on {out.device}")
+    ws, ws_bytes = 0, 0
+    if workspace is not None:
+        if not workspace.is_contiguous() or workspace.device != pool.device:
+            raise ValueError("attention workspace: not a contiguous tensor on the pool's device")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _on_pool_device(pool, stream, lambda s: _lib.flowkv_chunk_attention(
+        ctypes.byref(pool.desc), layer, ctypes.c_void_p(q.data_ptr()), qs, n, n_req, hq,
+        pool.kv_heads, dh, ctypes.c_void_p(q_offsets.data_ptr()),
+        ctypes.c_void_p(block_tables.data_ptr()), block_tables.shape[1],
+        ctypes.c_void_p(seq_lens.data_ptr()), max_new, max_seq_len, scale, split_tokens,
+        ctypes.c_void_p(out.data_ptr()), ctypes.c_void_p(ws), ws_bytes, s),
+        "flowkv_chunk_attention")
+
+
+def flowkv_copy_blocks(pool: KVPool, src_ids, dst_ids, tokens=None, stream=None) -> None:
+    """Copy blocks within the pool, every layer's K and V: whole ones, or the
+    first tokens[i] slots of each.  Lists on the host; a source may repeat, a
+    destination may not, nor be a source."""
+    s, d = _i32(src_ids), _i32(dst_ids)
+    k = None if tokens is None else _i32(tokens)
+    if s.ndim != 1 or d.shape != s.shape or (k is not None and k.shape != s.shape):
+        raise ValueError("source, destination and token lists differ in length")
+    slot = pool.kv_heads * pool.head_dim * pool.elem_bytes
+    _on_pool_device(pool, stream, lambda st: _lib.flowkv_copy_blocks(
+        ctypes.byref(pool.desc), _ptr(s), _ptr(d), None if k is None else _ptr(k), s.size, slot,
+        st), "flowkv_copy_blocks")
 
 
 def segments_to_device(segs: np.ndarray, device, stream=None):
