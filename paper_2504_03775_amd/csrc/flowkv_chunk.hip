@@ -50,7 +50,8 @@ struct ChunkArgs {
   const int32_t* tables;                // (n_req, max_blocks)
   uint16_t* out;                        // (n_tokens, Hq, Dh) bf16
   float* ws;                            // the splits' records
-  uint32_t bstride, sstride;            // bytes between blocks, slots
+  uint32_t bunits, sunits;              // 128-byte units between blocks, slots
+  uint32_t bs_magic, bs_shift;          // division by block_size
   int32_t pool_blocks, block_size, max_blocks, max_seq_len;
   int32_t n_tokens, n_req, q_heads, kv_heads, group;
   int32_t tiles, split_tokens, splits;
@@ -108,13 +109,17 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
 }
 
+// 16 bytes that a staged row of a token that cannot be read is made of.
+__device__ const u32x4 g_zeros = {0, 0, 0, 0};
+
 template <int kDh>
 struct ChunkLds {
-  alignas(16) u32x4 k[2][kKeys * kDh / 8];
-  alignas(16) u32x4 v[2][kKeys * kDh / 8];
-  alignas(16) uint32_t flags[2][kWaves];   // by the wave that staged: 1 dead tokens, 2 odd V
-  alignas(16) uint8_t dead[2][kKeys];
+  alignas(16) u32x4 k[kKeys * kDh / 8];
+  alignas(16) u32x4 v[kKeys * kDh / 8];
 };
+
+typedef __attribute__((address_space(1))) const void gvoid;
+typedef __attribute__((address_space(3))) void lvoid;
 
 template <int kDh>
 __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
@@ -159,8 +164,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
   const int64_t wrow = row0 + wave * 32;
   const bool any_row = wrow < rows;
   const int32_t wlast = any_row ? int32_t((wrow + 31 < rows ? wrow + 31 : rows - 1) / a.group) : 0;
-  const int32_t wlim = any_row ? seen(rq, wlast) : 0;
-  const int32_t wleast = any_row ? seen(rq, int32_t(wrow / a.group)) : 0;
+  const int32_t wlim = __builtin_amdgcn_readfirstlane(any_row ? seen(rq, wlast) : 0);
+  const int32_t wleast =
+      __builtin_amdgcn_readfirstlane(any_row ? seen(rq, int32_t(wrow / a.group)) : 0);
 
   bf16x8 qb[kI];
 #pragma unroll
@@ -171,61 +177,45 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
     qb[i] = __builtin_bit_cast(bf16x8, w);
   }
 
-  __shared__ ChunkLds<kDh> lds;
+  __shared__ ChunkLds<kDh> lds0, lds1;
 
-  // staging: lane takes piece lp of the tokens lr + e kLdRows of each tile
+  // Staging: K and V rows go from memory to LDS directly.  An instruction fills 64
+  // consecutive 16-byte places, so a lane's place is fixed, token lr + e kLdRows and
+  // piece lp of its row, and the swizzle is in which piece it reads.
   const int lr = tid / kPc, lp = tid % kPc;
-  const uint32_t bs = uint32_t(a.block_size);
   const int32_t* table = a.tables + int64_t(r) * a.max_blocks;
-  uint32_t sb[kLd], ss[kLd];                     // block and slot of the lane's tokens
-#pragma unroll
-  for (int e = 0; e < kLd; ++e) {
-    const uint32_t t = uint32_t(s0 + lr + e * kLdRows);
-    sb[e] = t / bs;
-    ss[e] = t - sb[e] * bs;
-  }
-  const uint32_t step_b = kKeys / bs, step_s = kKeys - step_b * bs;
-  const char* kb = a.kbase + g * kDh * 2 + 16 * lp;
-  u32x4 kw[kLd], vw[kLd];
-  uint32_t alive;                                // bit e: the lane's token e can be read
-  auto load = [&](int32_t t0) {
-    alive = 0;
-#pragma unroll
-    for (int e = 0; e < kLd; ++e) {
-      const bool in = t0 + lr + e * kLdRows < s1;
-      const int32_t b = table[in ? sb[e] : 0];   // (s1 lies within the block list)
-      const bool good = in && b >= 0 && b < a.pool_blocks;
-      const uint64_t off = good ? uint64_t(uint32_t(b)) * a.bstride + ss[e] * a.sstride : 0;
-      kw[e] = *(cgvec4*)(kb + off);
-      vw[e] = *(cgvec4*)(kb + a.voff + off);
-      alive |= uint32_t(good) << e;
-      ss[e] += step_s;
-      sb[e] += step_b;
-      if (ss[e] >= bs) {
-        ss[e] -= bs;
-        ++sb[e];
-      }
-    }
+  const char* kp = a.kbase + g * kDh * 2 + 16 * (lp ^ (kPc == 16 ? lr & 15 : lr >> 1 & 7));
+  const char* vp = a.kbase + a.voff + g * kDh * 2 +
+                   16 * (lp ^ (kPc == 16 ? (lr & 3) * 4 : (lr >> 1 & 1) * 4));
+  const char* const zeros = reinterpret_cast<const char*>(&g_zeros);
+  // lane ln's token of a tile: block ID, and its row's place in the pool in 128-byte
+  // units (all ones: it cannot be read)
+  uint32_t next_slot;
+  int32_t next_block;
+  bool next_in;
+  auto fetch = [&](int32_t t0) {
+    const uint32_t t = uint32_t(t0 + ln);
+    const uint32_t b = uint32_t((uint64_t(__umulhi(t, a.bs_magic)) + t) >> a.bs_shift);
+    next_slot = t - b * uint32_t(a.block_size);
+    next_in = int32_t(t) < s1;
+    next_block = table[next_in ? b : 0];         // (s1 lies within the block list)
   };
-  auto store = [&](int buf, int32_t t0) {
-    bool dead = false, odd = false;
+  uint64_t dead, next_dead;                      // tokens of a tile whose block is outside
+  auto stage = [&](ChunkLds<kDh>& to) {
+    const bool good = next_in && next_block >= 0 && next_block < a.pool_blocks;
+    next_dead = __ballot(next_in && !good);
+    const uint32_t at =
+        good ? uint32_t(next_block) * a.bunits + next_slot * a.sunits : 0xffffffffu;
 #pragma unroll
     for (int e = 0; e < kLd; ++e) {
-      const int x = lr + e * kLdRows;
-      const bool good = alive >> e & 1;
-      const u32x4 v = good ? vw[e] : u32x4{0, 0, 0, 0};
-      lds.k[buf][x * kPc + (lp ^ (kPc == 16 ? x & 15 : x >> 1 & 7))] = kw[e];
-      lds.v[buf][x * kPc + (lp ^ (kPc == 16 ? (x & 3) * 4 : (x >> 1 & 1) * 4))] = v;
-      const bool gone = !good && t0 + x < s1;    // a block outside the pool
-      if (lp == 0) lds.dead[buf][x] = gone;
-      dead |= gone;
-      if (t0 + kKeys > tile_least)               // some row does not see some token
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          odd |= (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
+      const uint32_t u = __shfl(at, lr + e * kLdRows);
+      const uint64_t off = uint64_t(u) * 128;
+      const char* ks = u != 0xffffffffu ? kp + off : zeros;
+      const char* vs = u != 0xffffffffu ? vp + off : zeros;
+      const int place = e * kThreads + wave * 64;
+      __builtin_amdgcn_global_load_lds((gvoid*)ks, (lvoid*)(to.k + place), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gvoid*)vs, (lvoid*)(to.v + place), 16, 0, 0);
     }
-    const uint32_t f = (__any(dead) ? 1u : 0u) | (__any(odd) ? 2u : 0u);
-    if (ln == 0) lds.flags[buf][wave] = f;
   };
 
   f32x16 o[kB];
@@ -233,48 +223,71 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
   for (int b = 0; b < kB; ++b) o[b] = f32x16{};
   float mref = -INFINITY, lsum = 0.f;            // of the lane's row; its own half of the tokens
 
-  if (s0 < s1) {
-    load(s0);
-    store(0, s0);
-  }
-  __syncthreads();
-  int buf = 0;
-  for (int32_t t0 = s0; t0 < s1; t0 += kKeys, buf ^= 1) {
-    const bool more = t0 + kKeys < s1;
-    if (more) load(t0 + kKeys);
-    if (t0 < wlim) {
-      const u32x4 fl = *reinterpret_cast<const u32x4*>(lds.flags[buf]);
-      const uint32_t flags =
-          __builtin_amdgcn_readfirstlane(fl[0] | fl[1] | fl[2] | fl[3]);
-      // S^T = K Q^T: rows are tokens, columns query rows
-      f32x16 s[2];
+  // Where some row does not see some token, an infinity or a NaN in V would reach it as
+  // 0 x inf: such values are taken out of the tile, and added at the end to the rows
+  // that see them.
+  bool odd = false;
+  auto clean = [&](ChunkLds<kDh>& lds) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        s[b] = f32x16{};
+    for (int e = 0; e < kLd; ++e) {
+      u32x4 w = lds.v[e * kThreads + tid];
+      bool any = false;
 #pragma unroll
-        for (int i = 0; i < kI; ++i) {
-          const int x = 32 * b + c32;
-          const u32x4 w =
-              lds.k[buf][x * kPc + ((2 * i + half) ^ (kPc == 16 ? x & 15 : x >> 1 & 7))];
-          s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), qb[i],
-                                                         s[b], 0, 0, 0);
+      for (int i = 0; i < 4; ++i) {
+        if ((w[i] & 0x7f80u) == 0x7f80u) {
+          w[i] &= 0xffff0000u;
+          any = true;
+        }
+        if ((w[i] & 0x7f800000u) == 0x7f800000u) {
+          w[i] &= 0xffffu;
+          any = true;
         }
       }
-      const bool masked = t0 + kKeys > wleast || (flags & 1);
-      if (masked) {
+      if (any) lds.v[e * kThreads + tid] = w;
+      odd |= any;
+    }
+    __syncthreads();
+  };
+
+  auto step = [&](int32_t t0, ChunkLds<kDh>& lds, ChunkLds<kDh>& other) {
+    dead = next_dead;
+    if (t0 + kKeys > tile_least) clean(lds);     // uniform
+    if (t0 + kKeys < s1) {
+      stage(other);
+      fetch(t0 + 2 * kKeys);
+    }
+    if (t0 < wlim) {
+      // S^T = K Q^T: rows are tokens, columns query rows
+      f32x16 s[2] = {f32x16{}, f32x16{}};
+      u32x4 w[2][kI];
+      auto k_at = [&](int b, int i) {
+        const int x = 32 * b + c32;
+        return lds.k[x * kPc + ((2 * i + half) ^ (kPc == 16 ? x & 15 : x >> 1 & 7))];
+      };
+#pragma unroll
+      for (int i = 0; i < kI; ++i) w[0][i] = k_at(0, i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < kI; ++i) {
+        w[1][i] = k_at(1, i);
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[0][i]), qb[i],
+                                                       s[0], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[1][i]), qb[i],
+                                                       s[1], 0, 0, 0);
+      if (t0 + kKeys > wleast || dead) {
         const int32_t last = lim - t0 - 4 * half;
+        const uint64_t d = dead >> (4 * half);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (32 * b + 8 * (i / 4) + i % 4 >= last) s[b][i] = -INFINITY;
-        if (flags & 1) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (lds.dead[buf][32 * b + 8 * (i / 4) + 4 * half + i % 4]) s[b][i] = -INFINITY;
-        }
+          for (int i = 0; i < 16; ++i) {
+            const int x = 32 * b + 8 * (i / 4) + i % 4;
+            if (x >= last || (d >> x & 1)) s[b][i] = -INFINITY;
+          }
       }
       float mx = s[0][0];
 #pragma unroll
@@ -307,63 +320,51 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
       auto v_at = [&](int b, int j) {
         const int x = 16 * j + 4 * half + (ln & 15) / 4;
         const int col = 32 * b + 16 * (ln >> 4 & 1) + 4 * (ln & 3);   // dim
-        const int at =
-            x * kPc + ((col >> 3) ^ (kPc == 16 ? (x & 3) * 4 : (x >> 1 & 1) * 4));
-        lds4* base = (lds4*)(reinterpret_cast<uint16_t*>(lds.v[buf]) + at * 8 + (col & 4));
+        const int at = x * kPc + ((col >> 3) ^ (kPc == 16 ? (x & 3) * 4 : (x >> 1 & 1) * 4));
+        lds4* base = (lds4*)(reinterpret_cast<const uint16_t*>(lds.v) + at * 8 + (col & 4));
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(base);
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(base + 8 * kPc * 2);
         return u32x4{__builtin_bit_cast(u32x2, lo)[0], __builtin_bit_cast(u32x2, lo)[1],
                      __builtin_bit_cast(u32x2, hi)[0], __builtin_bit_cast(u32x2, hi)[1]};
       };
-      if (masked && (flags & 2)) {
-        // A token that some row must not see holds an infinity or a NaN, and 0 x inf
-        // is not 0: the finite values go in as always, the others are added to the
-        // rows that see them.
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int b = 0; b < kB; ++b)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            u32x4 w = v_at(b, j);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
-              if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
-            }
-            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w),
-                                                           __builtin_bit_cast(bf16x8, p[j]), o[b],
-                                                           0, 0, 0);
-          }
-#pragma unroll 1
-        for (int x = 0; x < kKeys; ++x)
-#pragma unroll
-          for (int b = 0; b < kB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              const int col = 32 * b + 2 * i + 4 * half;
-              const int at = x * kPc + ((col >> 3) ^ (kPc == 16 ? (x & 3) * 4 : (x >> 1 & 1) * 4));
-              const u32x2 w = *reinterpret_cast<const u32x2*>(
-                  reinterpret_cast<const uint16_t*>(lds.v[buf]) + at * 8 + (col & 4));
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const uint32_t y = k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16;
-                if ((y & 0x7f800000u) == 0x7f800000u && t0 + x < lim)
-                  o[b][i + k] += __uint_as_float(y);
-              }
-            }
-      } else {
-#pragma unroll
-        for (int b = 0; b < kB; ++b)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(bf16x8, v_at(b, j)), __builtin_bit_cast(bf16x8, p[j]), o[b], 0,
-                0, 0);
-      }
+          o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_at(b, j)),
+                                                         __builtin_bit_cast(bf16x8, p[j]), o[b], 0,
+                                                         0, 0);
     }
-    if (more) store(buf ^ 1, t0 + kKeys);
     __syncthreads();
+  };
+  if (s0 < s1) {
+    fetch(s0);
+    stage(lds0);
+    fetch(s0 + kKeys);
+  }
+  __syncthreads();
+  for (int32_t t0 = s0; t0 < s1; t0 += 2 * kKeys) {
+    step(t0, lds0, lds1);
+    if (t0 + kKeys < s1) step(t0 + kKeys, lds1, lds0);
   }
 
+  if (__syncthreads_or(odd)) {
+    for (int32_t t = std::max(tile_least / kKeys * kKeys, s0); t < s1; ++t) {
+      const int32_t b = table[t / a.block_size];
+      if (b < 0 || b >= a.pool_blocks) continue;
+      const char* v = a.kbase + a.voff + g * kDh * 2 +
+                      (int64_t(b) * a.bunits + int64_t(t % a.block_size) * a.sunits) * 128;
+#pragma unroll
+      for (int b = 0; b < kB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t y = uint32_t(reinterpret_cast<const uint16_t*>(
+                                 v)[32 * b + 8 * (i / 4) + 4 * half + i % 4])
+                             << 16;
+          if ((y & 0x7f800000u) == 0x7f800000u && t < lim) o[b][i] += __uint_as_float(y);
+        }
+    }
+  }
   lsum += __shfl_xor(lsum, 32);
   if (!live) return;
   const int64_t orow = token * a.q_heads + head;
@@ -530,9 +531,13 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   const int64_t bs = pool->chunk_bytes / per_token;
   const bool lm = pool->layout == FLOWKV_LAYOUT_LAYER_MAJOR;
   const int64_t stride = lm ? pool->chunk_bytes : 2 * int64_t(pool->num_layers) * pool->chunk_bytes;
-  // the kernel forms block offsets in 32 bits: one block stride under 4 GiB
+  // one block stride under 4 GiB, as for decode attention; the kernel forms offsets in
+  // 128-byte units (a head's row is one or two) of 32 bits
   if (stride >= (int64_t(1) << 32))
     return fail(FLOWKV_EINVAL, "block stride of %lld bytes: need under 4 GiB", (long long)stride);
+  if (pool->num_blocks >= (int64_t(1) << 39) / stride)
+    return fail(FLOWKV_EINVAL, "%d blocks %lld bytes apart: need under 512 GiB", pool->num_blocks,
+                (long long)stride);
   if (max_blocks < 0 || int64_t(max_blocks) * bs > INT32_MAX)
     return fail(FLOWKV_EINVAL, "max_blocks %d x block_size %lld tokens: need 0 to 2^31 - 1",
                 max_blocks, (long long)bs);
@@ -571,8 +576,11 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   a.tables = block_tables_dev;
   a.out = static_cast<uint16_t*>(out_dev);
   a.ws = static_cast<float*>(workspace_dev);
-  a.bstride = uint32_t(stride);
-  a.sstride = uint32_t(per_token);
+  a.bunits = uint32_t(stride / 128);
+  a.sunits = uint32_t(per_token / 128);
+  // q = (umulhi(t, m) + t) >> l with l = ceil(log2 bs), m = floor(2^32 (2^l - bs) / bs) + 1
+  while ((int64_t(1) << a.bs_shift) < bs) ++a.bs_shift;
+  a.bs_magic = uint32_t((((uint64_t(1) << a.bs_shift) - uint64_t(bs)) << 32) / uint64_t(bs) + 1);
   a.pool_blocks = pool->num_blocks;
   a.block_size = int32_t(bs);
   a.max_blocks = max_blocks;
