@@ -33,10 +33,11 @@ typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) s16x4 lds4;
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
-constexpr int kRows = 32 * kWaves;         // query rows of a workgroup's tile
-constexpr int kKeys = 64;                  // cached tokens of a step
+typedef __attribute__((address_space(1))) const void gvoid;
+typedef __attribute__((address_space(3))) void lvoid;
+typedef __attribute__((address_space(3))) u32x4 lvec;
+typedef __attribute__((address_space(3))) uint8_t lbyte;
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;               // log2 of the largest unnormalised weight
 
@@ -54,17 +55,18 @@ struct ChunkArgs {
   uint32_t bs_magic, bs_shift;          // division by block_size
   int32_t pool_blocks, block_size, max_blocks, max_seq_len;
   int32_t n_tokens, n_req, q_heads, kv_heads, group;
+  int32_t rows;                         // query rows of a workgroup's tile
   int32_t tiles, split_tokens, splits;
   float scale_log2;                     // scale * log2(e)
 };
 
 // The rows of a request are its (new token, query head of the group) pairs,
-// token by token; a tile is kRows of them.  Tile slot x of the batch: request r
-// has the slots from floor(offsets[r] * G / kRows) + r, which are enough for its
-// rows whatever the offsets are, and at most n_tokens * G / kRows + n_req in all:
+// token by token; a tile is a.rows of them.  Tile slot x of the batch: request r
+// has the slots from floor(offsets[r] * G / rows) + r, which are enough for its
+// rows whatever the offsets are, and at most n_tokens * G / rows + n_req in all:
 // the grid needs no lengths on the host.
 __device__ __forceinline__ int64_t first_tile(const ChunkArgs& a, int32_t r) {
-  return int64_t(a.offsets[r]) * a.group / kRows + r;
+  return int64_t(a.offsets[r]) * a.group / a.rows + r;
 }
 
 struct Request {
@@ -109,27 +111,238 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
 }
 
-// 16 bytes that a staged row of a token that cannot be read is made of.
-__device__ const u32x4 g_zeros = {0, 0, 0, 0};
+// What the parts of one row weigh when they are joined under reference m: a part that saw
+// no token has a reference of -inf and a sum of 0 (one whose scores are all NaN has a sum
+// of NaN, which stays).
+__device__ __forceinline__ float part_weight(float mine, float sum, float m) {
+  return mine == -INFINITY ? (sum == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(mine - m);
+}
 
-template <int kDh>
-struct ChunkLds {
-  alignas(16) u32x4 k[kKeys * kDh / 8];
-  alignas(16) u32x4 v[kKeys * kDh / 8];
+// 16-byte piece p of token x's row is at place x kPc + (p ^ swizzle(x)) of a tile: so
+// neither the operand reads (32 rows of K at one piece; V transposed, 4 rows of 32 dims)
+// nor the rows' arrival meet in a bank.
+template <int kPc>
+__device__ __forceinline__ int k_swizzle(int x) {
+  return kPc == 16 ? x & 15 : x >> 1 & 7;
+}
+template <int kPc>
+__device__ __forceinline__ int v_swizzle(int x) {
+  return kPc == 16 ? (x & 3) * 4 : (x >> 1 & 1) * 4;
+}
+
+// The form of a workgroup: kRw waves side by side in rows (32 each), kKw in keys; a wave
+// takes kTile cached tokens a step.
+constexpr int kTile = 64;
+template <int kDh_, int kRw_, int kKw_>
+struct Form {
+  static constexpr int kDh = kDh_, kRw = kRw_, kKw = kKw_;
+  static constexpr int kWaves = kRw * kKw, kThreads = 64 * kWaves;
+  static constexpr int kRows = 32 * kRw;
+  static constexpr int kStep = kTile * kKw;         // tokens of a step
+  static constexpr int kPc = kDh / 8;            // 16-byte pieces of a row
+  static constexpr int kLd = kStep * kPc / kThreads;  // 16-byte loads of a step's K, or V, a lane
+  static constexpr int kLdRows = kThreads / kPc;      // tokens of one such load
+  static constexpr int kGroup = kThreads / kStep;     // steps whose places are found at once
+  // (the swizzles repeat with 16 rows; a group's places are found in its predecessor's
+  // first step and read in its last)
+  static_assert(kGroup >= 2 && kLdRows % 16 == 0);
 };
 
-typedef __attribute__((address_space(1))) const void gvoid;
-typedef __attribute__((address_space(3))) void lvoid;
+// What a wave carries through the steps.
+template <class F>
+struct Wave {
+  static constexpr int kPc = F::kPc;
+  static constexpr int kI = F::kDh / 16;         // MFMA steps of K.q
+  static constexpr int kB = F::kDh / 32;         // blocks of 32 dims
+  static constexpr int kN = kTile / 32;             // blocks of 32 tokens
+  bf16x8 q[kI];
+  f32x16 o[kB];
+  float mref, lsum;                              // of the lane's row; lsum of its own half's tokens
+  float scale_log2;
+  int half;
+  uint32_t ka[kI], va[kB];                       // LDS places of the operand reads in a step's rows
+  int32_t lim;                                   // tokens that the lane's row sees,
+  int32_t wlim, wleast;                          // at most and at least that one of the wave's sees
 
-template <int kDh>
-__global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
-  constexpr int kPc = kDh / 8;                   // 16-byte pieces of a row
-  constexpr int kI = kDh / 16;                   // MFMA steps of K.q
-  constexpr int kB = kDh / 32;                   // blocks of 32 dims
-  constexpr int kLd = kKeys * kPc / kThreads;    // 16-byte loads of a tile's K, and V, a lane
-  constexpr int kLdRows = kThreads / kPc;        // tokens of one such load
+  __device__ __forceinline__ void place_reads(int ln, int kw) {
+    half = ln >> 5;
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      const int x = kw * kTile + (ln & 31);
+      ka[i] = (x * kPc + ((2 * i + half) ^ k_swizzle<kPc>(x))) * 16;
+    }
+#pragma unroll
+    for (int d = 0; d < kB; ++d) {
+      const int x = kw * kTile + 4 * half + (ln & 15) / 4;
+      const int col = 32 * d + 16 * (ln >> 4 & 1) + 4 * (ln & 3);   // dim
+      va[d] = (x * kPc + ((col >> 3) ^ v_swizzle<kPc>(x))) * 16 + (col >> 2 & 1) * 8;
+    }
+  }
+  // Operands: dims 16 i + 8 half of token 32 b + ln % 32; and of V, transposed, dim
+  // 32 d + ln % 32 of the 8 tokens of k-step j that the scores' lanes hold.
+  __device__ __forceinline__ u32x4 keys(const lvec* k, int b, int i) const {
+    return *(const lvec*)((const lbyte*)k + ka[i] + b * 32 * kPc * 16);
+  }
+  __device__ __forceinline__ u32x4 values(const lvec* v, int d, int j) const {
+    const lbyte* p = (const lbyte*)v + va[d];
+    const u32x2 lo = __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + j * 16 * kPc * 16)));
+    const u32x2 hi = __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(p + (j * 16 + 8) * kPc * 16)));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+  }
+
+  // S^T = K Q^T: rows are tokens, columns query rows.  The operands of 8 products are read
+  // ahead.
+  __device__ __forceinline__ void scores(f32x16 (&s)[kN], const lvec* k) const {
+    constexpr int kM = kN * kI, kAhead = 8 < kM ? 8 : kM;
+    u32x4 w[kM];
+#pragma unroll
+    for (int b = 0; b < kN; ++b) s[b] = f32x16{};
+#pragma unroll
+    for (int m = 0; m < kAhead; ++m) w[m] = keys(k, m / kI, m % kI);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int m = 0; m < kM; ++m) {
+      if (m + kAhead < kM) w[m + kAhead] = keys(k, (m + kAhead) / kI, (m + kAhead) % kI);
+      s[m / kI] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[m]),
+                                                          q[m % kI], s[m / kI], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // The weights of the scores of the tokens from t on, as the B operand of P.V: a lane
+  // holds of its row what the operand wants of it, so they change no lane.
+  __device__ __forceinline__ void weigh(f32x16 (&s)[kN], int32_t t, uint64_t dead,
+                                        u32x4 (&p)[2 * kN]) {
+    if (t + kTile > wleast || dead) {
+      const int32_t last = lim - t - 4 * half;
+      const uint64_t d = dead >> (4 * half);
+#pragma unroll
+      for (int b = 0; b < kN; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int x = 32 * b + 8 * (i / 4) + i % 4;
+          if (x >= last || (d >> x & 1)) s[b][i] = -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int b = 0; b < kN; ++b)
+#pragma unroll
+      for (int i = b == 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+    mx *= scale_log2;
+    // the reference moves only where some score is more than kLazy above it
+    if (__any(mx > mref + kLazy)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      if (mx > mref + kLazy) {
+        const float c = __builtin_amdgcn_exp2f(mref - mx);
+        mref = mx;
+        lsum *= c;
+#pragma unroll
+        for (int b = 0; b < kB; ++b) o[b] *= c;
+      }
+    }
+    const float mu = mref == -INFINITY ? 0.f : mref;
+#pragma unroll
+    for (int b = 0; b < kN; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale_log2, -mu));
+        const float y = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], scale_log2, -mu));
+        lsum += x + y;
+        p[2 * b + i / 8][i % 8 / 2] = pack_bf16(x, y);
+      }
+  }
+
+  // O^T += V^T P^T: rows are dims.
+  __device__ __forceinline__ void add(const lvec* v, const u32x4 (&p)[2 * kN]) {
+#pragma unroll
+    for (int j = 0; j < 2 * kN; ++j)
+#pragma unroll
+      for (int d = 0; d < kB; ++d)
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, values(v, d, j)),
+                                                       __builtin_bit_cast(bf16x8, p[j]), o[d], 0, 0,
+                                                       0);
+  }
+};
+
+// Where the rows of the workgroup's K and V are, kThreads tokens at a time (a group): their
+// places in the pool in 128-byte units, and which of 64 tokens have a block outside it.
+template <class F>
+struct Places {
+  uint32_t at[2 * F::kThreads];
+  uint64_t dead[2 * F::kWaves];
+};
+
+template <class F>
+struct Source {
+  const char* base;                              // the head's K of block 0
+  int64_t voff;
+  const int32_t* table;
+  uint32_t bs, bs_magic, bs_shift, bunits, sunits;
+  int32_t pool_blocks, s0, s1;
+  int tid, wave;
+  uint32_t kpiece, vpiece;                       // the lane's bytes of a row,
+  uint32_t row;                                  // and its first row of a step
+  Places<F>* places;
+  int32_t next_block;
+  uint32_t next_slot;
+  bool next_in;
+
+  // a lane's token of a group: its block ID and slot
+  __device__ __forceinline__ void fetch(int group) {
+    const uint32_t t = uint32_t(s0) + uint32_t(group) * F::kThreads + uint32_t(tid);
+    const uint32_t b = uint32_t((uint64_t(__umulhi(t, bs_magic)) + t) >> bs_shift);
+    next_slot = t - b * bs;
+    next_in = t < uint32_t(s1);
+    next_block = table[next_in ? b : 0];         // (s1 lies within the block list)
+  }
+  // a token that cannot be read has the place of the pool's first row
+  __device__ __forceinline__ void place(int group) const {
+    const bool good = next_in & (uint32_t(next_block) < uint32_t(pool_blocks));
+    const uint64_t dead = __ballot(next_in & !good);
+    const uint32_t at = uint32_t(next_block) * bunits + next_slot * sunits;
+    places->at[(group & 1) * F::kThreads + tid] = good ? at : 0;
+    if ((tid & 63) == 0) places->dead[(group & 1) * F::kWaves + wave] = dead;
+  }
+  __device__ __forceinline__ bool any_dead(int group) const {
+    return __any((tid & 63) < F::kWaves &&
+                 places->dead[(group & 1) * F::kWaves + tid % F::kWaves] != 0);
+  }
+  // which of the tile's tokens have a block outside the pool; x: its first, counted from s0
+  __device__ __forceinline__ uint64_t dead(int32_t x) const {
+    const uint64_t d = places->dead[x / 64 % (2 * F::kWaves)];
+    return uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(d >> 32)))) << 32 |
+           uint32_t(__builtin_amdgcn_readfirstlane(int(d)));
+  }
+  // The rows of step i on their way to LDS, with no register between.  An instruction
+  // fills 64 consecutive 16-byte places, so a lane's place is fixed, and the swizzle is in
+  // which piece of the row it reads.
+  __device__ __forceinline__ void send(int i, lvec* k, lvec* v) const {
+    uint32_t u[F::kLd];
+#pragma unroll
+    for (int e = 0; e < F::kLd; ++e)
+      u[e] = places->at[i % (2 * F::kGroup) * F::kStep + row + e * F::kLdRows];
+#pragma unroll
+    for (int e = 0; e < F::kLd; ++e) {
+      const uint64_t off = uint64_t(u[e]) * 128;
+      const int to = e * F::kThreads + wave * 64;
+      __builtin_amdgcn_global_load_lds((gvoid*)(base + (off + kpiece)), (lvoid*)(k + to), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gvoid*)(base + voff + (off + vpiece)), (lvoid*)(v + to), 16,
+                                       0, 0);
+    }
+  }
+};
+
+template <class F>
+__global__ __launch_bounds__(F::kThreads, 2)
+void chunk_attn(const ChunkArgs a) {
+  typedef Wave<F> W;
+  constexpr int kDh = F::kDh, kPc = F::kPc, kStep = F::kStep, kB = W::kB;
   const int tid = threadIdx.x, ln = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rw = wave % F::kRw, kw = wave / F::kRw;
   const int half = ln >> 5, c32 = ln & 31;
 
   const uint32_t id = blockIdx.x;
@@ -142,9 +355,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
   const Request rq = request_at(a, r);
   const int64_t local = int64_t(slot) - first_tile(a, r);
   const int64_t rows = int64_t(rq.n_new) * a.group;
-  const int64_t row0 = local * kRows;
+  const int64_t row0 = local * F::kRows;
   if (local < 0 || row0 >= rows) return;
-  const int64_t row_end = row0 + kRows < rows ? row0 + kRows : rows;
+  const int64_t row_end = row0 + F::kRows < rows ? row0 + F::kRows : rows;
   const int32_t tile_limit = seen(rq, int32_t((row_end - 1) / a.group));
   const int32_t tile_least = seen(rq, int32_t(row0 / a.group));
   const int32_t s0 = split * a.split_tokens;
@@ -153,206 +366,166 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
   const bool direct = tile_limit <= a.split_tokens;
 
   // this lane's query row, as a column of S^T
-  const int64_t row = row0 + wave * 32 + c32;
+  const int64_t wrow = row0 + rw * 32, row = wrow + c32;
   const bool live = row < rows;
   const int32_t qi = live ? int32_t(row / a.group) : 0;
   const int32_t qh = live ? int32_t(row - int64_t(qi) * a.group) : 0;
-  const int32_t lim = live ? seen(rq, qi) : 0;
   const int64_t token = int64_t(rq.begin) + qi;
   const int32_t head = g * a.group + qh;
-  // what the wave's rows see at least and at most (it may hold no row)
-  const int64_t wrow = row0 + wave * 32;
-  const bool any_row = wrow < rows;
+  W w;
+  w.place_reads(ln, kw);
+  w.scale_log2 = a.scale_log2;
+  w.lim = live ? seen(rq, qi) : 0;
+  const bool any_row = wrow < rows;              // (the wave may hold no row)
   const int32_t wlast = any_row ? int32_t((wrow + 31 < rows ? wrow + 31 : rows - 1) / a.group) : 0;
-  const int32_t wlim = __builtin_amdgcn_readfirstlane(any_row ? seen(rq, wlast) : 0);
-  const int32_t wleast =
-      __builtin_amdgcn_readfirstlane(any_row ? seen(rq, int32_t(wrow / a.group)) : 0);
-
-  bf16x8 qb[kI];
+  w.wlim = __builtin_amdgcn_readfirstlane(any_row ? seen(rq, wlast) : 0);
+  w.wleast = __builtin_amdgcn_readfirstlane(any_row ? seen(rq, int32_t(wrow / a.group)) : 0);
 #pragma unroll
-  for (int i = 0; i < kI; ++i) {
-    u32x4 w = {0, 0, 0, 0};
-    if (live)
-      w = *(cgvec4*)(a.q + token * a.q_stride + head * kDh + 16 * i + 8 * half);
-    qb[i] = __builtin_bit_cast(bf16x8, w);
+  for (int i = 0; i < W::kI; ++i) {
+    u32x4 x = {0, 0, 0, 0};
+    if (live) x = *(cgvec4*)(a.q + token * a.q_stride + head * kDh + 16 * i + 8 * half);
+    w.q[i] = __builtin_bit_cast(bf16x8, x);
   }
+#pragma unroll
+  for (int b = 0; b < kB; ++b) w.o[b] = f32x16{};
+  w.mref = -INFINITY;
+  w.lsum = 0.f;
 
-  __shared__ ChunkLds<kDh> lds0, lds1;
+  __shared__ alignas(16) u32x4 sk0[kStep * kPc], sk1[kStep * kPc], sv0[kStep * kPc],
+      sv1[kStep * kPc];
+  __shared__ Places<F> places;
 
-  // Staging: K and V rows go from memory to LDS directly.  An instruction fills 64
-  // consecutive 16-byte places, so a lane's place is fixed, token lr + e kLdRows and
-  // piece lp of its row, and the swizzle is in which piece it reads.
   const int lr = tid / kPc, lp = tid % kPc;
-  const int32_t* table = a.tables + int64_t(r) * a.max_blocks;
-  const char* kp = a.kbase + g * kDh * 2 + 16 * (lp ^ (kPc == 16 ? lr & 15 : lr >> 1 & 7));
-  const char* vp = a.kbase + a.voff + g * kDh * 2 +
-                   16 * (lp ^ (kPc == 16 ? (lr & 3) * 4 : (lr >> 1 & 1) * 4));
-  const char* const zeros = reinterpret_cast<const char*>(&g_zeros);
-  // lane ln's token of a tile: block ID, and its row's place in the pool in 128-byte
-  // units (all ones: it cannot be read)
-  uint32_t next_slot;
-  int32_t next_block;
-  bool next_in;
-  auto fetch = [&](int32_t t0) {
-    const uint32_t t = uint32_t(t0 + ln);
-    const uint32_t b = uint32_t((uint64_t(__umulhi(t, a.bs_magic)) + t) >> a.bs_shift);
-    next_slot = t - b * uint32_t(a.block_size);
-    next_in = int32_t(t) < s1;
-    next_block = table[next_in ? b : 0];         // (s1 lies within the block list)
-  };
-  uint64_t dead, next_dead;                      // tokens of a tile whose block is outside
-  auto stage = [&](ChunkLds<kDh>& to) {
-    const bool good = next_in && next_block >= 0 && next_block < a.pool_blocks;
-    next_dead = __ballot(next_in && !good);
-    const uint32_t at =
-        good ? uint32_t(next_block) * a.bunits + next_slot * a.sunits : 0xffffffffu;
-#pragma unroll
-    for (int e = 0; e < kLd; ++e) {
-      const uint32_t u = __shfl(at, lr + e * kLdRows);
-      const uint64_t off = uint64_t(u) * 128;
-      const char* ks = u != 0xffffffffu ? kp + off : zeros;
-      const char* vs = u != 0xffffffffu ? vp + off : zeros;
-      const int place = e * kThreads + wave * 64;
-      __builtin_amdgcn_global_load_lds((gvoid*)ks, (lvoid*)(to.k + place), 16, 0, 0);
-      __builtin_amdgcn_global_load_lds((gvoid*)vs, (lvoid*)(to.v + place), 16, 0, 0);
-    }
-  };
+  Source<F> src;
+  src.base = a.kbase + g * kDh * 2;
+  src.voff = a.voff;
+  src.table = a.tables + int64_t(r) * a.max_blocks;
+  src.bs = uint32_t(a.block_size);
+  src.bs_magic = a.bs_magic;
+  src.bs_shift = a.bs_shift;
+  src.bunits = a.bunits;
+  src.sunits = a.sunits;
+  src.pool_blocks = a.pool_blocks;
+  src.s0 = s0;
+  src.s1 = s1;
+  src.tid = tid;
+  src.wave = wave;
+  src.row = lr;
+  src.kpiece = 16 * (lp ^ k_swizzle<kPc>(lr));
+  src.vpiece = 16 * (lp ^ v_swizzle<kPc>(lr));
+  src.places = &places;
 
-  f32x16 o[kB];
+  // Where some row does not see some token, or a block is missing, an infinity or a NaN
+  // in V would reach a row as 0 x inf: such values are taken out of the step's rows by the
+  // lanes that brought them, and added at the end to the rows that see them.
+  bool odd = false, suspect = false;             // suspect: a block is missing somewhere so far
+  int32_t odd_from = s1;
+  auto landed = [&](lvec* v, int32_t t0) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
+    if (__builtin_expect(t0 + kStep <= tile_least && !suspect, 1)) return;
+    odd_from = std::min(odd_from, t0);
 #pragma unroll
-  for (int b = 0; b < kB; ++b) o[b] = f32x16{};
-  float mref = -INFINITY, lsum = 0.f;            // of the lane's row; its own half of the tokens
-
-  // Where some row does not see some token, an infinity or a NaN in V would reach it as
-  // 0 x inf: such values are taken out of the tile, and added at the end to the rows
-  // that see them.
-  bool odd = false;
-  auto clean = [&](ChunkLds<kDh>& lds) {
-#pragma unroll
-    for (int e = 0; e < kLd; ++e) {
-      u32x4 w = lds.v[e * kThreads + tid];
+    for (int e = 0; e < F::kLd; ++e) {
+      u32x4 x = v[e * F::kThreads + tid];
       bool any = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if ((w[i] & 0x7f80u) == 0x7f80u) {
-          w[i] &= 0xffff0000u;
+        if ((x[i] & 0x7f80u) == 0x7f80u) {
+          x[i] &= 0xffff0000u;
           any = true;
         }
-        if ((w[i] & 0x7f800000u) == 0x7f800000u) {
-          w[i] &= 0xffffu;
+        if ((x[i] & 0x7f800000u) == 0x7f800000u) {
+          x[i] &= 0xffffu;
           any = true;
         }
       }
-      if (any) lds.v[e * kThreads + tid] = w;
+      if (any) v[e * F::kThreads + tid] = x;
       odd |= any;
     }
-    __syncthreads();
   };
 
-  auto step = [&](int32_t t0, ChunkLds<kDh>& lds, ChunkLds<kDh>& other) {
-    dead = next_dead;
-    if (t0 + kKeys > tile_least) clean(lds);     // uniform
-    if (t0 + kKeys < s1) {
-      stage(other);
-      fetch(t0 + 2 * kKeys);
-    }
-    if (t0 < wlim) {
-      // S^T = K Q^T: rows are tokens, columns query rows
-      f32x16 s[2] = {f32x16{}, f32x16{}};
-      u32x4 w[2][kI];
-      auto k_at = [&](int b, int i) {
-        const int x = 32 * b + c32;
-        return lds.k[x * kPc + ((2 * i + half) ^ (kPc == 16 ? x & 15 : x >> 1 & 7))];
-      };
-#pragma unroll
-      for (int i = 0; i < kI; ++i) w[0][i] = k_at(0, i);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < kI; ++i) {
-        w[1][i] = k_at(1, i);
-        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[0][i]), qb[i],
-                                                       s[0], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
+  if (s0 < s1) {                                 // uniform
+    int i = 0;
+    auto step = [&](int32_t t0, lvec* __restrict__ k, lvec* __restrict__ v, lvec* __restrict__ k_to,
+                    lvec* __restrict__ v_to) {
+      const bool more = t0 + kStep < s1;
+      const bool find = i % F::kGroup == 0;      // the next group's places
+      if (more) src.send(i + 1, k_to, v_to);
+      if (find) src.fetch(i / F::kGroup + 1);
+      const int32_t t = t0 + kw * kTile;
+      if (t < w.wlim && t < s1) {
+        f32x16 s[W::kN];
+        u32x4 p[2 * W::kN];
+        w.scores(s, k);
+        w.weigh(s, t, __builtin_expect(suspect, 0) ? src.dead(t - s0) : 0, p);
+        w.add(v, p);
       }
+      if (find) src.place(i / F::kGroup + 1);
+      if (more) landed(v_to, t0 + kStep);
+      __syncthreads();
+      if (find) suspect |= src.any_dead(i / F::kGroup + 1);
+      ++i;
+    };
+    lvec *const k0 = (lvec*)sk0, *const k1 = (lvec*)sk1, *const v0 = (lvec*)sv0,
+                *const v1 = (lvec*)sv1;
+    src.fetch(0);
+    src.place(0);
+    __syncthreads();
+    suspect = src.any_dead(0);
+    src.send(0, k0, v0);
+    landed(v0, s0);
+    __syncthreads();
+    for (int32_t t0 = s0; t0 < s1; t0 += 2 * kStep) {
+      step(t0, k0, v0, k1, v1);
+      if (t0 + kStep < s1) step(t0 + kStep, k1, v1, k0, v0);
+    }
+  }
+  const bool had_odd = __syncthreads_or(odd);
+  float lsum = w.lsum + __shfl_xor(w.lsum, 32);
+  float mref = w.mref;
+  if constexpr (F::kKw > 1) {
+    // The waves of other keys bring their sums to the first ones', through LDS, kR blocks of
+    // dims at a time: register j of lane l at place 64 j + l.
+    constexpr int kFit = int(sizeof(sk0)) / (F::kRw * 64 * 16 * int(sizeof(float)));
+    constexpr int kR = kFit < kB ? kFit : kB;
+    static_assert(kR >= 1 && kB % kR == 0 && sizeof(sk1) >= F::kRw * 2 * 64 * sizeof(float));
+    float* const sums = reinterpret_cast<float*>(sk0) + rw * (kR * 16 * 64) + ln;
+    float* const ml = reinterpret_cast<float*>(sk1) + rw * 128 + ln;
+    for (int from = 1; from < F::kKw; ++from) {
+      float c1 = 0.f, c2 = 0.f;
 #pragma unroll
-      for (int i = 0; i < kI; ++i)
-        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w[1][i]), qb[i],
-                                                       s[1], 0, 0, 0);
-      if (t0 + kKeys > wleast || dead) {
-        const int32_t last = lim - t0 - 4 * half;
-        const uint64_t d = dead >> (4 * half);
+      for (int b0 = 0; b0 < kB; b0 += kR) {
+        if (kw == from) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int x = 32 * b + 8 * (i / 4) + i % 4;
-            if (x >= last || (d >> x & 1)) s[b][i] = -INFINITY;
+          for (int j = 0; j < 16 * kR; ++j) sums[64 * j] = w.o[b0 + j / 16][j % 16];
+          if (b0 == 0) {
+            ml[0] = mref;
+            ml[64] = lsum;
           }
-      }
-      float mx = s[0][0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[0][i]);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[1][i]);
-      mx *= a.scale_log2;
-      if (__any(mx > mref + kLazy)) {
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        if (mx > mref + kLazy) {
-          const float c = __builtin_amdgcn_exp2f(mref - mx);
-          mref = mx;
-          lsum *= c;
-#pragma unroll
-          for (int b = 0; b < kB; ++b) o[b] *= c;
         }
-      }
-      const float mu = mref == -INFINITY ? 0.f : mref;
-      u32x4 p[4];                                // k-step j: the B operand
+        __syncthreads();
+        if (kw == 0) {
+          if (b0 == 0) {
+            const float m2 = ml[0], l2 = ml[64], m = fmaxf(mref, m2);
+            c1 = part_weight(mref, lsum, m);
+            c2 = part_weight(m2, l2, m);
+            mref = m;
+            lsum = lsum * c1 + l2 * c2;
+          }
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const float x = __builtin_amdgcn_exp2f(fmaf(s[b][i], a.scale_log2, -mu));
-          const float y = __builtin_amdgcn_exp2f(fmaf(s[b][i + 1], a.scale_log2, -mu));
-          lsum += x + y;
-          p[2 * b + i / 8][i % 8 / 2] = pack_bf16(x, y);
+          for (int j = 0; j < 16 * kR; ++j)
+            w.o[b0 + j / 16][j % 16] = w.o[b0 + j / 16][j % 16] * c1 + sums[64 * j] * c2;
         }
-      // O^T += V^T P^T: rows are dims.  V is read transposed
-      auto v_at = [&](int b, int j) {
-        const int x = 16 * j + 4 * half + (ln & 15) / 4;
-        const int col = 32 * b + 16 * (ln >> 4 & 1) + 4 * (ln & 3);   // dim
-        const int at = x * kPc + ((col >> 3) ^ (kPc == 16 ? (x & 3) * 4 : (x >> 1 & 1) * 4));
-        lds4* base = (lds4*)(reinterpret_cast<const uint16_t*>(lds.v) + at * 8 + (col & 4));
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(base);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(base + 8 * kPc * 2);
-        return u32x4{__builtin_bit_cast(u32x2, lo)[0], __builtin_bit_cast(u32x2, lo)[1],
-                     __builtin_bit_cast(u32x2, hi)[0], __builtin_bit_cast(u32x2, hi)[1]};
-      };
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int b = 0; b < kB; ++b)
-          o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_at(b, j)),
-                                                         __builtin_bit_cast(bf16x8, p[j]), o[b], 0,
-                                                         0, 0);
+        __syncthreads();
+      }
     }
-    __syncthreads();
-  };
-  if (s0 < s1) {
-    fetch(s0);
-    stage(lds0);
-    fetch(s0 + kKeys);
+    if (kw > 0) return;
   }
-  __syncthreads();
-  for (int32_t t0 = s0; t0 < s1; t0 += 2 * kKeys) {
-    step(t0, lds0, lds1);
-    if (t0 + kKeys < s1) step(t0 + kKeys, lds1, lds0);
-  }
-
-  if (__syncthreads_or(odd)) {
-    for (int32_t t = std::max(tile_least / kKeys * kKeys, s0); t < s1; ++t) {
-      const int32_t b = table[t / a.block_size];
+  if (had_odd) {
+    for (int32_t t = odd_from; t < s1; ++t) {
+      const int32_t b = src.table[t / a.block_size];
       if (b < 0 || b >= a.pool_blocks) continue;
-      const char* v = a.kbase + a.voff + g * kDh * 2 +
+      const char* v = src.base + a.voff +
                       (int64_t(b) * a.bunits + int64_t(t % a.block_size) * a.sunits) * 128;
 #pragma unroll
       for (int b = 0; b < kB; ++b)
@@ -361,11 +534,10 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
           const uint32_t y = uint32_t(reinterpret_cast<const uint16_t*>(
                                  v)[32 * b + 8 * (i / 4) + 4 * half + i % 4])
                              << 16;
-          if ((y & 0x7f800000u) == 0x7f800000u && t < lim) o[b][i] += __uint_as_float(y);
+          if ((y & 0x7f800000u) == 0x7f800000u && t < w.lim) w.o[b][i] += __uint_as_float(y);
         }
     }
   }
-  lsum += __shfl_xor(lsum, 32);
   if (!live) return;
   const int64_t orow = token * a.q_heads + head;
   if (direct) {
@@ -374,9 +546,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
     for (int b = 0; b < kB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; i += 4) {
-        const u32x2 w = {pack_bf16(o[b][i] * inv, o[b][i + 1] * inv),
-                         pack_bf16(o[b][i + 2] * inv, o[b][i + 3] * inv)};
-        *reinterpret_cast<u32x2*>(a.out + orow * kDh + 32 * b + 2 * i + 4 * half) = w;
+        const u32x2 x = {pack_bf16(w.o[b][i] * inv, w.o[b][i + 1] * inv),
+                         pack_bf16(w.o[b][i + 2] * inv, w.o[b][i + 3] * inv)};
+        *reinterpret_cast<u32x2*>(a.out + orow * kDh + 32 * b + 2 * i + 4 * half) = x;
       }
   } else {
     const int64_t rec = record_at(a, orow, split);
@@ -385,19 +557,355 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_attn(const ChunkArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
         *reinterpret_cast<f32x4u*>(record_sums(a, kDh, rec) + 32 * b + 2 * i + 4 * half) =
-            f32x4u{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+            f32x4u{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
     if (half == 0) *record_ml(a, kDh, rec) = f32x2u{mref, lsum};
   }
 }
 
-// Joins the splits' records of the rows whose tile has more than one: a wave per
-// (new token, query head), Dh / 4 lanes a record.
-template <int kDh>
-__global__ __launch_bounds__(kThreads) void chunk_attn_merge(const ChunkArgs a) {
-  constexpr int kLanes = kDh / 4, kParts = 64 / kLanes;
+// ---- few rows ----------------------------------------------------------------------
+//
+// A request of a few new tokens reads every cached K and V for a handful of rows: that is
+// bound by HBM, as the decode step is, and wants many loads in flight rather than many rows
+// per byte.  A workgroup takes 16 rows, as the 16 columns of S^T, and each of its four
+// waves tiles of 32 tokens of its own, four tiles apart, with no barrier between:
+//   - K and V rows arrive whole in registers (16 lanes a row of K; a lane of group q4 =
+//     lane / 16 has V of the tokens 4 e + q4, e = 0..7), the next tile's while this one is
+//     worked on;
+//   - K goes through the wave's part of LDS into the A operand, row m of half gg being
+//     token 16 gg + 4 (m % 4) + m / 4: a lane's scores are then those of the tokens whose
+//     V it holds, and P and V are operands of P.V where they are.
+constexpr int kFewWaves = 4;
+constexpr int kFewThreads = 64 * kFewWaves;
+constexpr int kFewTile = 32;
+constexpr int kFewSplit = 2048;            // most tokens of a workgroup: their places are in LDS
+
+template <int kDh, int kC>
+struct FewLds {
+  static constexpr int kRows = 16 * kC;
+  uint32_t at[kFewSplit];                  // a tile's token 4 e + q4 at 8 q4 + e, in 128-byte units
+  // K's staging, a tile per wave; after the loop the waves' weighted sums
+  alignas(16) uint8_t area[kFewWaves * kRows * kDh * sizeof(float)];
+  uint32_t dead[kFewSplit / kFewTile];
+  float m[kFewWaves][kRows], l[kFewWaves][kRows];
+  int32_t lim[kRows];
+  static_assert(kFewWaves * kFewTile * kDh * 2 <= sizeof(area));
+};
+
+__device__ __forceinline__ uint32_t pair_hi(uint32_t lo, uint32_t hi) {
+  return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+}
+__device__ __forceinline__ uint32_t pair_lo(uint32_t lo, uint32_t hi) {
+  return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+
+// Takes infinities and NaN out of two bf16; whether there was one.
+__device__ __forceinline__ bool tame(uint32_t& w) {
+  bool any = false;
+  if ((w & 0x7f80u) == 0x7f80u) {
+    w &= 0xffff0000u;
+    any = true;
+  }
+  if ((w & 0x7f800000u) == 0x7f800000u) {
+    w &= 0xffffu;
+    any = true;
+  }
+  return any;
+}
+
+template <int kDh, int kC>
+__global__ __launch_bounds__(kFewThreads, (kDh == 64 ? 4 : 3) - (kC - 1))
+void chunk_attn_few(const ChunkArgs a) {
+  constexpr int kFewRows = 16 * kC;
+  constexpr int kI = kDh / 32;                   // MFMA steps of K.q
+  constexpr int kT = kDh / 16;                   // dims a lane owns in P.V
+  constexpr int kVW = kT / 2;                    // V words per token and lane
+  constexpr int kPc = kDh / 8;                   // 16-byte pieces of a K row
+  constexpr int kKL = kFewTile * kPc / 64;       // K loads of a tile and lane
+  typedef uint32_t VT __attribute__((ext_vector_type(kVW)));
+  typedef __attribute__((address_space(1))) const VT cgv;
+  const int tid = threadIdx.x, ln = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int q4 = ln >> 4, c16 = ln & 15;
+
+  const uint32_t id = blockIdx.x;
+  const int g = int(id % uint32_t(a.kv_heads));
+  const uint32_t rest = id / uint32_t(a.kv_heads);
+  const int split = int(rest / uint32_t(a.tiles));
+  const int slot = int(rest % uint32_t(a.tiles));
+  const int32_t r =
+      flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); });
+  const Request rq = request_at(a, r);
+  const int64_t local = int64_t(slot) - first_tile(a, r);
+  const int64_t rows = int64_t(rq.n_new) * a.group;
+  const int64_t row0 = local * kFewRows;
+  if (local < 0 || row0 >= rows) return;
+  const int64_t row_end = row0 + kFewRows < rows ? row0 + kFewRows : rows;
+  const int32_t tile_limit = seen(rq, int32_t((row_end - 1) / a.group));
+  const int32_t tile_least = seen(rq, int32_t(row0 / a.group));
+  const int32_t s0 = split * a.split_tokens;
+  if (split > 0 && s0 >= tile_limit) return;
+  const int32_t s1 = tile_limit - s0 > a.split_tokens ? s0 + a.split_tokens : tile_limit;
+  const bool direct = tile_limit <= a.split_tokens;
+  const int n_tiles = (s1 - s0 + kFewTile - 1) / kFewTile;
+
+  __shared__ FewLds<kDh, kC> lds;
+  int32_t lim[kC];
+  bf16x8 qb[kC][kI];
+#pragma unroll
+  for (int c = 0; c < kC; ++c) {
+    const int64_t row = row0 + 16 * c + c16;
+    const bool live = row < rows;
+    const int32_t qi = live ? int32_t(row / a.group) : 0;
+    const int32_t qh = live ? int32_t(row - int64_t(qi) * a.group) : 0;
+    lim[c] = live ? seen(rq, qi) : 0;
+    if (tid < 16) lds.lim[16 * c + tid] = lim[c];
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      u32x4 x = {0, 0, 0, 0};
+      if (live)
+        x = *(cgvec4*)(a.q + (int64_t(rq.begin) + qi) * a.q_stride +
+                       (g * a.group + qh) * int64_t(kDh) + 32 * i + 8 * q4);
+      qb[c][i] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  const int32_t* table = a.tables + int64_t(r) * a.max_blocks;
+  for (int x = tid; x < n_tiles * kFewTile; x += kFewThreads) {
+    const uint32_t t = uint32_t(s0 + x);
+    const uint32_t b = uint32_t((uint64_t(__umulhi(t, a.bs_magic)) + t) >> a.bs_shift);
+    const bool in = int32_t(t) < s1;
+    const int32_t blk = table[in ? b : 0];       // (s1 lies within the block list)
+    const bool good = in && blk >= 0 && blk < a.pool_blocks;
+    const uint64_t dead = __ballot(!good);
+    lds.at[(x & -kFewTile) + (x & 3) * 8 + (x >> 2 & 7)] =
+        good ? uint32_t(blk) * a.bunits + (t - b * uint32_t(a.block_size)) * a.sunits : 0;
+    if (ln % kFewTile == 0) lds.dead[x / kFewTile] = uint32_t(dead >> ln);
+  }
+  u32x4* const s_k = reinterpret_cast<u32x4*>(lds.area + wave * (kFewTile * kDh * 2));
+  f32x4 o[kC][kT];
+  float mref[kC], lsum[kC];                      // of the column's row; this lane's tokens
+#pragma unroll
+  for (int c = 0; c < kC; ++c) {
+    mref[c] = -INFINITY;
+    lsum[c] = 0.f;
+#pragma unroll
+    for (int t = 0; t < kT; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  bool odd = false;
+  __syncthreads();
+
+  u32x4 kw[kKL];
+  VT vw[8];
+  constexpr int kStride = 64 / kPc;              // tokens of one K load
+  const int kt = ln / kPc, kp = ln % kPc;
+  const char* const kbase = a.kbase + g * kDh * 2 + 16 * kp;
+  const char* const vbase = a.kbase + a.voff + g * kDh * 2 + c16 * (kVW * 4);
+  auto swz = [](int token) { return (token * kPc >> 4) & (kPc - 1); };
+  auto load_k = [&](int tile) {
+#pragma unroll
+    for (int e = 0; e < kKL; ++e) {
+      const int x = kt + e * kStride;            // token of the tile
+      kw[e] = __builtin_nontemporal_load((cgvec4*)(kbase + uint64_t(lds.at[tile * kFewTile + (x & 3) * 8 + (x >> 2)]) * 128));
+    }
+  };
+  auto load_v = [&](int tile) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      vw[e] = __builtin_nontemporal_load((cgv*)(vbase + uint64_t(lds.at[tile * kFewTile + 8 * q4 + e]) * 128));
+  };
+  if (wave < n_tiles) {
+    load_k(wave);
+    load_v(wave);
+  }
+  for (int tile = wave; tile < n_tiles; tile += kFewWaves) {
+    // (past the wave's last tile: its own again, so that as many loads are under way)
+    const int next = tile + kFewWaves < n_tiles ? tile + kFewWaves : tile;
+#pragma unroll
+    for (int e = 0; e < kKL; ++e) {
+      const int x = kt + e * kStride;
+      s_k[x * kPc + (kp ^ swz(x))] = kw[e];
+    }
+    __builtin_amdgcn_wave_barrier();
+    const int kr[2] = {4 * (c16 & 3) + (c16 >> 2), 16 + 4 * (c16 & 3) + (c16 >> 2)};
+    bf16x8 ka[2][kI];
+#pragma unroll
+    for (int gg = 0; gg < 2; ++gg)
+#pragma unroll
+      for (int i = 0; i < kI; ++i)
+        ka[gg][i] = __builtin_bit_cast(bf16x8, s_k[kr[gg] * kPc + ((4 * i + q4) ^ swz(kr[gg]))]);
+    f32x4 s[kC][2];
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int gg = 0; gg < 2; ++gg) {
+        s[c][gg] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+          s[c][gg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[gg][i], qb[c][i], s[c][gg], 0, 0, 0);
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    load_k(next);
+    __builtin_amdgcn_sched_barrier(0);
+    const int32_t t0 = s0 + tile * kFewTile;
+    const uint32_t dead = __builtin_amdgcn_readfirstlane(lds.dead[tile]) >> q4;   // bit 4 e
+    const bool masked = t0 + kFewTile > tile_least || __any(dead != 0);           // uniform
+    u32x4 p[kC];
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (t0 + 4 * e + q4 >= lim[c] || (dead >> (4 * e) & 1)) s[c][e >> 2][e & 3] = -INFINITY;
+      }
+      float mx = fmaxf(fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3])),
+                       fmaxf(fmaxf(s[c][1][0], s[c][1][1]), fmaxf(s[c][1][2], s[c][1][3]))) *
+                 a.scale_log2;
+      if (__any(mx > mref[c] + kLazy)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        float f = 1.f;
+        if (mx > mref[c] + kLazy) {
+          f = __builtin_amdgcn_exp2f(mref[c] - mx);
+          mref[c] = mx;
+        }
+        lsum[c] *= f;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float fx = __shfl(f, 4 * q4 + x);
+#pragma unroll
+          for (int t = 0; t < kT; ++t) o[c][t][x] *= fx;
+        }
+      }
+      const float mu = mref[c] == -INFINITY ? 0.f : mref[c];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[c][i >> 1][2 * i & 3], a.scale_log2, -mu));
+        const float y =
+            __builtin_amdgcn_exp2f(fmaf(s[c][i >> 1][(2 * i & 3) + 1], a.scale_log2, -mu));
+        lsum[c] += x + y;
+        p[c][i] = pack_bf16(x, y);
+      }
+    }
+    if (masked) {                                // 0 x inf is not 0
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (dead >> (4 * e) & 1) vw[e] = VT{};
+#pragma unroll
+        for (int i = 0; i < kVW; ++i) {
+          uint32_t x = vw[e][i];
+          odd |= tame(x);
+          vw[e][i] = x;
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int m = 0; m < kVW; ++m) {
+      u32x4 w[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[0][i] = pair_lo(vw[2 * i][m], vw[2 * i + 1][m]);
+        w[1][i] = pair_hi(vw[2 * i][m], vw[2 * i + 1][m]);
+      }
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          o[c][2 * m + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(bf16x8, p[c]), __builtin_bit_cast(bf16x8, w[h]), o[c][2 * m + h], 0,
+              0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(next);
+  }
+
+#pragma unroll
+  for (int c = 0; c < kC; ++c) {
+    lsum[c] += __shfl_xor(lsum[c], 16);
+    lsum[c] += __shfl_xor(lsum[c], 32);
+    if (q4 == 0) {
+      lds.m[wave][16 * c + c16] = mref[c];
+      lds.l[wave][16 * c + c16] = lsum[c];
+    }
+  }
+  const bool had_odd = __syncthreads_or(odd);    // every wave is past the loop: the area is free
+  float* const s_o = reinterpret_cast<float*>(lds.area);   // [wave][row][dim]
+#pragma unroll
+  for (int c = 0; c < kC; ++c)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int t = 0; t < kT; t += 4)
+        *reinterpret_cast<f32x4*>(
+            &s_o[(wave * kFewRows + 16 * c + 4 * q4 + x) * kDh + kT * c16 + t]) =
+            f32x4{o[c][t][x], o[c][t + 1][x], o[c][t + 2][x], o[c][t + 3][x]};
+  __syncthreads();
+  // a row's dims 4 at a time
+  for (int i = tid; i < kFewRows * kDh / 4; i += kFewThreads) {
+    const int h = i / (kDh / 4), d = i % (kDh / 4) * 4;
+    if (row0 + h >= rows) break;
+    float M = -INFINITY, L = 0.f;
+    f32x4 A = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) M = fmaxf(M, lds.m[w][h]);
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      const float wt = part_weight(lds.m[w][h], lds.l[w][h], M);
+      L += lds.l[w][h] * wt;
+      A += *reinterpret_cast<const f32x4*>(&s_o[(w * kFewRows + h) * kDh + d]) * wt;
+    }
+    if (had_odd) {
+      for (int32_t t = s0; t < s1; ++t) {
+        const int32_t b = table[t / a.block_size];
+        if (b < 0 || b >= a.pool_blocks || t >= lds.lim[h]) continue;
+        const uint16_t* v = reinterpret_cast<const uint16_t*>(
+            a.kbase + a.voff + g * kDh * 2 +
+            (int64_t(b) * a.bunits + int64_t(t % a.block_size) * a.sunits) * 128);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t y = uint32_t(v[d + k]) << 16;
+          if ((y & 0x7f800000u) == 0x7f800000u) A[k] += __uint_as_float(y);
+        }
+      }
+    }
+    const int64_t tr = row0 + h;
+    const int64_t orow = (int64_t(rq.begin) + tr / a.group) * a.q_heads + g * a.group + tr % a.group;
+    if (direct) {
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      const u32x2 x = {pack_bf16(A[0] * inv, A[1] * inv), pack_bf16(A[2] * inv, A[3] * inv)};
+      *reinterpret_cast<u32x2*>(a.out + orow * kDh + d) = x;
+    } else {
+      const int64_t rec = record_at(a, orow, split);
+      *reinterpret_cast<f32x4u*>(record_sums(a, kDh, rec) + d) = A;
+      if (d == 0) *record_ml(a, kDh, rec) = f32x2u{M, L};
+    }
+  }
+}
+
+// Joins the splits' records of the rows whose tile has more than one: a wave, or the four
+// of a workgroup, per (new token, query head), Dh / 4 lanes a record, kMergeChunk records
+// of a lane group under way at once.
+constexpr int kMergeThreads = 256;
+constexpr int kMergeChunk = 8;
+
+struct Running {
+  float m, l;
+  f32x4 v;
+};
+__device__ __forceinline__ Running join(const Running& a, const Running& b) {
+  Running r;
+  r.m = fmaxf(a.m, b.m);
+  const float wa = part_weight(a.m, a.l, r.m), wb = part_weight(b.m, b.l, r.m);
+  r.l = a.l * wa + b.l * wb;
+  r.v = a.v * wa + b.v * wb;
+  return r;
+}
+
+template <int kDh, int kWavesPer>
+__global__ __launch_bounds__(kMergeThreads) void chunk_attn_merge(const ChunkArgs a) {
+  constexpr int kLanes = kDh / 4, kParts = 64 * kWavesPer / kLanes;
   const int ln = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t orow = int64_t(blockIdx.x) * kWaves + wave;
+  const int64_t orow = kWavesPer == 1 ? int64_t(blockIdx.x) * 4 + wave : int64_t(blockIdx.x);
   if (orow >= int64_t(a.n_tokens) * a.q_heads) return;
   const int32_t token = int32_t(orow / a.q_heads), head = int32_t(orow - int64_t(token) * a.q_heads);
   const int32_t r =
@@ -407,63 +915,93 @@ __global__ __launch_bounds__(kThreads) void chunk_attn_merge(const ChunkArgs a) 
   if (i < 0 || i >= rq.n_new) return;
   // the tile that the row was in, as its workgroups saw it
   const int64_t row = int64_t(i) * a.group + head % a.group;
-  const int64_t end = std::min<int64_t>((row / kRows + 1) * kRows, int64_t(rq.n_new) * a.group);
+  const int64_t end = std::min<int64_t>((row / a.rows + 1) * a.rows, int64_t(rq.n_new) * a.group);
   const int32_t tile_limit = seen(rq, int32_t((end - 1) / a.group));
   if (tile_limit <= a.split_tokens) return;      // written already
   const int32_t n = (seen(rq, i) + a.split_tokens - 1) / a.split_tokens;
   const int64_t rec = record_at(a, orow, 0);
-  const float* sums = record_sums(a, kDh, rec) + 4 * (ln % kLanes);
+  const int tid = kWavesPer == 1 ? ln : threadIdx.x;
+  const float* sums = record_sums(a, kDh, rec) + 4 * (tid % kLanes);
   const f32x2u* ml = record_ml(a, kDh, rec);
-  float m = -INFINITY, l = 0.f;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  for (int32_t s = ln / kLanes; s < n; s += kParts) {
-    const f32x2u x = ml[s];
-    const f32x4u y = *reinterpret_cast<const f32x4u*>(sums + int64_t(s) * kDh);
-    // (a split whose scores are all NaN has a max of -inf, and a sum of NaN)
-    if (x[0] == -INFINITY && x[1] == 0.f) continue;
-    const float mn = fmaxf(m, x[0]);
-    const float c = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - mn);
-    const float w = x[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(x[0] - mn);
-    m = mn;
-    l = l * c + x[1] * w;
+  Running x{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+  for (int32_t s = tid / kLanes; s < n; s += kParts * kMergeChunk) {
+    Running y[kMergeChunk];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = v[k] * c + y[k] * w;
+    for (int j = 0; j < kMergeChunk; ++j) {      // (past the end: the first record, not used)
+      const int32_t at = s + j * kParts < n ? s + j * kParts : 0;
+      const f32x2u m = ml[at];
+      y[j] = Running{m[0], m[1], *reinterpret_cast<const f32x4u*>(sums + int64_t(at) * kDh)};
+    }
+#pragma unroll
+    for (int j = 0; j < kMergeChunk; ++j)
+      if (s + j * kParts < n) x = join(x, y[j]);
   }
 #pragma unroll
   for (int off = kLanes; off < 64; off *= 2) {
-    const float m2 = __shfl_xor(m, off), l2 = __shfl_xor(l, off);
-    const float mn = fmaxf(m, m2);
-    const float c = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - mn);
-    const float w = m2 == -INFINITY ? (l2 == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m2 - mn);
-    l = l * c + l2 * w;
+    Running y;
+    y.m = __shfl_xor(x.m, off);
+    y.l = __shfl_xor(x.l, off);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = v[k] * c + __shfl_xor(v[k], off) * w;
-    m = mn;
+    for (int k = 0; k < 4; ++k) y.v[k] = __shfl_xor(x.v[k], off);
+    x = join(x, y);
+  }
+  if constexpr (kWavesPer > 1) {
+    __shared__ float s_ml[kWavesPer][2];
+    __shared__ f32x4 s_v[kWavesPer][kLanes];
+    if (ln < kLanes) s_v[wave][ln] = x.v;
+    if (ln == 0) {
+      s_ml[wave][0] = x.m;
+      s_ml[wave][1] = x.l;
+    }
+    __syncthreads();
+    if (threadIdx.x >= kLanes) return;
+    x = Running{s_ml[0][0], s_ml[0][1], s_v[0][ln]};
+#pragma unroll
+    for (int k = 1; k < kWavesPer; ++k) x = join(x, Running{s_ml[k][0], s_ml[k][1], s_v[k][ln]});
   }
   if (ln < kLanes) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const u32x2 w = {pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv)};
-    *reinterpret_cast<u32x2*>(a.out + orow * kDh + 4 * ln) = w;
+    const float inv = x.l == 0.f ? 0.f : 1.f / x.l;
+    const u32x2 y = {pack_bf16(x.v[0] * inv, x.v[1] * inv), pack_bf16(x.v[2] * inv, x.v[3] * inv)};
+    *reinterpret_cast<u32x2*>(a.out + orow * kDh + 4 * ln) = y;
   }
 }
 
-// Tokens a split takes where the caller leaves it to the library.
-int32_t auto_split(int64_t n_tokens, int32_t n_req, int32_t kv_heads, int32_t group,
-                   int32_t max_new, int32_t max_seq_len) {
-  const int64_t by_req = int64_t(n_req) * ((int64_t(max_new) * group + kRows - 1) / kRows);
-  const int64_t tiles = std::min(by_req, n_tokens * group / kRows + n_req) * kv_heads;
-  const int64_t want = tiles >= 256 ? 1 : (512 + tiles - 1) / std::max<int64_t>(tiles, 1);
-  int64_t s = (int64_t(max_seq_len) + want - 1) / want;
-  s = std::max<int64_t>((s + kKeys - 1) / kKeys * kKeys, 4 * kKeys);
-  return int32_t(std::min<int64_t>(s, (int64_t(INT32_MAX) / kKeys) * kKeys));
+typedef void (*ChunkFn)(ChunkArgs);
+
+// The forms, by how many rows a request brings and how many workgroups there are.
+struct Kind {
+  int rows, threads, step;
+  ChunkFn fn[2];                                 // head_dim 64, 128
+};
+template <class F64, class F128>
+constexpr Kind kind_of() {
+  static_assert(F64::kRows == F128::kRows && F64::kThreads == F128::kThreads &&
+                F64::kStep == F128::kStep);
+  return Kind{F64::kRows, F64::kThreads, F64::kStep, {chunk_attn<F64>, chunk_attn<F128>}};
+}
+const Kind kKinds[] = {
+    {16, kFewThreads, kFewTile, {chunk_attn_few<64, 1>, chunk_attn_few<128, 1>}},
+    {32, kFewThreads, kFewTile, {chunk_attn_few<64, 2>, chunk_attn_few<128, 2>}},
+    kind_of<Form<64, 4, 2>, Form<128, 4, 2>>(),
+    kind_of<Form<64, 8, 1>, Form<128, 8, 1>>(),
+};
+constexpr int kSplitUnit = 64;
+
+// Tiles of `rows` rows that the batch has at most.
+int64_t tiles_of(int64_t n_tokens, int64_t n_req, int group, int64_t max_new, int rows) {
+  return std::min(n_req * ((max_new * group + rows - 1) / rows), n_tokens * group / rows + n_req);
 }
 
 struct Shape {
+  int kind;
   int32_t split, splits;
   int64_t need;
 };
 
-// The split of a call and the workspace that it takes.
+// CUs that a call is spread over (MI355X's, also where no device is asked).
+constexpr int kCus = 256;
+
+// The form and the split of a call, and the workspace that it takes.
 int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads,
                int32_t head_dim, int32_t max_new, int32_t max_seq_len, int32_t split_tokens,
                Shape* out) {
@@ -473,11 +1011,23 @@ int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_head
     return fail(FLOWKV_EINVAL, "head_dim %d: need 64 or 128", head_dim);
   if (kv_heads < 1 || q_heads < 1 || q_heads % kv_heads)
     return fail(FLOWKV_EINVAL, "q_heads %d not a multiple of kv_heads %d", q_heads, kv_heads);
-  if (split_tokens < 0 || split_tokens % kKeys)
-    return fail(FLOWKV_EINVAL, "split_tokens %d: need 0 or a multiple of %d", split_tokens, kKeys);
-  if (split_tokens == 0)
-    split_tokens =
-        auto_split(n_tokens, n_req, kv_heads, q_heads / kv_heads, max_new, max_seq_len);
+  if (split_tokens < 0 || split_tokens % kSplitUnit)
+    return fail(FLOWKV_EINVAL, "split_tokens %d: need 0 or a multiple of %d", split_tokens,
+                kSplitUnit);
+  const int group = q_heads / kv_heads;
+  out->kind = 3;
+  if (int64_t(max_new) * group <= 32 && split_tokens <= kFewSplit)
+    out->kind = int64_t(max_new) * group > 16;
+  else if (tiles_of(n_tokens, n_req, group, max_new, kKinds[3].rows) * kv_heads < kCus) out->kind = 2;
+  const int64_t tiles =
+      std::max<int64_t>(tiles_of(n_tokens, n_req, group, max_new, kKinds[out->kind].rows) * kv_heads, 1);
+  if (split_tokens == 0) {
+    const int64_t aim = out->kind <= 1 ? 4 * kCus : kCus, want = (aim + tiles - 1) / tiles;
+    int64_t s = (int64_t(max_seq_len) + want - 1) / want;
+    s = std::max<int64_t>((s + 127) / 128 * 128, 256);
+    if (out->kind <= 1) s = std::min<int64_t>(s, kFewSplit);
+    split_tokens = int32_t(std::min<int64_t>(s, INT32_MAX / kSplitUnit * kSplitUnit));
+  }
   out->split = split_tokens;
   out->splits = int32_t((int64_t(max_seq_len) + split_tokens - 1) / split_tokens);
   if (out->splits < 1) out->splits = 1;
@@ -593,22 +1143,27 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   a.split_tokens = sh.split;
   a.splits = sh.splits;
   a.scale_log2 = scale * kLog2e;
-  const int64_t tiles = int64_t(n_tokens) * a.group / kRows + n_req;
+  const Kind& kind = kKinds[sh.kind];
+  a.rows = kind.rows;
+  const int64_t tiles = int64_t(n_tokens) * a.group / kind.rows + n_req;
   const int64_t grid = tiles * kv_heads;
-  const int64_t merge = (int64_t(n_tokens) * q_heads + kWaves - 1) / kWaves;
+  // a wave per (new token, query head) where its lane groups hold all records at once
+  const bool one = sh.splits <= kMergeChunk * 64 * 4 / head_dim;
+  const int64_t out_rows = int64_t(n_tokens) * q_heads, merge = one ? (out_rows + 3) / 4 : out_rows;
   if (grid > INT32_MAX / sh.splits || merge > INT32_MAX)
     return fail(FLOWKV_EINVAL, "%lld tiles of queries x %d splits: too many for one call",
                 (long long)grid, sh.splits);
   a.tiles = int32_t(tiles);
   void* args[] = {&a};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const void* fn = head_dim == 64 ? reinterpret_cast<const void*>(chunk_attn<64>)
-                                  : reinterpret_cast<const void*>(chunk_attn<128>);
-  hipError_t e = hipLaunchKernel(fn, dim3(unsigned(grid * sh.splits)), dim3(kThreads), args, 0, st);
+  hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kind.fn[head_dim == 128]),
+                                 dim3(unsigned(grid * sh.splits)), dim3(unsigned(kind.threads)), args,
+                                 0, st);
   if (e == hipSuccess && sh.splits > 1) {
-    fn = head_dim == 64 ? reinterpret_cast<const void*>(chunk_attn_merge<64>)
-                        : reinterpret_cast<const void*>(chunk_attn_merge<128>);
-    e = hipLaunchKernel(fn, dim3(unsigned(merge)), dim3(kThreads), args, 0, st);
+    ChunkFn fn = head_dim == 64 ? (one ? chunk_attn_merge<64, 1> : chunk_attn_merge<64, 4>)
+                                : (one ? chunk_attn_merge<128, 1> : chunk_attn_merge<128, 4>);
+    e = hipLaunchKernel(reinterpret_cast<const void*>(fn), dim3(unsigned(merge)),
+                        dim3(kMergeThreads), args, 0, st);
   }
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess) return fail(FLOWKV_EHIP, "chunk attention launch: %s", hipGetErrorString(e));

@@ -51,7 +51,8 @@ BATCHES = [  # (new tokens, tokens in all) of each request
     ([1], [1]), ([1, 1, 1], [1, 64, 65]), ([5], [300]), ([0, 3, 0, 2, 0], [9, 40, 0, 2, 700]),
     ([200], [200]), ([31, 33, 1], [31, 500, 129]), ([128, 127, 129], [128, 400, 129]),
     ([1, 260, 1, 70], [1000, 260, 63, 900]), ([16] * 9, [16 * (i + 1) for i in range(9)]),
-    ([2, 8, 4, 1], [1500, 700, 4, 2000]), ([700], [1400]),
+    ([2, 8, 4, 1], [1500, 700, 4, 2000]), ([700], [1400]), ([1, 2, 1], [5000, 2049, 2048]),
+    ([3], [9000]),
 ]
 
 
@@ -61,7 +62,7 @@ def test_against_the_formula(shape, batch):
     L, hk, d, bs, G = SHAPES[shape]
     seed = 31 * shape + batch
     layout = (BM, LM)[seed % 2]
-    split = [0, 64, 128, 0, 1024][seed % 5]
+    split = [0, 64, 128, 0, 1024, 2048, 4096][seed % 7]
     geom = Geometry(f"chunk{shape}", L, hk, d, bs, "bfloat16")
     b = Batch(geom, layout, *BATCHES[batch], seed, pad=(seed % 3, seed % 4))
     say(f"chunk attention {NAMES[layout]} shape {SHAPES[shape]} new {b.new.tolist()} of "
@@ -189,6 +190,28 @@ def test_odd_values_reach_only_the_rows_that_see_them(d, split, bad):
     assert torch.equal(out[rows], ref[rows])
     rows = torch.as_tensor(first + np.flatnonzero(sees), device="cuda")
     assert torch.isnan(out[rows].float()).all()
+
+
+@pytest.mark.parametrize("new", [3, 7, 60])
+@pytest.mark.parametrize("d", [64, 128])
+def test_odd_values_beside_missing_blocks_reach_every_row(d, new):
+    """A block outside the pool in the middle of what every row sees: infinities of the
+    tokens around it count as they do elsewhere."""
+    geom = Geometry("chunkodd2", 1, 1, d, 4, "bfloat16")
+    b = Batch(geom, LM, [new], [300], 19)
+    t = b.layer_view(0)
+    b.tab[0, 20] = b.blocks + 3
+    b.upload()
+    q = queries(b, 4, 19)
+    ref = attend(b, 0, q, 0.1)
+    check_attention(b, 0, q, 0.1, ref)
+    t[1, int(b.tab[0, 19]), 2, 0, 7] = float("inf")         # tokens 78 and 85
+    t[1, int(b.tab[0, 21]), 1, 0, 9] = float("-inf")
+    out = attend(b, 0, q, 0.1)
+    assert (out[:, :, 7].float() == float("inf")).all()
+    assert (out[:, :, 9].float() == float("-inf")).all()
+    rest = [i for i in range(d) if i not in (7, 9)]
+    assert torch.equal(out[:, :, rest], ref[:, :, rest])
 
 
 @pytest.mark.parametrize("split", [0, 64])
