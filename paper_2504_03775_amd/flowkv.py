@@ -528,6 +528,7 @@ class KVPool:
         self._bases = (ctypes.c_void_p * len(self.tensors))(*[x.data_ptr() for x in self.tensors])
         self.desc = flowkv_pool(layout, L, B, 0, self.chunk_bytes,
                                 ctypes.cast(self._bases, ctypes.POINTER(ctypes.c_void_p)))
+        self.ref = ctypes.byref(self.desc)
 
 
 def _stream_handle(stream) -> Optional[int]:
@@ -720,45 +721,63 @@ def flowkv_decode_attention(pool: KVPool, layer: int, q, block_tables, seq_lens,
         "flowkv_decode_attention")
 
 
-def _on_pool_device(pool: KVPool, stream, call, where: str) -> None:
-    """``call(stream handle)`` with the pool's device current."""
+def _on_pool_device(pool: KVPool, stream, where: str, fn, *args) -> None:
+    """``fn(pool, *args, stream)`` with the pool's device current: the library
+    launches on the current device.  Addresses go as plain integers, and the
+    current device and stream come from torch's private calls where it has them
+    (append of a decode step, 8.8 us of host time without either)."""
     import torch
 
     if stream is not None and stream.device != pool.device:
         raise ValueError(f"{where}: the stream is on {stream.device}, the pool on {pool.device}")
-    if pool.device.index == torch.cuda.current_device():
-        _check(call(ctypes.c_void_p(_stream_handle(stream))), where)
+    index = pool.device.index
+    try:
+        current, raw = torch._C._cuda_getDevice(), torch._C._cuda_getCurrentRawStream
+    except AttributeError:
+        current = torch.cuda.current_device()
+
+        def raw(i):
+            return torch.cuda.current_stream(i).cuda_stream
+    handle = raw(index) if stream is None else stream.cuda_stream
+    if current == index:
+        rc = fn(pool.ref, *args, handle)
     else:
-        with torch.cuda.device(pool.device):
-            _check(call(ctypes.c_void_p(_stream_handle(stream))), where)
+        with torch.cuda.device(index):
+            rc = fn(pool.ref, *args, handle)
+    if rc != OK:
+        raise FlowKVError(rc, where)
 
 
 def _check_ragged(pool: KVPool, q_offsets, block_tables, seq_lens) -> int:
     """The batch arrays of flowkv_append and flowkv_chunk_attention; the requests' count."""
     import torch
 
+    dev, i32 = pool.device, torch.int32
     n = seq_lens.numel()
     for t, dims in ((q_offsets, 1), (block_tables, 2), (seq_lens, 1)):
-        if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() \
-                or t.device != pool.device:
+        if t.dtype is not i32 or t.dim() != dims or not t.is_contiguous() or t.device != dev:
             raise ValueError(f"q_offsets, block_tables and seq_lens: need contiguous int32 tensors "
-                             f"of 1, 2 and 1 dimensions on {pool.device}, got {t.dtype} "
-                             f"{tuple(t.shape)} on {t.device}")
-    if q_offsets.numel() != n + 1 or block_tables.shape[0] != n:
+                             f"of 1, 2 and 1 dimensions on {dev}, got {t.dtype} {tuple(t.shape)} "
+                             f"on {t.device}")
+    if q_offsets.numel() != n + 1 or len(block_tables) != n:
         raise ValueError(f"{n} lengths, {q_offsets.numel()} offsets (one more is needed) and "
-                         f"{block_tables.shape[0]} block lists")
+                         f"{len(block_tables)} block lists")
     return n
 
 
-def _token_stride(t, name: str, shape, dtype, device) -> int:
-    """Elements between the tokens of a (n, heads, head_dim) tensor whose tokens
-    are each in one piece."""
-    if t.dim() != 3 or tuple(t.shape[1:]) != tuple(shape) or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name}: need (tokens, {shape[0]}, {shape[1]}) {dtype} on {device}, got "
-                         f"{tuple(t.shape)} {t.dtype} on {t.device}")
-    if t.numel() and (t.stride(2) != 1 or (shape[0] > 1 and t.stride(1) != shape[1])):
-        raise ValueError(f"{name}: a token's heads must lie together, strides are {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else shape[0] * shape[1]
+def _token_stride(t, name: str, heads: int, dim: int, dtype, device) -> int:
+    """Elements between the tokens of a (n, heads, dim) tensor whose tokens are
+    each in one piece."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or t.dtype is not dtype \
+            or t.device != device:
+        raise ValueError(f"{name}: need (tokens, {heads}, {dim}) {dtype} on {device}, got "
+                         f"{tuple(shape)} {t.dtype} on {t.device}")
+    if shape[0] == 0:
+        return heads * dim
+    if (dim > 1 and stride[2] != 1) or (heads > 1 and stride[1] != dim):
+        raise ValueError(f"{name}: a token's heads must lie together, strides are {stride}")
+    return stride[0] if shape[0] > 1 else heads * dim
 
 
 def flowkv_append(pool: KVPool, layer: int, k, v, q_offsets, block_tables, seq_lens,
@@ -770,17 +789,15 @@ def flowkv_append(pool: KVPool, layer: int, k, v, q_offsets, block_tables, seq_l
     (n_req,) int32 on the pool's device, the lengths counted with the new
     tokens."""
     n_req = _check_ragged(pool, q_offsets, block_tables, seq_lens)
-    shape, dtype = (pool.kv_heads, pool.head_dim), pool.tensors[0].dtype
-    ks = _token_stride(k, "k", shape, dtype, pool.device)
-    vs = _token_stride(v, "v", shape, dtype, pool.device)
-    if k.shape[0] != v.shape[0]:
-        raise ValueError(f"{k.shape[0]} tokens of K and {v.shape[0]} of V")
-    e = pool.elem_bytes
-    _on_pool_device(pool, stream, lambda s: _lib.flowkv_append(
-        ctypes.byref(pool.desc), layer, ctypes.c_void_p(k.data_ptr()), ks * e,
-        ctypes.c_void_p(v.data_ptr()), vs * e, pool.kv_heads * pool.head_dim * e, k.shape[0], n_req,
-        ctypes.c_void_p(q_offsets.data_ptr()), ctypes.c_void_p(block_tables.data_ptr()),
-        block_tables.shape[1], ctypes.c_void_p(seq_lens.data_ptr()), s), "flowkv_append")
+    h, d, e, dtype = pool.kv_heads, pool.head_dim, pool.elem_bytes, pool.tensors[0].dtype
+    ks = _token_stride(k, "k", h, d, dtype, pool.device)
+    vs = _token_stride(v, "v", h, d, dtype, pool.device)
+    n = k.shape[0]
+    if v.shape[0] != n:
+        raise ValueError(f"{n} tokens of K and {v.shape[0]} of V")
+    _on_pool_device(pool, stream, "flowkv_append", _lib.flowkv_append, layer, k.data_ptr(), ks * e,
+                    v.data_ptr(), vs * e, h * d * e, n, n_req, q_offsets.data_ptr(),
+                    block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr())
 
 
 def flowkv_chunk_attention_workspace(n_tokens: int, n_req: int, q_heads: int, kv_heads: int,
@@ -806,15 +823,15 @@ def flowkv_chunk_attention(pool: KVPool, layer: int, q, q_offsets, block_tables,
     import torch
 
     n_req = _check_ragged(pool, q_offsets, block_tables, seq_lens)
-    if any(t.dtype != torch.bfloat16 for t in pool.tensors):
+    if pool.tensors[0].dtype is not torch.bfloat16:      # (a pool's tensors have one type)
         raise ValueError(f"attention reads bfloat16 K/V: the pool holds {pool.tensors[0].dtype}")
     if q.dim() != 3:
         raise ValueError(f"q: need (tokens, heads, head_dim), got {tuple(q.shape)}")
     n, hq, dh = q.shape
     if dh != pool.head_dim:
         raise ValueError(f"q has a head_dim of {dh}, the pool of {pool.head_dim}")
-    qs = _token_stride(q, "q", (hq, dh), torch.bfloat16, pool.device)
-    if tuple(out.shape) != (n, hq, dh) or out.dtype != torch.bfloat16 or not out.is_contiguous() \
+    qs = _token_stride(q, "q", hq, dh, torch.bfloat16, pool.device)
+    if out.shape != q.shape or out.dtype is not torch.bfloat16 or not out.is_contiguous() \
             or out.device != pool.device:
         raise ValueError(f"out: need contiguous {(n, hq, dh)} bfloat16 on {pool.device}, got "
                          f"{tuple(out.shape)} {out.dtype} on {out.device}")
@@ -823,13 +840,10 @@ def flowkv_chunk_attention(pool: KVPool, layer: int, q, q_offsets, block_tables,
         if not workspace.is_contiguous() or workspace.device != pool.device:
             raise ValueError("attention workspace: not a contiguous tensor on the pool's device")
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _on_pool_device(pool, stream, lambda s: _lib.flowkv_chunk_attention(
-        ctypes.byref(pool.desc), layer, ctypes.c_void_p(q.data_ptr()), qs, n, n_req, hq,
-        pool.kv_heads, dh, ctypes.c_void_p(q_offsets.data_ptr()),
-        ctypes.c_void_p(block_tables.data_ptr()), block_tables.shape[1],
-        ctypes.c_void_p(seq_lens.data_ptr()), max_new, max_seq_len, scale, split_tokens,
-        ctypes.c_void_p(out.data_ptr()), ctypes.c_void_p(ws), ws_bytes, s),
-        "flowkv_chunk_attention")
+    _on_pool_device(pool, stream, "flowkv_chunk_attention", _lib.flowkv_chunk_attention, layer,
+                    q.data_ptr(), qs, n, n_req, hq, pool.kv_heads, dh, q_offsets.data_ptr(),
+                    block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), max_new,
+                    max_seq_len, scale, split_tokens, out.data_ptr(), ws, ws_bytes)
 
 
 def flowkv_copy_blocks(pool: KVPool, src_ids, dst_ids, tokens=None, stream=None) -> None:
@@ -840,10 +854,9 @@ def flowkv_copy_blocks(pool: KVPool, src_ids, dst_ids, tokens=None, stream=None)
     k = None if tokens is None else _i32(tokens)
     if s.ndim != 1 or d.shape != s.shape or (k is not None and k.shape != s.shape):
         raise ValueError("source, destination and token lists differ in length")
-    slot = pool.kv_heads * pool.head_dim * pool.elem_bytes
-    _on_pool_device(pool, stream, lambda st: _lib.flowkv_copy_blocks(
-        ctypes.byref(pool.desc), _ptr(s), _ptr(d), None if k is None else _ptr(k), s.size, slot,
-        st), "flowkv_copy_blocks")
+    _on_pool_device(pool, stream, "flowkv_copy_blocks", _lib.flowkv_copy_blocks, _ptr(s), _ptr(d),
+                    None if k is None else _ptr(k), s.size,
+                    pool.kv_heads * pool.head_dim * pool.elem_bytes)
 
 
 def segments_to_device(segs: np.ndarray, device, stream=None):
