@@ -45,12 +45,16 @@ struct AppendArgs {
 // or with a block outside the pool is dropped.
 //
 // Work: the 16-byte pieces of all tokens' K and V, in order; a wave takes 64
-// consecutive ones kAppendUnroll times.  What bounds it: up to a few thousand
-// tokens a launch and three dependent loads (the offsets, the length, the table
-// entry); the data's own loads are under way meanwhile.
+// consecutive ones, or twice 64 in a long call.  What bounds it: up to a few hundred
+// tokens a launch and its dependent loads (the offsets, the length, the table
+// entry), with the data's own loads under way meanwhile: 32 tokens of 8 KV heads of
+// 128 take 2.9 us in a graph (3.2 with two pieces a lane, 4.1 with four).  A long
+// call is bound by memory: 18,750 tokens of one KV head (19.2 MB read and written)
+// 6.3 us, 6.9 with one piece a lane; the two are level at 2^18 pieces.
 constexpr int kAppendThreads = 256;
-constexpr int kAppendUnroll = 4;
+constexpr int64_t kAppendFew = 1 << 18;              // pieces up to which a lane takes one
 
+template <int kAppendUnroll>
 __global__ __launch_bounds__(kAppendThreads) void kv_append(const AppendArgs a) {
   const int ln = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -81,6 +85,10 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append(const AppendArgs a) 
   const int32_t r1 =
       t1 == t0 ? r0
                : flowkv::last_at_most(a.n_req, t1, [&](int32_t r) { return a.offsets[r]; });
+  // no branch but the search's, so that the pieces' loads are under way together
+  uint32_t slot[kAppendUnroll];
+  int32_t id[kAppendUnroll];
+  bool in[kAppendUnroll];
 #pragma unroll
   for (int u = 0; u < kAppendUnroll; ++u) {
     int32_t r = r0;
@@ -94,15 +102,18 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append(const AppendArgs a) 
     }
     const int32_t begin = a.offsets[r], end = a.offsets[r + 1];
     const int64_t p = int64_t(a.seq_lens[r]) - (int64_t(end) - begin) + (token[u] - begin);
-    const uint64_t b = uint64_t(p) / uint32_t(a.block_size);
-    const bool in = first + u * 64 + ln < items && token[u] >= begin && token[u] < end && p >= 0 &&
-                    b < uint64_t(a.max_blocks);
-    const int32_t id = in ? a.tables[int64_t(r) * a.max_blocks + int64_t(b)] : -1;
-    if (id < 0 || id >= a.pool_blocks) continue;
+    const uint32_t b = uint32_t(p) / uint32_t(a.block_size);   // p < 2^31: below a length
+    in[u] = first + u * 64 + ln < items && token[u] >= begin && token[u] < end && p >= 0 &&
+            b < uint32_t(a.max_blocks);
+    id[u] = a.tables[in[u] ? int64_t(r) * a.max_blocks + b : 0];
+    slot[u] = uint32_t(p) - b * uint32_t(a.block_size);
+  }
+#pragma unroll
+  for (int u = 0; u < kAppendUnroll; ++u) {
+    if (!in[u] || id[u] < 0 || id[u] >= a.pool_blocks) continue;
     const bool v = piece[u] >= uint32_t(a.pieces);
-    const int64_t slot = p - int64_t(b) * a.block_size;
-    char* dst = a.kbase + (v ? a.voff : 0) + id * a.bstride +
-                (slot * a.pieces + (v ? piece[u] - a.pieces : piece[u])) * 16;
+    char* dst = a.kbase + (v ? a.voff : 0) + id[u] * a.bstride +
+                (int64_t(slot[u]) * a.pieces + (v ? piece[u] - a.pieces : piece[u])) * 16;
     *(gvec*)dst = x[u];
   }
 }
@@ -116,6 +127,9 @@ struct PairTokens {
   int32_t src, dst, tokens;
 };
 
+__device__ inline int32_t tokens_of(const PairOf&) { return 0; }
+__device__ inline int32_t tokens_of(const PairTokens& r) { return r.tokens; }
+
 template <class Rec, int kBases, int kRecs>
 struct CopyArgs {
   typedef Rec Record;
@@ -126,7 +140,8 @@ struct CopyArgs {
   int32_t n;                          // records
   int32_t num_layers;
   int32_t slot_pieces;                // 16-byte pieces of a slot (token counts only)
-  int32_t tiles;                      // of a whole block
+  int32_t chunk_pieces;               // the most that a record moves of a chunk
+  int32_t tiles;                      // of a record, or of a plane
   int64_t perm_mul;
   char* base[kBases];
   Rec rec[kRecs];
@@ -143,29 +158,35 @@ static_assert(sizeof(CopyLM) + kImplicitArgBytes <= 4096, "kernel arguments");
 static_assert(sizeof(CopyTokensBM) + kImplicitArgBytes <= 4096, "kernel arguments");
 static_assert(sizeof(CopyTokensLM) + kImplicitArgBytes <= 4096, "kernel arguments");
 
-constexpr int kCopyUnroll = 4;
+// The two kernels below move the same bytes: of each record the first `tokens`
+// slots (all of them without token counts) of its 2 L chunks, in 16-byte pieces.
+// Both are bound by memory.  A call that reads and writes up to 256 MiB takes the
+// first, a larger one the second: of 2 MiB blocks (32 layers of 8 x 128, block-major)
+// 60 take 37.9 us in the first and 39.4 in the second, 90 take 66.2 and 59.2, 1,000
+// take 774 and 643 (6.5 TB/s); 24 partly filled ones 9.3 and 12.0.
+//
+// The first: what it reads was written a moment ago as a rule (the block that a
+// prompt ends in) and is looked for in the caches.  A record's pieces are one span,
+// two pieces a lane, 512 lanes, a record's tiles together, records scattered
+// (x -> x m mod n).
+constexpr int kCopyThreads = 512;
+constexpr int kCopyUnroll = 2;
 
-// A record's bytes: the first `tokens` slots (all of them without token counts)
-// of each of its 2 L chunks, taken as one span of 16-byte pieces, tile by tile.
 template <class A, bool kLM>
-__global__ __launch_bounds__(1024) void kv_block_copy(const A a) {
+__global__ __launch_bounds__(kCopyThreads) void kv_block_copy(const A a) {
   constexpr bool kTokens = sizeof(typename A::Record) == sizeof(PairTokens);
   __shared__ char* s_base[kLM ? FLOWKV_MAX_LAYERS : 1];
-  const uint32_t line = blockDim.x;
-  // blocks scattered (x -> x m mod n, m coprime to n): tile-major in a block-major
-  // pool, a block's tiles together in a layer-major one
-  const uint32_t u = blockIdx.x;
-  const uint32_t t = kLM ? u % uint32_t(a.tiles) : u / uint32_t(a.n);
-  const uint32_t i0 = kLM ? u / uint32_t(a.tiles) : u % uint32_t(a.n);
-  const uint32_t i = uint32_t(uint64_t(i0) * uint64_t(a.perm_mul) % uint32_t(a.n));
+  const uint32_t t = blockIdx.x % uint32_t(a.tiles);
+  const uint32_t i =
+      uint32_t(uint64_t(blockIdx.x / uint32_t(a.tiles)) * uint64_t(a.perm_mul) % uint32_t(a.n));
   const int64_t src = a.rec[i].src, dst = a.rec[i].dst;
   uint32_t chunk = uint32_t(a.chunk_bytes / 16);     // pieces moved of a chunk
   if constexpr (kTokens) chunk = uint32_t(a.rec[i].tokens) * uint32_t(a.slot_pieces);
   const uint32_t span = chunk * 2u * uint32_t(a.num_layers);
-  const uint32_t o0 = t * (line * kCopyUnroll);
+  const uint32_t o0 = t * uint32_t(kCopyThreads * kCopyUnroll);
   if (o0 >= span) return;
   if constexpr (kLM) {
-    for (uint32_t l = threadIdx.x; l < uint32_t(a.num_layers); l += blockDim.x)
+    for (uint32_t l = threadIdx.x; l < uint32_t(a.num_layers); l += kCopyThreads)
       s_base[l] = a.base[l];
     __syncthreads();
   }
@@ -184,14 +205,51 @@ __global__ __launch_bounds__(1024) void kv_block_copy(const A a) {
   u32x4 x[kCopyUnroll];
 #pragma unroll
   for (int k = 0; k < kCopyUnroll; ++k) {
-    const uint32_t o = o0 + k * line + threadIdx.x;
-    if (o < span) x[k] = __builtin_nontemporal_load((cgvec*)at(src, o));
+    const uint32_t o = o0 + k * kCopyThreads + threadIdx.x;
+    if (o < span) x[k] = *(cgvec*)at(src, o);
   }
 #pragma unroll
   for (int k = 0; k < kCopyUnroll; ++k) {
-    const uint32_t o = o0 + k * line + threadIdx.x;
+    const uint32_t o = o0 + k * kCopyThreads + threadIdx.x;
     if (o < span) __builtin_nontemporal_store(x[k], (gvec*)at(dst, o));
   }
+}
+
+// The second: one wave and one piece a lane to a workgroup, past the caches, so that
+// the memory's channels are shared out in steps of 1 KiB.  (64 lanes x 1 piece: 643
+// us at the 1,000 blocks above; 64 x 2: 711, 256 x 1: 713, 1,024 x 4: 716.)  A
+// block-major record's tiles follow each other; a layer-major launch goes plane by
+// plane (a layer's K, or its V), each plane's pieces of all records in order: 1,500
+// blocks of 80 layers of 4 KiB chunks take 337 us (5.8 TB/s), block by block 384.
+constexpr int kStreamThreads = 64;
+
+template <class A, bool kLM>
+__global__ __launch_bounds__(kStreamThreads) void kv_block_stream(const A a) {
+  constexpr bool kTokens = sizeof(typename A::Record) == sizeof(PairTokens);
+  const uint32_t t = blockIdx.x % uint32_t(a.tiles), u = blockIdx.x / uint32_t(a.tiles);
+  const uint32_t o = t * kStreamThreads + threadIdx.x;
+  const char* src;
+  char* dst;
+  if constexpr (kLM) {
+    const uint32_t chunk = uint32_t(a.chunk_pieces);
+    const uint32_t i = o / chunk, w = o - i * chunk;
+    if (i >= uint32_t(a.n)) return;
+    if constexpr (kTokens)
+      if (w >= uint32_t(a.rec[i].tokens) * uint32_t(a.slot_pieces)) return;
+    char* plane = a.base[u >> 1] + int64_t(u & 1) * a.num_blocks * a.chunk_bytes + int64_t(w) * 16;
+    src = plane + int64_t(a.rec[i].src) * a.chunk_bytes;
+    dst = plane + int64_t(a.rec[i].dst) * a.chunk_bytes;
+  } else {
+    const uint32_t i = uint32_t(uint64_t(u) * uint64_t(a.perm_mul) % uint32_t(a.n));
+    const uint32_t chunk =
+        kTokens ? uint32_t(tokens_of(a.rec[i])) * uint32_t(a.slot_pieces) : uint32_t(a.chunk_pieces);
+    if (o >= chunk * 2u * uint32_t(a.num_layers)) return;
+    int64_t off = int64_t(o) * 16;
+    if constexpr (kTokens) off = int64_t(o / chunk) * a.chunk_bytes + int64_t(o % chunk) * 16;
+    src = a.base[0] + a.rec[i].src * a.block_bytes + off;
+    dst = a.base[0] + a.rec[i].dst * a.block_bytes + off;
+  }
+  __builtin_nontemporal_store(__builtin_nontemporal_load((cgvec*)src), (gvec*)dst);
 }
 
 // The pool's descriptor, as every call here checks it.
@@ -233,8 +291,8 @@ extern "C" int flowkv_append(const flowkv_pool* pool, int32_t layer, const void*
                 "slot of %lld bytes: need a multiple of 16 that divides chunk_bytes %lld",
                 (long long)slot_bytes, (long long)pool->chunk_bytes);
   if (n_tokens < 0 || n_req < 0 || max_blocks < 0) return fail(FLOWKV_EINVAL, "negative sizes");
-  if (n_tokens == 0 || n_req == 0) return ok();
-  if (!k_dev || !v_dev || !offsets_dev || !seq_lens_dev || (max_blocks > 0 && !block_tables_dev))
+  if (n_tokens == 0 || n_req == 0 || max_blocks == 0) return ok();
+  if (!k_dev || !v_dev || !offsets_dev || !seq_lens_dev || !block_tables_dev)
     return fail(FLOWKV_EINVAL, "NULL device pointer");
   if (reinterpret_cast<uintptr_t>(k_dev) % 16 || reinterpret_cast<uintptr_t>(v_dev) % 16 ||
       k_stride % 16 || v_stride % 16)
@@ -261,15 +319,17 @@ extern "C" int flowkv_append(const flowkv_pool* pool, int32_t layer, const void*
   a.pool_blocks = pool->num_blocks;
   a.block_size = int32_t(pool->chunk_bytes / slot_bytes);
   a.pieces = int32_t(slot_bytes / 16);
-  const int64_t per_group = int64_t(kAppendThreads) * kAppendUnroll;
-  const int64_t groups = (int64_t(n_tokens) * 2 * a.pieces + per_group - 1) / per_group;
-  if (groups > INT32_MAX)
+  const int64_t items = int64_t(n_tokens) * 2 * a.pieces;
+  const bool few = items <= kAppendFew;
+  const int64_t per_group = int64_t(kAppendThreads) * (few ? 1 : 2);
+  const int64_t groups = (items + per_group - 1) / per_group;
+  if (groups * kAppendThreads > UINT32_MAX)          // lanes of a launch
     return fail(FLOWKV_EINVAL, "%d tokens of %lld bytes: too many for one call", n_tokens,
                 (long long)slot_bytes);
   void* args[] = {&a};
-  hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kv_append), dim3(unsigned(groups)),
-                                 dim3(kAppendThreads), args, 0,
-                                 static_cast<hipStream_t>(hip_stream));
+  hipError_t e = hipLaunchKernel(
+      few ? reinterpret_cast<const void*>(kv_append<1>) : reinterpret_cast<const void*>(kv_append<2>),
+      dim3(unsigned(groups)), dim3(kAppendThreads), args, 0, static_cast<hipStream_t>(hip_stream));
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess) return fail(FLOWKV_EHIP, "append launch: %s", hipGetErrorString(e));
   return ok();
@@ -295,6 +355,9 @@ int check_pairs(const int32_t* src, const int32_t* dst, int32_t n, int32_t block
   return FLOWKV_OK;
 }
 
+// Bytes read and written by a call up to which the first kernel takes it.
+constexpr int64_t kCopyCached = int64_t(256) << 20;
+
 template <class A, bool kLM>
 int launch_copy(const flowkv_pool* p, const int32_t* src, const int32_t* dst,
                 const int32_t* tokens, int32_t n, int64_t slot_bytes, void* stream) {
@@ -308,28 +371,43 @@ int launch_copy(const flowkv_pool* p, const int32_t* src, const int32_t* dst,
   a.slot_pieces = int32_t(slot_bytes / 16);
   for (int i = 0; i < (kLM ? p->num_layers : 1); ++i)
     a.base[i] = static_cast<char*>(p->layer_base[i]);
-  const int threads = 1024;
-  for (int32_t at = 0; at < n; at += A::kMaxRecs) {
-    const int32_t m = std::min<int32_t>(n - at, A::kMaxRecs);
-    int64_t most = span;
-    if constexpr (kTokens) most = 0;
+  const int64_t planes = 2 * int64_t(p->num_layers);
+  int64_t all = n * span;
+  if constexpr (kTokens) {
+    all = 0;
+    for (int32_t i = 0; i < n; ++i) all += planes * tokens[i] * slot_bytes;
+  }
+  const bool stream_past = 2 * all > kCopyCached;
+  for (int32_t at = 0; at < n;) {
+    // a launch has fewer than 2^32 lanes, a piece each
+    const int32_t m =
+        int32_t(std::min<int64_t>({int64_t(n) - at, A::kMaxRecs,
+                                   std::max<int64_t>(1, (int64_t(1) << 31) / (span / 16))}));
+    int64_t most = kTokens ? 0 : p->chunk_bytes;       // moved of a chunk
     for (int32_t i = 0; i < m; ++i) {
       a.rec[i].src = src[at + i];
       a.rec[i].dst = dst[at + i];
       if constexpr (kTokens) {
         a.rec[i].tokens = tokens[at + i];
-        most = std::max(most, 2 * int64_t(p->num_layers) * tokens[at + i] * slot_bytes);
+        most = std::max(most, tokens[at + i] * slot_bytes);
       }
     }
+    at += m;
     if (most == 0) continue;
-    const int64_t tile = int64_t(threads) * kCopyUnroll * 16;
+    const bool by_plane = kLM && stream_past;
+    const int64_t pieces = most / 16 * (by_plane ? m : planes);
+    const int64_t line = stream_past ? kStreamThreads : kCopyThreads * kCopyUnroll;
     a.n = m;
-    a.tiles = int32_t((most + tile - 1) / tile);
+    a.chunk_pieces = int32_t(most / 16);
+    a.tiles = int32_t((pieces + line - 1) / line);
     a.perm_mul = int64_t(2654435761ull % uint64_t(m));   // a prime above m: a bijection mod m
     void* args[] = {&a};
-    hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kv_block_copy<A, kLM>),
-                                   dim3(unsigned(a.tiles) * unsigned(m)), dim3(threads), args, 0,
-                                   static_cast<hipStream_t>(stream));
+    hipError_t e = hipLaunchKernel(
+        stream_past ? reinterpret_cast<const void*>(kv_block_stream<A, kLM>)
+                    : reinterpret_cast<const void*>(kv_block_copy<A, kLM>),
+        dim3(unsigned(a.tiles) * unsigned(by_plane ? planes : m)),
+        dim3(stream_past ? kStreamThreads : kCopyThreads), args, 0,
+        static_cast<hipStream_t>(stream));
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess) return fail(FLOWKV_EHIP, "block copy launch: %s", hipGetErrorString(e));
   }

@@ -115,6 +115,27 @@ def test_append_of_a_whole_prompt_and_far_blocks():
         torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("layout", [BM, LM], ids=lambda x: NAMES[x])
+def test_a_long_append_of_many_requests_some_without_a_place(layout):
+    """More pieces than one a lane takes; requests of every length, empty ones, blocks
+    outside the pool, a length below its new tokens."""
+    g = np.random.default_rng(31)
+    new = [0, 700, 1, 0, 333, 64, 1, 1, 129, 0, 17] + [int(x) for x in g.integers(0, 40, 60)]
+    total = [m + int(x) for m, x in zip(new, g.integers(0, 300, len(new)))]
+    total[4] = new[4] - 100                            # the first 100 have no position
+    b = Batch(Geometry("appendlong", 2, 8, 72, 13, "bfloat16"), layout, new, total, 31)
+    assert b.n_tokens * 2 * 8 * 72 * 2 // 16 > 1 << 18
+    b.tab[1, 3], b.tab[5, 1], b.tab[8, 0] = -7, b.blocks, 2 ** 31 - 1
+    b.upload()
+    k, v = new_kv(b, 31, lead=16)
+    say(f"long append {NAMES[layout]} of {b.n_tokens} tokens")
+    want = [t.clone() for t in b.pool.tensors]
+    append_plain(b, 1, k, v, want)
+    fk.flowkv_append(b.pool, 1, k, v, *b.args())
+    torch.cuda.synchronize()
+    assert same(b.pool.tensors, want)
+
+
 def copy_plain(tensors, layout, src, dst, tokens, bs):
     for i, (s, d) in enumerate(zip(src, dst)):
         k = bs if tokens is None else int(tokens[i])
@@ -140,6 +161,30 @@ def test_copy_blocks(layout, shape, n, tokens):
     dst = ids[:n]
     src = g.choice(ids[n:], n).astype(np.int32)        # a source may repeat
     tok = g.integers(0, bs + 1, n).astype(np.int32) if tokens else None
+    say(f"copy {NAMES[layout]} {shape} {n} blocks tokens {tokens}")
+    want = [t.clone() for t in pool.tensors]
+    copy_plain(want, layout, src, dst, tok, bs)
+    fk.flowkv_copy_blocks(pool, src, dst, tok)
+    torch.cuda.synchronize()
+    assert same(pool.tensors, want)
+
+
+@pytest.mark.parametrize("tokens", [False, True], ids=["whole", "tokens"])
+@pytest.mark.parametrize("shape", [(80, 3, 72, 7), (6, 8, 128, 16), (2, 1, 8, 33333)])
+@pytest.mark.parametrize("layout", [BM, LM], ids=lambda x: NAMES[x])
+def test_copies_too_large_for_the_caches(layout, shape, tokens):
+    """Over 256 MiB read and written, by a few hundred blocks in several launches."""
+    L, hk, d, bs = shape
+    block = 2 * L * hk * d * bs * 2
+    n = (280 << 20) // block + 1                       # half as many bytes with token counts
+    g = np.random.default_rng(n)
+    B = 2 * n + 9
+    pool = fk.KVPool(layout, make_device_pool(Geometry("copyall", L, hk, d, bs, "bfloat16"), layout,
+                                              B, "cuda", n))
+    ids = g.permutation(B).astype(np.int32)
+    src, dst = g.choice(ids[n:], n).astype(np.int32), ids[:n]
+    tok = g.integers(0, bs + 1, n).astype(np.int32) if tokens else None
+    assert 2 * block * n // (2 if tokens else 1) > 256 << 20
     say(f"copy {NAMES[layout]} {shape} {n} blocks tokens {tokens}")
     want = [t.clone() for t in pool.tensors]
     copy_plain(want, layout, src, dst, tok, bs)
