@@ -489,12 +489,11 @@ int flowkv_append(const flowkv_pool* pool, int32_t layer, const void* k_dev, int
    length; both size the launch, and rows past max_new are computed all the
    same.  head_dim 64 or 128; any whole number of query heads per KV head.
    split_tokens: cached tokens per workgroup, a multiple of 64; 0 takes the
-   library's rule.  One launch on hip_stream, two where max_seq_len is more than
-   split_tokens; then workspace_dev holds at least
-   flowkv_chunk_attention_workspace(...) bytes, owned by the caller and busy
-   until the stream passes the call (NULL when that is 0; calls that may overlap
-   need one each).  EINVAL for bad shapes or pointers, ECAP for a short
-   workspace. */
+   library's rule.  One launch on hip_stream, two where the workspace is not 0:
+   then workspace_dev holds at least flowkv_chunk_attention_workspace(...) bytes
+   for the same arguments, 4-byte aligned, owned by the caller and busy until
+   the stream passes the call (NULL when that is 0; calls that may overlap need
+   one each).  EINVAL for bad shapes or pointers, ECAP for a short workspace. */
 int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, const void* q_dev,
                            int64_t q_stride, int32_t n_tokens, int32_t n_req, int32_t q_heads,
                            int32_t kv_heads, int32_t head_dim, const int32_t* offsets_dev,
@@ -503,9 +502,12 @@ int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, const void* q
                            float scale, int32_t split_tokens, void* out_dev, void* workspace_dev,
                            int64_t workspace_bytes, void* hip_stream);
 
-/* Workspace bytes of flowkv_chunk_attention for these arguments: 0 where one
-   split covers max_seq_len, else n_tokens x q_heads x ceil(max_seq_len /
-   split_tokens) x (head_dim + 2) floats. */
+/* Workspace bytes of flowkv_chunk_attention for these arguments.  With
+   split_tokens 0 where it covers max_seq_len, else n_tokens x q_heads x
+   ceil(max_seq_len / split_tokens) x (head_dim + 2) floats; with 0, the
+   library's rule, no more than 34 MB where requests bring many tokens (0 for
+   the most part), and as above, of at most 2,048 tokens a split, where they
+   bring few. */
 int flowkv_chunk_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q_heads,
                                      int32_t kv_heads, int32_t head_dim, int32_t max_new,
                                      int32_t max_seq_len, int32_t split_tokens, int64_t* bytes);

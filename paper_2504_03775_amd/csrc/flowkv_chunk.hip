@@ -57,6 +57,7 @@ struct ChunkArgs {
   int32_t n_tokens, n_req, q_heads, kv_heads, group;
   int32_t rows;                         // query rows of a workgroup's tile
   int32_t tiles, split_tokens, splits;
+  int32_t pieces;                       // work by the lengths: of all tiles; 0: whole tiles
   float scale_log2;                     // scale * log2(e)
 };
 
@@ -335,7 +336,160 @@ struct Source {
   }
 };
 
+// ---- work by the lengths ------------------------------------------------------------
+//
+// The host sees only the longest request.  Two kinds of call have every workgroup look at
+// all lengths first (about 2 us), and find what it does from them by itself:
+//   - fewer tiles than CUs, but long ones: a tile's steps are cut into pieces, one to a
+//     workgroup, no longer than need be for all tiles' to be a CU's each.  (With one length
+//     of split for contexts of 500 to 9,000 tokens, or under the causal diagonal, some CUs
+//     have nothing while others go round twice.)  Tiles in more than one piece are joined
+//     from their records by a second kernel.  Chunks of 100 to 700 tokens beside 20 single
+//     ones over up to 8,000 cached, 8 heads of 128 on one KV head: 69 us, by even splits 84;
+//     512 tokens behind 8,000, 32 heads on 8: 87 and 94; 4,000 behind none, 8 on 1: 61 and
+//     72.  With few steps the even splits are faster: 256 behind 4,000, 32 on 8: 38 and 42.
+//   - more tiles than CUs, of requests with much in the cache: whole tiles, the longest
+//     first, so that the last ones to end are short.  4 chunks of 100 to 600 tokens beside 36
+//     single ones over 100 to 6,600, 32 heads on 8: 255 us, in the requests' order 339.
+//     (Prompts with nothing cached gain nothing: the diagonal orders each of them.)
+constexpr int kPieceTiles = 512;           // most tile slots, and requests, of such a call
+constexpr int kPieces = 256;               // MI355X's CUs
+constexpr int kPieceLeast = 2;             // steps
+constexpr int kCutSteps = 16;              // steps a CU, were all tiles the longest, from which on
+
+struct Cut {
+  int32_t start[kPieceTiles];              // a request's first tile slot
+  union {                                  // of a tile slot
+    alignas(16) float steps[kPieceTiles];
+    alignas(16) uint32_t key[kPieceTiles];
+  };
+  // pieces before a tile slot's, of one KV head; or the tile slots (-1: none), longest first
+  int32_t first[kPieceTiles + 1];
+  int32_t part[2][8];
+  int32_t length;
+};
+
+// Pieces of a tile (steps >= 0, whole), by the reciprocal of their length: at the exact
+// multiples it may give one more, the same one wherever it is asked.
+__device__ __forceinline__ float pieces_of(float steps, float inv) {
+  return ceilf(steps * inv);
+}
+
+// Fills c; kPieceTiles lanes.
 template <class F>
+__device__ __forceinline__ void cut_tiles(const ChunkArgs& a, Cut& c) {
+  static_assert(F::kThreads == kPieceTiles);
+  const int tid = threadIdx.x, ln = tid & 63, wave = tid >> 6;
+  // (at most kPieceTiles x kRows rows: 32 bits hold what valid offsets give)
+  if (tid < a.n_req)
+    c.start[tid] = int32_t(uint32_t(a.offsets[tid]) * uint32_t(a.group) / F::kRows) + tid;
+  if (tid == 0) c.length = INT32_MAX;
+  __syncthreads();
+  int32_t n = 0;
+  if (tid < a.tiles) {
+    int32_t r = 0, hi = a.n_req;
+    while (hi - r > 1) {
+      const int32_t mid = r + (hi - r) / 2;
+      if (c.start[mid] <= tid) r = mid;
+      else hi = mid;
+    }
+    const Request rq = request_at(a, r);
+    const int32_t rows = rq.n_new * a.group, row0 = (tid - c.start[r]) * F::kRows;
+    if (row0 >= 0 && row0 < rows) {
+      const int32_t end = row0 + F::kRows < rows ? row0 + F::kRows : rows;
+      const int32_t limit = seen(rq, int32_t(uint32_t(end - 1) / uint32_t(a.group)));
+      n = limit > F::kStep ? (limit + F::kStep - 1) / F::kStep : 1;
+    }
+  }
+  if (a.pieces == 0) {                           // each counts the longer ones
+    const uint32_t key = uint32_t(n) * kPieceTiles + uint32_t(tid);
+    c.key[tid] = key;
+    __syncthreads();
+    if (tid < a.tiles) {
+      int32_t before = 0;
+#pragma unroll 4
+      for (int32_t i = 0; i < a.tiles; i += 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(&c.key[i]);
+        before += x[0] > key;
+        before += x[1] > key;
+        before += x[2] > key;
+        before += x[3] > key;
+      }
+      c.first[before] = n > 0 ? tid : -1;
+    }
+    __syncthreads();
+    return;
+  }
+  c.steps[tid] = float(n);
+  int32_t sum = n, most = n;
+#pragma unroll
+  for (int off = 1; off < 64; off *= 2) {
+    sum += __shfl_xor(sum, off);
+    most = std::max(most, __shfl_xor(most, off));
+  }
+  if (ln == 0) {
+    c.part[0][wave] = sum;
+    c.part[1][wave] = most;
+  }
+  __syncthreads();
+  sum = most = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    sum += c.part[0][w];
+    most = std::max(most, c.part[1][w]);
+  }
+  // a lane tries a length: the least one that leaves few enough pieces
+  const int32_t each = std::max(a.pieces / a.kv_heads, 1);
+  const int32_t least = std::max((sum + each - 1) / each, kPieceLeast);
+  const int32_t by = most > least ? (most - least + F::kThreads - 1) / F::kThreads : 1;
+  const int32_t mine = least + tid * by;
+  if (mine - by < most) {
+    const float inv = mine >= most ? 0.f : 1.f / float(mine);
+    float pieces = 0.f;
+#pragma unroll 4
+    for (int32_t i = 0; i < a.tiles; i += 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(&c.steps[i]);
+      pieces += (pieces_of(x[0], inv) + pieces_of(x[1], inv)) +
+                (pieces_of(x[2], inv) + pieces_of(x[3], inv));
+    }
+    if (pieces <= float(each)) atomicMin(&c.length, mine);
+  }
+  __syncthreads();
+  const int32_t length = c.length;
+  const int32_t pieces =
+      n == 0 ? 0 : length >= most ? 1 : int32_t(pieces_of(float(n), 1.f / float(length)));
+  sum = pieces;
+#pragma unroll
+  for (int off = 1; off < 64; off *= 2) {
+    const int32_t y = __shfl_up(sum, off);
+    if (ln >= off) sum += y;
+  }
+  if (ln == 63) c.part[0][wave] = sum;
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) sum += c.part[0][w];
+  c.first[tid + 1] = sum;
+  if (tid == 0) c.first[0] = 0;
+  __syncthreads();
+}
+
+// The workspace of a call in pieces: a record a piece, its rows as the waves hold them:
+// register 4 j + i of lane l of dim block b at (j * 64 + l) * 4 + i; then the rows' (reference, sum); then
+// Cut::first.
+template <class F>
+__device__ __forceinline__ float* piece_sums(const ChunkArgs& a, int64_t rec, int rw, int b) {
+  return a.ws + ((rec * F::kRw + rw) * (F::kDh / 32) + b) * 1024;
+}
+template <class F>
+__device__ __forceinline__ f32x2u* piece_ml(const ChunkArgs& a, int64_t rec, int rw) {
+  return reinterpret_cast<f32x2u*>(a.ws + int64_t(kPieces) * F::kRows * F::kDh) +
+         (rec * F::kRw + rw) * 32;
+}
+template <class F>
+__device__ __forceinline__ int32_t* piece_first(const ChunkArgs& a) {
+  return reinterpret_cast<int32_t*>(a.ws + int64_t(kPieces) * F::kRows * (F::kDh + 2));
+}
+
+template <class F, bool kCut>
 __global__ __launch_bounds__(F::kThreads, 2)
 void chunk_attn(const ChunkArgs a) {
   typedef Wave<F> W;
@@ -345,25 +499,55 @@ void chunk_attn(const ChunkArgs a) {
   const int rw = wave % F::kRw, kw = wave / F::kRw;
   const int half = ln >> 5, c32 = ln & 31;
 
-  const uint32_t id = blockIdx.x;
-  const int g = int(id % uint32_t(a.kv_heads));
-  const uint32_t rest = id / uint32_t(a.kv_heads);
-  const int split = int(rest / uint32_t(a.tiles));
-  const int slot = a.tiles - 1 - int(rest % uint32_t(a.tiles));  // the longest first
-  const int32_t r =
-      flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); });
+  int g, slot;
+  int32_t r, split = 0, record = 0, pieces = 1;
+  int64_t local;
+  if constexpr (kCut) {
+    __shared__ Cut cut;
+    cut_tiles<F>(a, cut);
+    if (a.pieces == 0) {
+      g = int(blockIdx.x % uint32_t(a.kv_heads));
+      slot = cut.first[blockIdx.x / uint32_t(a.kv_heads)];
+      if (slot < 0) return;
+    } else {
+      const int32_t total = cut.first[a.tiles];
+      // an XCD's workgroups have pieces in a row
+      const int32_t x = int32_t(blockIdx.x) % 8, n8 = int32_t(gridDim.x) / 8;
+      record = x * n8 + std::min(x, int32_t(gridDim.x) % 8) + int32_t(blockIdx.x) / 8;
+      if (record == 0)
+        for (int32_t i = tid; i <= a.tiles; i += F::kThreads) piece_first<F>(a)[i] = cut.first[i];
+      if (record >= total * a.kv_heads) return;
+      g = record / total;
+      const int32_t at = record - g * total;
+      slot = flowkv::last_at_most(a.tiles, at, [&](int32_t i) { return cut.first[i]; });
+      split = at - cut.first[slot];
+      pieces = cut.first[slot + 1] - cut.first[slot];
+    }
+    r = flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return cut.start[i]; });
+    local = int64_t(slot) - cut.start[r];
+  } else {
+    const uint32_t id = blockIdx.x;
+    g = int(id % uint32_t(a.kv_heads));
+    const uint32_t rest = id / uint32_t(a.kv_heads);
+    split = int(rest / uint32_t(a.tiles));
+    slot = a.tiles - 1 - int(rest % uint32_t(a.tiles));  // the longest first
+    r = flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); });
+    local = int64_t(slot) - first_tile(a, r);
+  }
   const Request rq = request_at(a, r);
-  const int64_t local = int64_t(slot) - first_tile(a, r);
   const int64_t rows = int64_t(rq.n_new) * a.group;
   const int64_t row0 = local * F::kRows;
   if (local < 0 || row0 >= rows) return;
   const int64_t row_end = row0 + F::kRows < rows ? row0 + F::kRows : rows;
   const int32_t tile_limit = seen(rq, int32_t((row_end - 1) / a.group));
   const int32_t tile_least = seen(rq, int32_t(row0 / a.group));
-  const int32_t s0 = split * a.split_tokens;
-  if (split > 0 && s0 >= tile_limit) return;     // (split 0 writes the rows that see nothing)
-  const int32_t s1 = tile_limit - s0 > a.split_tokens ? s0 + a.split_tokens : tile_limit;
-  const bool direct = tile_limit <= a.split_tokens;
+  int32_t length = a.split_tokens;
+  if constexpr (kCut)                            // (a piece's, of as many even ones)
+    length = (tile_limit + pieces * F::kStep - 1) / (pieces * F::kStep) * F::kStep;
+  const int32_t s0 = split * length;
+  if (!kCut && split > 0 && s0 >= tile_limit) return;   // (split 0 writes what sees nothing)
+  const int32_t s1 = tile_limit - s0 > length ? s0 + length : tile_limit;
+  const bool direct = kCut ? pieces == 1 : tile_limit <= length;
 
   // this lane's query row, as a column of S^T
   const int64_t wrow = row0 + rw * 32, row = wrow + c32;
@@ -538,6 +722,15 @@ void chunk_attn(const ChunkArgs a) {
         }
     }
   }
+  if (kCut && !direct && any_row) {
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4u*>(piece_sums<F>(a, record, rw, b) + (j * 64 + ln) * 4) =
+            f32x4u{w.o[b][4 * j], w.o[b][4 * j + 1], w.o[b][4 * j + 2], w.o[b][4 * j + 3]};
+    if (half == 0) piece_ml<F>(a, record, rw)[c32] = f32x2u{mref, lsum};
+  }
   if (!live) return;
   const int64_t orow = token * a.q_heads + head;
   if (direct) {
@@ -550,7 +743,7 @@ void chunk_attn(const ChunkArgs a) {
                          pack_bf16(w.o[b][i + 2] * inv, w.o[b][i + 3] * inv)};
         *reinterpret_cast<u32x2*>(a.out + orow * kDh + 32 * b + 2 * i + 4 * half) = x;
       }
-  } else {
+  } else if constexpr (!kCut) {
     const int64_t rec = record_at(a, orow, split);
 #pragma unroll
     for (int b = 0; b < kB; ++b)
@@ -559,6 +752,62 @@ void chunk_attn(const ChunkArgs a) {
         *reinterpret_cast<f32x4u*>(record_sums(a, kDh, rec) + 32 * b + 2 * i + 4 * half) =
             f32x4u{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
     if (half == 0) *record_ml(a, kDh, rec) = f32x2u{mref, lsum};
+  }
+}
+
+// Joins the records of the tiles that are in more than one piece: a wave per 32 rows and
+// 32 dims.
+template <class F>
+__global__ __launch_bounds__(2 * F::kDh) void chunk_attn_join(const ChunkArgs a) {
+  const int ln = threadIdx.x & 63, half = ln >> 5, c32 = ln & 31;
+  const int b = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rw = int(blockIdx.x % F::kRw);
+  const uint32_t rest = blockIdx.x / F::kRw;
+  const int g = int(rest % uint32_t(a.kv_heads)), slot = int(rest / uint32_t(a.kv_heads));
+  const int32_t* first = piece_first<F>(a);
+  const int32_t total = first[a.tiles], from = first[slot], to = first[slot + 1];
+  if (to - from < 2) return;                     // written already
+  const int32_t r =
+      flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); });
+  const Request rq = request_at(a, r);
+  const int64_t row = (int64_t(slot) - first_tile(a, r)) * F::kRows + rw * 32 + c32;
+  const bool live = row >= 0 && row < int64_t(rq.n_new) * a.group;
+  if (!__any(live)) return;
+  float m = -INFINITY, l = 0.f;
+  f32x4 x[4] = {};
+  constexpr int kAhead = 4;                      // records under way
+  for (int32_t w = from; w < to; w += kAhead) {
+    f32x2u ml[kAhead];
+    f32x4 y[kAhead][4];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {           // (past the end: the last record, not used)
+      const int64_t rec = int64_t(g) * total + std::min(w + k, to - 1);
+      ml[k] = piece_ml<F>(a, rec, rw)[c32];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        y[k][j] =
+            *reinterpret_cast<const f32x4u*>(piece_sums<F>(a, rec, rw, b) + (j * 64 + ln) * 4);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (w + k >= to) break;
+      const float mm = fmaxf(m, ml[k][0]);
+      const float c1 = part_weight(m, l, mm), c2 = part_weight(ml[k][0], ml[k][1], mm);
+      m = mm;
+      l = l * c1 + ml[k][1] * c2;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = x[j] * c1 + y[k][j] * c2;
+    }
+  }
+  if (!live) return;
+  const int64_t qi = row / a.group;
+  const int64_t orow = (int64_t(rq.begin) + qi) * a.q_heads + g * a.group + (row - qi * a.group);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const u32x2 y = {pack_bf16(x[j][0] * inv, x[j][1] * inv),
+                     pack_bf16(x[j][2] * inv, x[j][3] * inv)};
+    *reinterpret_cast<u32x2*>(a.out + orow * F::kDh + 32 * b + 8 * j + 4 * half) = y;
   }
 }
 
@@ -704,13 +953,15 @@ void chunk_attn_few(const ChunkArgs a) {
 #pragma unroll
     for (int e = 0; e < kKL; ++e) {
       const int x = kt + e * kStride;            // token of the tile
-      kw[e] = __builtin_nontemporal_load((cgvec4*)(kbase + uint64_t(lds.at[tile * kFewTile + (x & 3) * 8 + (x >> 2)]) * 128));
+      kw[e] = __builtin_nontemporal_load(
+          (cgvec4*)(kbase + uint64_t(lds.at[tile * kFewTile + (x & 3) * 8 + (x >> 2)]) * 128));
     }
   };
   auto load_v = [&](int tile) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      vw[e] = __builtin_nontemporal_load((cgv*)(vbase + uint64_t(lds.at[tile * kFewTile + 8 * q4 + e]) * 128));
+      vw[e] = __builtin_nontemporal_load(
+          (cgv*)(vbase + uint64_t(lds.at[tile * kFewTile + 8 * q4 + e]) * 128));
   };
   if (wave < n_tiles) {
     load_k(wave);
@@ -972,29 +1223,50 @@ typedef void (*ChunkFn)(ChunkArgs);
 struct Kind {
   int rows, threads, step;
   ChunkFn fn[2];                                 // head_dim 64, 128
+  ChunkFn cut[2], join[2];                       // work by the lengths
 };
 template <class F64, class F128>
-constexpr Kind kind_of() {
+constexpr Kind kind_of(ChunkFn join64, ChunkFn join128) {
   static_assert(F64::kRows == F128::kRows && F64::kThreads == F128::kThreads &&
                 F64::kStep == F128::kStep);
-  return Kind{F64::kRows, F64::kThreads, F64::kStep, {chunk_attn<F64>, chunk_attn<F128>}};
+  return Kind{F64::kRows,
+              F64::kThreads,
+              F64::kStep,
+              {chunk_attn<F64, false>, chunk_attn<F128, false>},
+              {chunk_attn<F64, true>, chunk_attn<F128, true>},
+              {join64, join128}};
 }
 const Kind kKinds[] = {
-    {16, kFewThreads, kFewTile, {chunk_attn_few<64, 1>, chunk_attn_few<128, 1>}},
-    {32, kFewThreads, kFewTile, {chunk_attn_few<64, 2>, chunk_attn_few<128, 2>}},
-    kind_of<Form<64, 4, 2>, Form<128, 4, 2>>(),
-    kind_of<Form<64, 8, 1>, Form<128, 8, 1>>(),
+    {16, kFewThreads, kFewTile, {chunk_attn_few<64, 1>, chunk_attn_few<128, 1>}, {}, {}},
+    {32, kFewThreads, kFewTile, {chunk_attn_few<64, 2>, chunk_attn_few<128, 2>}, {}, {}},
+    kind_of<Form<64, 4, 2>, Form<128, 4, 2>>(chunk_attn_join<Form<64, 4, 2>>, nullptr),
+    kind_of<Form<64, 8, 1>, Form<128, 8, 1>>(nullptr, chunk_attn_join<Form<128, 8, 1>>),
 };
 constexpr int kSplitUnit = 64;
 
+// Tile slots of a call, see first_tile.
+int64_t tile_slots(int64_t n_tokens, int64_t n_req, int group, int rows) {
+  return n_tokens * group / rows + n_req;
+}
+
 // Tiles of `rows` rows that the batch has at most.
 int64_t tiles_of(int64_t n_tokens, int64_t n_req, int group, int64_t max_new, int rows) {
-  return std::min(n_req * ((max_new * group + rows - 1) / rows), n_tokens * group / rows + n_req);
+  return std::min(n_req * ((max_new * group + rows - 1) / rows),
+                  tile_slots(n_tokens, n_req, group, rows));
+}
+
+// Whether the kernels that look at all lengths take a call: their tables' sizes, and
+// steps x kPieceTiles within 32 bits.
+bool by_lengths(int64_t n_tokens, int64_t n_req, int group, int64_t max_seq_len, const Kind& kind) {
+  const int64_t slots = tile_slots(n_tokens, n_req, group, kind.rows);
+  return slots <= kPieceTiles && n_req <= kPieceTiles &&
+         slots * ((max_seq_len + kind.step - 1) / kind.step) < 1 << 22;
 }
 
 struct Shape {
   int kind;
   int32_t split, splits;
+  bool cut, order;                               // pieces by the lengths; tiles, the longest first
   int64_t need;
 };
 
@@ -1015,13 +1287,41 @@ int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_head
     return fail(FLOWKV_EINVAL, "split_tokens %d: need 0 or a multiple of %d", split_tokens,
                 kSplitUnit);
   const int group = q_heads / kv_heads;
-  out->kind = 3;
-  if (int64_t(max_new) * group <= 32 && split_tokens <= kFewSplit)
+  // A step of 256 rows x 64 tokens moves half as much as one of 128 x 128, and the smaller
+  // tiles share out better where there are few.
+  const int64_t t256 = tiles_of(n_tokens, n_req, group, max_new, 256) * kv_heads;
+  const int64_t t128 = tiles_of(n_tokens, n_req, group, max_new, 128) * kv_heads;
+  const bool rule = split_tokens == 0;
+  out->cut = out->order = false;
+  if (int64_t(max_new) * group <= 32 && split_tokens <= kFewSplit) {
     out->kind = int64_t(max_new) * group > 16;
-  else if (tiles_of(n_tokens, n_req, group, max_new, kKinds[3].rows) * kv_heads < kCus) out->kind = 2;
+  } else if (t256 >= kCus) {
+    out->kind = 3;
+  } else {
+    const int kind = head_dim == 128 ? 3 : 2;
+    const int64_t tiles = kind == 3 ? t256 : t128, step = kKinds[kind].step;
+    out->cut = rule && tiles < kCus &&
+               by_lengths(n_tokens, n_req, group, max_seq_len, kKinds[kind]) &&
+               tiles * ((max_seq_len + step - 1) / step) >= kCutSteps * kCus;
+    out->kind = out->cut ? kind : 2;
+  }
+  const Kind& kind = kKinds[out->kind];
+  if (rule && out->kind >= 2 && !out->cut)
+    out->order = n_req > 1 && max_seq_len / 2 >= max_new && (out->kind == 3 ? t256 : t128) > kCus &&
+                 by_lengths(n_tokens, n_req, group, max_seq_len, kind);
+  if (out->cut || out->order) {
+    out->split = 0;
+    out->splits = 1;
+    out->need = 0;
+    if (out->cut)
+      out->need = (int64_t(kPieces) * kind.rows * (head_dim + 2) +
+                   tile_slots(n_tokens, n_req, group, kind.rows) + 1) *
+                  int64_t(sizeof(float));
+    return FLOWKV_OK;
+  }
   const int64_t tiles =
-      std::max<int64_t>(tiles_of(n_tokens, n_req, group, max_new, kKinds[out->kind].rows) * kv_heads, 1);
-  if (split_tokens == 0) {
+      std::max<int64_t>(tiles_of(n_tokens, n_req, group, max_new, kind.rows) * kv_heads, 1);
+  if (rule) {
     const int64_t aim = out->kind <= 1 ? 4 * kCus : kCus, want = (aim + tiles - 1) / tiles;
     int64_t s = (int64_t(max_seq_len) + want - 1) / want;
     s = std::max<int64_t>((s + 127) / 128 * 128, 256);
@@ -1145,20 +1445,28 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   a.scale_log2 = scale * kLog2e;
   const Kind& kind = kKinds[sh.kind];
   a.rows = kind.rows;
-  const int64_t tiles = int64_t(n_tokens) * a.group / kind.rows + n_req;
+  const int64_t tiles = tile_slots(n_tokens, n_req, a.group, kind.rows);
   const int64_t grid = tiles * kv_heads;
   // a wave per (new token, query head) where its lane groups hold all records at once
   const bool one = sh.splits <= kMergeChunk * 64 * 4 / head_dim;
   const int64_t out_rows = int64_t(n_tokens) * q_heads, merge = one ? (out_rows + 3) / 4 : out_rows;
-  if (grid > INT32_MAX / sh.splits || merge > INT32_MAX)
+  // lanes of a launch in 32 bits
+  if (grid > UINT32_MAX / kind.threads / sh.splits || merge > UINT32_MAX / kMergeThreads)
     return fail(FLOWKV_EINVAL, "%lld tiles of queries x %d splits: too many for one call",
                 (long long)grid, sh.splits);
   a.tiles = int32_t(tiles);
+  a.pieces = sh.cut ? kPieces : 0;
   void* args[] = {&a};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(kind.fn[head_dim == 128]),
-                                 dim3(unsigned(grid * sh.splits)), dim3(unsigned(kind.threads)), args,
-                                 0, st);
+  const int d128 = head_dim == 128;
+  const int64_t groups = sh.cut ? std::max<int64_t>(grid, kPieces) : grid * sh.splits;
+  hipError_t e = hipLaunchKernel(
+      reinterpret_cast<const void*>(sh.cut || sh.order ? kind.cut[d128] : kind.fn[d128]),
+      dim3(unsigned(groups)), dim3(unsigned(kind.threads)), args, 0, st);
+  if (e == hipSuccess && sh.cut)
+    e = hipLaunchKernel(reinterpret_cast<const void*>(kind.join[d128]),
+                        dim3(unsigned(grid * (kind.rows / 32))), dim3(unsigned(2 * head_dim)), args,
+                        0, st);
   if (e == hipSuccess && sh.splits > 1) {
     ChunkFn fn = head_dim == 64 ? (one ? chunk_attn_merge<64, 1> : chunk_attn_merge<64, 4>)
                                 : (one ? chunk_attn_merge<128, 1> : chunk_attn_merge<128, 4>);

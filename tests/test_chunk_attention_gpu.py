@@ -320,6 +320,123 @@ def test_replayed_graph_follows_the_lengths_on_the_device():
         assert torch.isnan(out[int(b.off[-1]):].float()).all()
 
 
+LONGEST = 400_000       # a length that the caller has to allow for, whatever the batch holds
+
+
+def pieces_bytes(b, hk, G, d):
+    """Workspace of a call whose tiles are cut by the lengths on the device."""
+    rows = 256 if d == 128 else 128
+    return (256 * rows * (d + 2) + b.n_tokens * G // rows + len(b.new) + 1) * 4
+
+
+MIXED = [  # as BATCHES, with more than 32 rows of a request in every shape
+    ([200], [200]), ([31, 64, 1], [31, 500, 129]), ([128, 127, 129], [128, 400, 129]),
+    ([1, 260, 1, 70], [1000, 260, 63, 900]), ([0, 3, 0, 40, 0, 0], [9, 40, 0, 40, 700, 0]),
+    ([700], [1400]), ([40] * 12, [40 + 150 * i for i in range(12)]), ([50], [9000]),
+    ([1] * 30 + [90], [333 * i + 1 for i in range(30)] + [300]),
+]
+
+
+@pytest.mark.parametrize("batch", range(len(MIXED)))
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_pieces_by_the_lengths_against_the_formula(shape, batch):
+    L, hk, d, bs, G = SHAPES[shape]
+    seed = 29 * shape + batch
+    layout = (BM, LM)[seed % 2]
+    b = Batch(Geometry(f"pieces{shape}", L, hk, d, bs, "bfloat16"), layout, *MIXED[batch], seed,
+              pad=(seed % 3, seed % 4))
+    say(f"pieces {NAMES[layout]} shape {SHAPES[shape]} new {b.new.tolist()} of {b.total.tolist()}")
+    need = fk.flowkv_chunk_attention_workspace(b.n_tokens, len(b.new), hk * G, hk, d, b.max_new,
+                                               LONGEST)
+    rows = 256 if d == 128 else 128
+    tiles = hk * min(len(b.new) * -(-b.max_new * G // rows), b.n_tokens * G // rows + len(b.new))
+    assert need == (pieces_bytes(b, hk, G, d) if tiles < 256 else 0)    # (whole tiles from there)
+    q = queries(b, hk * G, seed, lead=(0, 8, 2 * d)[seed % 3])
+    out = attend(b, L - 1, q, d ** -0.5, max_len=LONGEST)
+    rel, worst = check_attention(b, L - 1, q, d ** -0.5, out, max_seq=LONGEST)
+    say(f"  relative error {rel:.2e}, worst error / bound {worst:.2f}")
+    inside = torch.zeros(b.n_tokens, dtype=torch.bool, device="cuda")
+    inside[int(b.off[0]):int(b.off[-1])] = True
+    assert (out[~inside] == 7).all(), "a row of no request was written"
+
+
+@pytest.mark.parametrize("hk,d,G,n_req,top", [(4, 64, 2, 130, 40), (8, 64, 2, 20, 120),
+                                              (8, 128, 4, 20, 64), (2, 128, 8, 150, 30),
+                                              (8, 128, 4, 60, 100), (1, 64, 5, 400, 17)])
+@pytest.mark.parametrize("layout", [BM, LM], ids=lambda x: NAMES[x])
+def test_tiles_in_the_order_of_the_lengths(layout, hk, d, G, n_req, top):
+    """More tiles than CUs, of requests of every length, some with no token."""
+    g = np.random.default_rng(n_req + d)
+    new = g.integers(0, top + 1, n_req)
+    new[n_req // 2] = top
+    b = Batch(Geometry("order", 1, hk, d, 16, "bfloat16"), layout, new,
+              new + g.integers(0, 600, n_req), 23)
+    say(f"order {NAMES[layout]} {n_req} requests of up to {top}, {hk} x {d}, group {G}")
+    q = queries(b, hk * G, 23)
+    out = attend(b, 0, q, d ** -0.5)
+    check_attention(b, 0, q, d ** -0.5, out)
+    assert torch.equal(attend(b, 0, q, d ** -0.5, split=1 << 20), out)     # one piece a tile too
+
+
+@pytest.mark.parametrize("rule", [
+    lambda: [test_rows_that_see_nothing_are_zero(d, 0) for d in (64, 128)],
+    lambda: [test_blocks_outside_the_pool_contribute_nothing(0)],
+    lambda: [test_odd_values_reach_only_the_rows_that_see_them(d, 0, bad)
+             for d in (64, 128) for bad in (float("nan"), float("inf"), float("-inf"))],
+    lambda: [test_odd_values_beside_missing_blocks_reach_every_row(d, 60) for d in (64, 128)],
+    lambda: [test_infinite_scores(0)],
+    lambda: [test_large_scores_and_rising_maxima(0)],
+], ids=["nothing", "missing", "odd", "odd-missing", "infinite", "large"])
+def test_pieces_keep_the_rules(rule, monkeypatch):
+    plain = attend
+    monkeypatch.setitem(globals(), "attend",
+                        lambda b, layer, q, scale, split=0, out=None, max_len=None, stream=None:
+                        plain(b, layer, q, scale, 0, out, LONGEST, stream))
+    rule()
+
+
+def test_pieces_in_a_replayed_graph_and_on_two_streams():
+    """One capture, other lengths in the same memory; two calls at once, a workspace each."""
+    geom = Geometry("piecesgraph", 2, 2, 128, 16, "bfloat16")
+    b = Batch(geom, LM, [40, 1, 9], [900, 500, 9], 17)
+    q = queries(b, 8, 17)
+    out = [torch.zeros(q.shape, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    need = fk.flowkv_chunk_attention_workspace(50, 3, 8, 2, 128, 50, LONGEST)
+    assert need == pieces_bytes(b, 2, 4, 128)
+    ws = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2)]
+
+    def call(l=1, stream=None):
+        fk.flowkv_chunk_attention(b.pool, l, q, b.offsets, b.tables, b.lens, 50, LONGEST, 0.1,
+                                  out[l], ws[l], stream=stream)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for new, total in (([40, 1, 9], [900, 500, 9]), ([0, 30, 20], [900, 60, 20]),
+                       ([1, 1, 1], [2, 512, 9]), ([10, 10, 30], [900, 512, 30])):
+        b.new, b.total = np.asarray(new), np.asarray(total)
+        b.off = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
+        b.offsets.copy_(torch.as_tensor(b.off))
+        b.lens.copy_(torch.as_tensor(b.total.astype(np.int32)))
+        for l in range(2):
+            out[l].fill_(float("nan"))
+            ws[l].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_attention(b, 1, q, 0.1, out[1], max_seq=LONGEST)
+        assert torch.isnan(out[1][int(b.off[-1]):].float()).all()
+        once = out[1].clone()
+        for _ in range(5):
+            for l in range(2):
+                call(l, streams[l])
+        torch.cuda.synchronize()
+        check_attention(b, 0, q, 0.1, out[0], max_seq=LONGEST)
+        assert torch.equal(out[1][:int(b.off[-1])], once[:int(b.off[-1])])
+
+
 def test_refused_by_the_binding():
     geom = Geometry("chunkref", 2, 2, 64, 16, "bfloat16")
     b = Batch(geom, BM, [4, 3], [40, 30], 18)
