@@ -52,22 +52,28 @@ struct ChunkArgs {
   uint16_t* out;                        // (n_tokens, Hq, Dh) bf16
   float* ws;                            // the splits' records
   uint32_t bunits, sunits;              // 128-byte units between blocks, slots
-  uint32_t bs_magic, bs_shift;          // division by block_size
+  uint32_t bs_magic, bs_shift;          // division by block_size,
+  uint32_t g_magic, g_shift;            // and by the group
   int32_t pool_blocks, block_size, max_blocks, max_seq_len;
   int32_t n_tokens, n_req, q_heads, kv_heads, group;
-  int32_t rows;                         // query rows of a workgroup's tile
+  int32_t row_shift;                    // query rows of a workgroup's tile: 2^row_shift
   int32_t tiles, split_tokens, splits;
   int32_t pieces;                       // work by the lengths: of all tiles; 0: whole tiles
   float scale_log2;                     // scale * log2(e)
 };
 
 // The rows of a request are its (new token, query head of the group) pairs,
-// token by token; a tile is a.rows of them.  Tile slot x of the batch: request r
+// token by token; a tile is 2^row_shift of them.  Tile slot x of the batch: request r
 // has the slots from floor(offsets[r] * G / rows) + r, which are enough for its
 // rows whatever the offsets are, and at most n_tokens * G / rows + n_req in all:
 // the grid needs no lengths on the host.
 __device__ __forceinline__ int64_t first_tile(const ChunkArgs& a, int32_t r) {
-  return int64_t(a.offsets[r]) * a.group / a.rows + r;
+  return (int64_t(a.offsets[r]) * a.group >> a.row_shift) + r;
+}
+
+// The token of a request's row x (0 <= x < 2^31).
+__device__ __forceinline__ int32_t token_of(const ChunkArgs& a, int32_t x) {
+  return int32_t((__umulhi(uint32_t(x), a.g_magic) + uint32_t(x)) >> a.g_shift);
 }
 
 struct Request {
@@ -95,6 +101,8 @@ __device__ __forceinline__ int32_t seen(const Request& q, int32_t i) {
   const int32_t n = q.base + i + 1;
   return n < 0 ? 0 : n < q.limit ? n : q.limit;
 }
+
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // The workspace holds a record per (new token, query head, split): the weighted V
 // (Dh floats) of all records first, then all records' (reference max, sum).
@@ -339,7 +347,7 @@ struct Source {
 // ---- work by the lengths ------------------------------------------------------------
 //
 // The host sees only the longest request.  Two kinds of call have every workgroup look at
-// all lengths first (about 2 us), and find what it does from them by itself:
+// all lengths first (about 3 us), and find what it does from them by itself:
 //   - fewer tiles than CUs, but long ones: a tile's steps are cut into pieces, one to a
 //     workgroup, no longer than need be for all tiles' to be a CU's each.  (With one length
 //     of split for contexts of 500 to 9,000 tokens, or under the causal diagonal, some CUs
@@ -357,119 +365,26 @@ constexpr int kPieces = 256;               // MI355X's CUs
 constexpr int kPieceLeast = 2;             // steps
 constexpr int kCutSteps = 16;              // steps a CU, were all tiles the longest, from which on
 
+struct Mine {                              // what a workgroup does; pieces 0: nothing
+  Request rq;
+  int32_t row0, split, pieces;
+};
+
 struct Cut {
   int32_t start[kPieceTiles];              // a request's first tile slot
   union {                                  // of a tile slot
     alignas(16) float steps[kPieceTiles];
     alignas(16) uint32_t key[kPieceTiles];
   };
-  // pieces before a tile slot's, of one KV head; or the tile slots (-1: none), longest first
-  int32_t first[kPieceTiles + 1];
   int32_t part[2][8];
   int32_t length;
+  Mine mine;
 };
 
 // Pieces of a tile (steps >= 0, whole), by the reciprocal of their length: at the exact
 // multiples it may give one more, the same one wherever it is asked.
 __device__ __forceinline__ float pieces_of(float steps, float inv) {
   return ceilf(steps * inv);
-}
-
-// Fills c; kPieceTiles lanes.
-template <class F>
-__device__ __forceinline__ void cut_tiles(const ChunkArgs& a, Cut& c) {
-  static_assert(F::kThreads == kPieceTiles);
-  const int tid = threadIdx.x, ln = tid & 63, wave = tid >> 6;
-  // (at most kPieceTiles x kRows rows: 32 bits hold what valid offsets give)
-  if (tid < a.n_req)
-    c.start[tid] = int32_t(uint32_t(a.offsets[tid]) * uint32_t(a.group) / F::kRows) + tid;
-  if (tid == 0) c.length = INT32_MAX;
-  __syncthreads();
-  int32_t n = 0;
-  if (tid < a.tiles) {
-    int32_t r = 0, hi = a.n_req;
-    while (hi - r > 1) {
-      const int32_t mid = r + (hi - r) / 2;
-      if (c.start[mid] <= tid) r = mid;
-      else hi = mid;
-    }
-    const Request rq = request_at(a, r);
-    const int32_t rows = rq.n_new * a.group, row0 = (tid - c.start[r]) * F::kRows;
-    if (row0 >= 0 && row0 < rows) {
-      const int32_t end = row0 + F::kRows < rows ? row0 + F::kRows : rows;
-      const int32_t limit = seen(rq, int32_t(uint32_t(end - 1) / uint32_t(a.group)));
-      n = limit > F::kStep ? (limit + F::kStep - 1) / F::kStep : 1;
-    }
-  }
-  if (a.pieces == 0) {                           // each counts the longer ones
-    const uint32_t key = uint32_t(n) * kPieceTiles + uint32_t(tid);
-    c.key[tid] = key;
-    __syncthreads();
-    if (tid < a.tiles) {
-      int32_t before = 0;
-#pragma unroll 4
-      for (int32_t i = 0; i < a.tiles; i += 4) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(&c.key[i]);
-        before += x[0] > key;
-        before += x[1] > key;
-        before += x[2] > key;
-        before += x[3] > key;
-      }
-      c.first[before] = n > 0 ? tid : -1;
-    }
-    __syncthreads();
-    return;
-  }
-  c.steps[tid] = float(n);
-  int32_t sum = n, most = n;
-#pragma unroll
-  for (int off = 1; off < 64; off *= 2) {
-    sum += __shfl_xor(sum, off);
-    most = std::max(most, __shfl_xor(most, off));
-  }
-  if (ln == 0) {
-    c.part[0][wave] = sum;
-    c.part[1][wave] = most;
-  }
-  __syncthreads();
-  sum = most = 0;
-#pragma unroll
-  for (int w = 0; w < 8; ++w) {
-    sum += c.part[0][w];
-    most = std::max(most, c.part[1][w]);
-  }
-  // a lane tries a length: the least one that leaves few enough pieces
-  const int32_t each = std::max(a.pieces / a.kv_heads, 1);
-  const int32_t least = std::max((sum + each - 1) / each, kPieceLeast);
-  const int32_t by = most > least ? (most - least + F::kThreads - 1) / F::kThreads : 1;
-  const int32_t mine = least + tid * by;
-  if (mine - by < most) {
-    const float inv = mine >= most ? 0.f : 1.f / float(mine);
-    float pieces = 0.f;
-#pragma unroll 4
-    for (int32_t i = 0; i < a.tiles; i += 4) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(&c.steps[i]);
-      pieces += (pieces_of(x[0], inv) + pieces_of(x[1], inv)) +
-                (pieces_of(x[2], inv) + pieces_of(x[3], inv));
-    }
-    if (pieces <= float(each)) atomicMin(&c.length, mine);
-  }
-  __syncthreads();
-  const int32_t length = c.length;
-  const int32_t pieces =
-      n == 0 ? 0 : length >= most ? 1 : int32_t(pieces_of(float(n), 1.f / float(length)));
-  sum = pieces;
-#pragma unroll
-  for (int off = 1; off < 64; off *= 2) {
-    const int32_t y = __shfl_up(sum, off);
-    if (ln >= off) sum += y;
-  }
-  if (ln == 63) c.part[0][wave] = sum;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) sum += c.part[0][w];
-  c.first[tid + 1] = sum;
-  if (tid == 0) c.first[0] = 0;
-  __syncthreads();
 }
 
 // The workspace of a call in pieces: a record a piece, its rows as the waves hold them:
@@ -489,6 +404,134 @@ __device__ __forceinline__ int32_t* piece_first(const ChunkArgs& a) {
   return reinterpret_cast<int32_t*>(a.ws + int64_t(kPieces) * F::kRows * (F::kDh + 2));
 }
 
+// Finds the workgroup's tile, or its piece of one, and the KV head; kPieceTiles lanes, one
+// to a tile slot.  The first workgroup leaves the pieces before each slot in the workspace.
+template <class F>
+__device__ __forceinline__ Mine cut_tiles(const ChunkArgs& a, Cut& c, int& g, int32_t& record) {
+  static_assert(F::kThreads == kPieceTiles);
+  const int tid = threadIdx.x, ln = tid & 63, wave = tid >> 6;
+  // (at most kPieceTiles x kRows rows: 32 bits hold what valid offsets give)
+  if (tid < a.n_req)
+    c.start[tid] = int32_t(uint32_t(a.offsets[tid]) * uint32_t(a.group) / F::kRows) + tid;
+  if (tid == 0) {
+    c.length = INT32_MAX;
+    c.mine.pieces = 0;
+  }
+  __syncthreads();
+  int32_t n = 0;                                 // steps
+  Mine mine;
+  if (tid < a.tiles) {
+    int32_t r = 0, hi = a.n_req;
+    while (hi - r > 1) {
+      const int32_t mid = r + (hi - r) / 2;
+      if (c.start[mid] <= tid) r = mid;
+      else hi = mid;
+    }
+    mine.rq = request_at(a, r);
+    const int32_t rows = mine.rq.n_new * a.group;
+    mine.row0 = (tid - c.start[r]) * F::kRows;
+    if (mine.row0 >= 0 && mine.row0 < rows) {
+      const int32_t end = std::min(mine.row0 + F::kRows, rows);
+      const int32_t limit = seen(mine.rq, token_of(a, end - 1));
+      n = limit > F::kStep ? (limit + F::kStep - 1) / F::kStep : 1;
+    }
+  }
+  if (a.pieces == 0) {                           // each counts the longer ones
+    const uint32_t key = uint32_t(n) * kPieceTiles + uint32_t(tid);
+    c.key[tid] = key;
+    __syncthreads();
+    g = int(blockIdx.x % uint32_t(a.kv_heads));
+    if (n > 0) {
+      int32_t before = 0;
+#pragma unroll 4
+      for (int32_t i = 0; i < a.tiles; i += 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(&c.key[i]);
+        before += x[0] > key;
+        before += x[1] > key;
+        before += x[2] > key;
+        before += x[3] > key;
+      }
+      if (before == int32_t(blockIdx.x / uint32_t(a.kv_heads))) {
+        mine.split = 0;
+        mine.pieces = 1;
+        c.mine = mine;
+      }
+    }
+    __syncthreads();
+  } else {
+    c.steps[tid] = float(n);
+    int32_t sum = n, most = n;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      sum += __shfl_xor(sum, off);
+      most = std::max(most, __shfl_xor(most, off));
+    }
+    if (ln == 0) {
+      c.part[0][wave] = sum;
+      c.part[1][wave] = most;
+    }
+    __syncthreads();
+    sum = most = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      sum += c.part[0][w];
+      most = std::max(most, c.part[1][w]);
+    }
+    // a lane tries a length: the least one that leaves few enough pieces
+    constexpr int kTries = F::kThreads / 2;
+    const int32_t each = std::max(a.pieces / a.kv_heads, 1);
+    const int32_t least = std::max((sum + each - 1) / each, kPieceLeast);
+    const int32_t by = most > least ? (most - least + kTries - 1) / kTries : 1;
+    const int32_t tried = least + tid * by;
+    if (tid < kTries && tried - by < most) {
+      const float inv = tried >= most ? 0.f : 1.f / float(tried);
+      float pieces = 0.f;
+#pragma unroll 4
+      for (int32_t i = 0; i < a.tiles; i += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(&c.steps[i]);
+        pieces += (pieces_of(x[0], inv) + pieces_of(x[1], inv)) +
+                  (pieces_of(x[2], inv) + pieces_of(x[3], inv));
+      }
+      if (pieces <= float(each)) atomicMin(&c.length, tried);
+    }
+    __syncthreads();
+    const int32_t length = c.length;
+    mine.pieces =
+        n == 0 ? 0 : length >= most ? 1 : int32_t(pieces_of(float(n), 1.f / float(length)));
+    sum = mine.pieces;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      const int32_t y = __shfl_up(sum, off);
+      if (ln >= off) sum += y;
+    }
+    if (ln == 63) c.part[0][wave] = sum;
+    __syncthreads();
+    int32_t total = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      if (w < wave) sum += c.part[0][w];
+      total += c.part[0][w];
+    }
+    // an XCD's workgroups have pieces in a row
+    const int32_t x = int32_t(blockIdx.x) % 8, n8 = int32_t(gridDim.x) / 8;
+    record = x * n8 + std::min(x, int32_t(gridDim.x) % 8) + int32_t(blockIdx.x) / 8;
+    if (record == 0) {
+      if (tid == 0) piece_first<F>(a)[0] = 0;
+      if (tid < a.tiles) piece_first<F>(a)[tid + 1] = sum;
+    }
+    g = total ? record / total : 0;
+    mine.split = record - g * total - (sum - mine.pieces);
+    if (mine.split >= 0 && mine.split < mine.pieces && g < a.kv_heads) c.mine = mine;
+    __syncthreads();
+  }
+  mine.rq = {uniform(c.mine.rq.r), uniform(c.mine.rq.begin), uniform(c.mine.rq.n_new),
+             uniform(c.mine.rq.base), uniform(c.mine.rq.limit)};
+  mine.row0 = uniform(c.mine.row0);
+  mine.split = uniform(c.mine.split);
+  mine.pieces = uniform(c.mine.pieces);
+  return mine;
+}
+
 template <class F, bool kCut>
 __global__ __launch_bounds__(F::kThreads, 2)
 void chunk_attn(const ChunkArgs a) {
@@ -499,48 +542,32 @@ void chunk_attn(const ChunkArgs a) {
   const int rw = wave % F::kRw, kw = wave / F::kRw;
   const int half = ln >> 5, c32 = ln & 31;
 
-  int g, slot;
-  int32_t r, split = 0, record = 0, pieces = 1;
-  int64_t local;
+  int g;
+  int32_t row0, split, record = 0, pieces = 1;
+  Request rq;
   if constexpr (kCut) {
-    __shared__ Cut cut;
-    cut_tiles<F>(a, cut);
-    if (a.pieces == 0) {
-      g = int(blockIdx.x % uint32_t(a.kv_heads));
-      slot = cut.first[blockIdx.x / uint32_t(a.kv_heads)];
-      if (slot < 0) return;
-    } else {
-      const int32_t total = cut.first[a.tiles];
-      // an XCD's workgroups have pieces in a row
-      const int32_t x = int32_t(blockIdx.x) % 8, n8 = int32_t(gridDim.x) / 8;
-      record = x * n8 + std::min(x, int32_t(gridDim.x) % 8) + int32_t(blockIdx.x) / 8;
-      if (record == 0)
-        for (int32_t i = tid; i <= a.tiles; i += F::kThreads) piece_first<F>(a)[i] = cut.first[i];
-      if (record >= total * a.kv_heads) return;
-      g = record / total;
-      const int32_t at = record - g * total;
-      slot = flowkv::last_at_most(a.tiles, at, [&](int32_t i) { return cut.first[i]; });
-      split = at - cut.first[slot];
-      pieces = cut.first[slot + 1] - cut.first[slot];
-    }
-    r = flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return cut.start[i]; });
-    local = int64_t(slot) - cut.start[r];
+    __shared__ Cut c;
+    const Mine mine = cut_tiles<F>(a, c, g, record);
+    if (mine.pieces == 0) return;
+    rq = mine.rq;
+    row0 = mine.row0;
+    split = mine.split;
+    pieces = mine.pieces;
   } else {
     const uint32_t id = blockIdx.x;
     g = int(id % uint32_t(a.kv_heads));
     const uint32_t rest = id / uint32_t(a.kv_heads);
     split = int(rest / uint32_t(a.tiles));
-    slot = a.tiles - 1 - int(rest % uint32_t(a.tiles));  // the longest first
-    r = flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); });
-    local = int64_t(slot) - first_tile(a, r);
+    const int slot = a.tiles - 1 - int(rest % uint32_t(a.tiles));  // the longest first
+    rq = request_at(
+        a, flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); }));
+    const int64_t local = int64_t(slot) - first_tile(a, rq.r);
+    if (local < 0 || local * F::kRows >= int64_t(rq.n_new) * a.group) return;
+    row0 = int32_t(local) * F::kRows;
   }
-  const Request rq = request_at(a, r);
-  const int64_t rows = int64_t(rq.n_new) * a.group;
-  const int64_t row0 = local * F::kRows;
-  if (local < 0 || row0 >= rows) return;
-  const int64_t row_end = row0 + F::kRows < rows ? row0 + F::kRows : rows;
-  const int32_t tile_limit = seen(rq, int32_t((row_end - 1) / a.group));
-  const int32_t tile_least = seen(rq, int32_t(row0 / a.group));
+  const int32_t rows = rq.n_new * a.group, row_end = std::min(row0 + F::kRows, rows);
+  const int32_t tile_limit = seen(rq, token_of(a, row_end - 1));
+  const int32_t tile_least = seen(rq, token_of(a, row0));
   int32_t length = a.split_tokens;
   if constexpr (kCut)                            // (a piece's, of as many even ones)
     length = (tile_limit + pieces * F::kStep - 1) / (pieces * F::kStep) * F::kStep;
@@ -550,10 +577,10 @@ void chunk_attn(const ChunkArgs a) {
   const bool direct = kCut ? pieces == 1 : tile_limit <= length;
 
   // this lane's query row, as a column of S^T
-  const int64_t wrow = row0 + rw * 32, row = wrow + c32;
+  const int32_t wrow = row0 + rw * 32, row = wrow + c32;
   const bool live = row < rows;
-  const int32_t qi = live ? int32_t(row / a.group) : 0;
-  const int32_t qh = live ? int32_t(row - int64_t(qi) * a.group) : 0;
+  const int32_t qi = live ? token_of(a, row) : 0;
+  const int32_t qh = live ? row - qi * a.group : 0;
   const int64_t token = int64_t(rq.begin) + qi;
   const int32_t head = g * a.group + qh;
   W w;
@@ -561,9 +588,8 @@ void chunk_attn(const ChunkArgs a) {
   w.scale_log2 = a.scale_log2;
   w.lim = live ? seen(rq, qi) : 0;
   const bool any_row = wrow < rows;              // (the wave may hold no row)
-  const int32_t wlast = any_row ? int32_t((wrow + 31 < rows ? wrow + 31 : rows - 1) / a.group) : 0;
-  w.wlim = __builtin_amdgcn_readfirstlane(any_row ? seen(rq, wlast) : 0);
-  w.wleast = __builtin_amdgcn_readfirstlane(any_row ? seen(rq, int32_t(wrow / a.group)) : 0);
+  w.wlim = uniform(any_row ? seen(rq, token_of(a, std::min(wrow + 31, rows - 1))) : 0);
+  w.wleast = uniform(any_row ? seen(rq, token_of(a, wrow)) : 0);
 #pragma unroll
   for (int i = 0; i < W::kI; ++i) {
     u32x4 x = {0, 0, 0, 0};
@@ -583,7 +609,7 @@ void chunk_attn(const ChunkArgs a) {
   Source<F> src;
   src.base = a.kbase + g * kDh * 2;
   src.voff = a.voff;
-  src.table = a.tables + int64_t(r) * a.max_blocks;
+  src.table = a.tables + int64_t(rq.r) * a.max_blocks;
   src.bs = uint32_t(a.block_size);
   src.bs_magic = a.bs_magic;
   src.bs_shift = a.bs_shift;
@@ -800,8 +826,9 @@ __global__ __launch_bounds__(2 * F::kDh) void chunk_attn_join(const ChunkArgs a)
     }
   }
   if (!live) return;
-  const int64_t qi = row / a.group;
-  const int64_t orow = (int64_t(rq.begin) + qi) * a.q_heads + g * a.group + (row - qi * a.group);
+  const int32_t qi = token_of(a, int32_t(row));
+  const int64_t orow =
+      (int64_t(rq.begin) + qi) * a.q_heads + g * a.group + (int32_t(row) - qi * a.group);
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -885,12 +912,10 @@ void chunk_attn_few(const ChunkArgs a) {
       flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); });
   const Request rq = request_at(a, r);
   const int64_t local = int64_t(slot) - first_tile(a, r);
-  const int64_t rows = int64_t(rq.n_new) * a.group;
-  const int64_t row0 = local * kFewRows;
-  if (local < 0 || row0 >= rows) return;
-  const int64_t row_end = row0 + kFewRows < rows ? row0 + kFewRows : rows;
-  const int32_t tile_limit = seen(rq, int32_t((row_end - 1) / a.group));
-  const int32_t tile_least = seen(rq, int32_t(row0 / a.group));
+  if (local < 0 || local * kFewRows >= int64_t(rq.n_new) * a.group) return;
+  const int32_t row0 = int32_t(local) * kFewRows, rows = rq.n_new * a.group;
+  const int32_t tile_limit = seen(rq, token_of(a, std::min(row0 + kFewRows, rows) - 1));
+  const int32_t tile_least = seen(rq, token_of(a, row0));
   const int32_t s0 = split * a.split_tokens;
   if (split > 0 && s0 >= tile_limit) return;
   const int32_t s1 = tile_limit - s0 > a.split_tokens ? s0 + a.split_tokens : tile_limit;
@@ -902,10 +927,10 @@ void chunk_attn_few(const ChunkArgs a) {
   bf16x8 qb[kC][kI];
 #pragma unroll
   for (int c = 0; c < kC; ++c) {
-    const int64_t row = row0 + 16 * c + c16;
+    const int32_t row = row0 + 16 * c + c16;
     const bool live = row < rows;
-    const int32_t qi = live ? int32_t(row / a.group) : 0;
-    const int32_t qh = live ? int32_t(row - int64_t(qi) * a.group) : 0;
+    const int32_t qi = live ? token_of(a, row) : 0;
+    const int32_t qh = live ? row - qi * a.group : 0;
     lim[c] = live ? seen(rq, qi) : 0;
     if (tid < 16) lds.lim[16 * c + tid] = lim[c];
 #pragma unroll
@@ -1118,8 +1143,9 @@ void chunk_attn_few(const ChunkArgs a) {
         }
       }
     }
-    const int64_t tr = row0 + h;
-    const int64_t orow = (int64_t(rq.begin) + tr / a.group) * a.q_heads + g * a.group + tr % a.group;
+    const int32_t qi = token_of(a, row0 + h);
+    const int64_t orow =
+        (int64_t(rq.begin) + qi) * a.q_heads + g * a.group + (row0 + h - qi * a.group);
     if (direct) {
       const float inv = L == 0.f ? 0.f : 1.f / L;
       const u32x2 x = {pack_bf16(A[0] * inv, A[1] * inv), pack_bf16(A[2] * inv, A[3] * inv)};
@@ -1158,16 +1184,17 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_attn_merge(const ChunkArg
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t orow = kWavesPer == 1 ? int64_t(blockIdx.x) * 4 + wave : int64_t(blockIdx.x);
   if (orow >= int64_t(a.n_tokens) * a.q_heads) return;
-  const int32_t token = int32_t(orow / a.q_heads), head = int32_t(orow - int64_t(token) * a.q_heads);
+  const int32_t token = int32_t(uint32_t(orow) / uint32_t(a.q_heads));   // (orow < 2^26)
+  const int32_t head = int32_t(orow) - token * a.q_heads;
   const int32_t r =
       flowkv::last_at_most(a.n_req, token, [&](int32_t i) { return a.offsets[i]; });
   const Request rq = request_at(a, r);
   const int32_t i = token - rq.begin;
   if (i < 0 || i >= rq.n_new) return;
   // the tile that the row was in, as its workgroups saw it
-  const int64_t row = int64_t(i) * a.group + head % a.group;
-  const int64_t end = std::min<int64_t>((row / a.rows + 1) * a.rows, int64_t(rq.n_new) * a.group);
-  const int32_t tile_limit = seen(rq, int32_t((end - 1) / a.group));
+  const int32_t row = i * a.group + int32_t(uint32_t(head) % uint32_t(a.group));
+  const int32_t end = std::min(((row >> a.row_shift) + 1) << a.row_shift, rq.n_new * a.group);
+  const int32_t tile_limit = seen(rq, token_of(a, end - 1));
   if (tile_limit <= a.split_tokens) return;      // written already
   const int32_t n = (seen(rq, i) + a.split_tokens - 1) / a.split_tokens;
   const int64_t rec = record_at(a, orow, 0);
@@ -1243,6 +1270,14 @@ const Kind kKinds[] = {
     kind_of<Form<64, 8, 1>, Form<128, 8, 1>>(nullptr, chunk_attn_join<Form<128, 8, 1>>),
 };
 constexpr int kSplitUnit = 64;
+constexpr int kFewSteps = 8;               // of 32 tokens, a CU
+
+// x / d = (umulhi(x, m) + x) >> l with l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1.
+void by_product(uint32_t d, uint32_t* magic, uint32_t* shift) {
+  *shift = 0;
+  while ((uint64_t(1) << *shift) < d) ++*shift;
+  *magic = uint32_t((((uint64_t(1) << *shift) - d) << 32) / d + 1);
+}
 
 // Tile slots of a call, see first_tile.
 int64_t tile_slots(int64_t n_tokens, int64_t n_req, int group, int rows) {
@@ -1287,13 +1322,23 @@ int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_head
     return fail(FLOWKV_EINVAL, "split_tokens %d: need 0 or a multiple of %d", split_tokens,
                 kSplitUnit);
   const int group = q_heads / kv_heads;
+  if (int64_t(n_tokens) * group > INT32_MAX - 512)
+    return fail(FLOWKV_EINVAL, "%d tokens x %d query heads a KV head: need under 2^31 - 512",
+                n_tokens, group);
   // A step of 256 rows x 64 tokens moves half as much as one of 128 x 128, and the smaller
   // tiles share out better where there are few.
   const int64_t t256 = tiles_of(n_tokens, n_req, group, max_new, 256) * kv_heads;
   const int64_t t128 = tiles_of(n_tokens, n_req, group, max_new, 128) * kv_heads;
+  // Up to 32 rows a request, or few steps in all: 32 rows a workgroup and its waves apart in
+  // the keys end soonest.  (60 tokens behind 140, 4 heads of 64 on 2: 8.9 us, in 128 rows
+  // 10.1; 30 behind 500, 32 of 128 on 8: 13.6 and 16.8; but 1,000 behind none, 8 on 1: 29.0
+  // and 23.2.)
+  const int64_t t32 = tiles_of(n_tokens, n_req, group, max_new, 32) * kv_heads;
   const bool rule = split_tokens == 0;
   out->cut = out->order = false;
-  if (int64_t(max_new) * group <= 32 && split_tokens <= kFewSplit) {
+  if (split_tokens <= kFewSplit &&
+      (int64_t(max_new) * group <= 32 ||
+       (rule && t32 <= kCus && t32 * ((int64_t(max_seq_len) + 31) / 32) <= kFewSteps * kCus))) {
     out->kind = int64_t(max_new) * group > 16;
   } else if (t256 >= kCus) {
     out->kind = 3;
@@ -1428,9 +1473,8 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   a.ws = static_cast<float*>(workspace_dev);
   a.bunits = uint32_t(stride / 128);
   a.sunits = uint32_t(per_token / 128);
-  // q = (umulhi(t, m) + t) >> l with l = ceil(log2 bs), m = floor(2^32 (2^l - bs) / bs) + 1
-  while ((int64_t(1) << a.bs_shift) < bs) ++a.bs_shift;
-  a.bs_magic = uint32_t((((uint64_t(1) << a.bs_shift) - uint64_t(bs)) << 32) / uint64_t(bs) + 1);
+  by_product(uint32_t(bs), &a.bs_magic, &a.bs_shift);
+  by_product(uint32_t(q_heads / kv_heads), &a.g_magic, &a.g_shift);
   a.pool_blocks = pool->num_blocks;
   a.block_size = int32_t(bs);
   a.max_blocks = max_blocks;
@@ -1444,7 +1488,7 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   a.splits = sh.splits;
   a.scale_log2 = scale * kLog2e;
   const Kind& kind = kKinds[sh.kind];
-  a.rows = kind.rows;
+  while (1 << a.row_shift < kind.rows) ++a.row_shift;
   const int64_t tiles = tile_slots(n_tokens, n_req, a.group, kind.rows);
   const int64_t grid = tiles * kv_heads;
   // a wave per (new token, query head) where its lane groups hold all records at once
