@@ -62,6 +62,15 @@ struct ChunkArgs {
   float scale_log2;                     // scale * log2(e)
 };
 
+// The kernel's arguments, loaded here and not before.
+__device__ __forceinline__ ChunkArgs late_args() {
+  auto p = (const __attribute__((address_space(4))) void*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  ChunkArgs a;
+  __builtin_memcpy(&a, (const void*)p, sizeof(a));
+  return a;
+}
+
 // The rows of a request are its (new token, query head of the group) pairs,
 // token by token; a tile is 2^row_shift of them.  Tile slot x of the batch: request r
 // has the slots from floor(offsets[r] * G / rows) + r, which are enough for its
@@ -690,6 +699,8 @@ void chunk_attn(const ChunkArgs a) {
       if (t0 + kStep < s1) step(t0 + kStep, k1, v1, k0, v0);
     }
   }
+  // (read again where they are used: the loop has no scalar registers left for them)
+  const ChunkArgs e = late_args();
   const bool had_odd = __syncthreads_or(odd);
   float lsum = w.lsum + __shfl_xor(w.lsum, 32);
   float mref = w.mref;
@@ -733,10 +744,10 @@ void chunk_attn(const ChunkArgs a) {
   }
   if (had_odd) {
     for (int32_t t = odd_from; t < s1; ++t) {
-      const int32_t b = src.table[t / a.block_size];
-      if (b < 0 || b >= a.pool_blocks) continue;
-      const char* v = src.base + a.voff +
-                      (int64_t(b) * a.bunits + int64_t(t % a.block_size) * a.sunits) * 128;
+      const int32_t b = src.table[t / e.block_size];
+      if (b < 0 || b >= e.pool_blocks) continue;
+      const char* v = src.base + e.voff +
+                      (int64_t(b) * e.bunits + int64_t(t % e.block_size) * e.sunits) * 128;
 #pragma unroll
       for (int b = 0; b < kB; ++b)
 #pragma unroll
@@ -753,12 +764,12 @@ void chunk_attn(const ChunkArgs a) {
     for (int b = 0; b < kB; ++b)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<f32x4u*>(piece_sums<F>(a, record, rw, b) + (j * 64 + ln) * 4) =
+        *reinterpret_cast<f32x4u*>(piece_sums<F>(e, record, rw, b) + (j * 64 + ln) * 4) =
             f32x4u{w.o[b][4 * j], w.o[b][4 * j + 1], w.o[b][4 * j + 2], w.o[b][4 * j + 3]};
-    if (half == 0) piece_ml<F>(a, record, rw)[c32] = f32x2u{mref, lsum};
+    if (half == 0) piece_ml<F>(e, record, rw)[c32] = f32x2u{mref, lsum};
   }
   if (!live) return;
-  const int64_t orow = token * a.q_heads + head;
+  const int64_t orow = token * e.q_heads + head;
   if (direct) {
     const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
 #pragma unroll
@@ -767,17 +778,17 @@ void chunk_attn(const ChunkArgs a) {
       for (int i = 0; i < 16; i += 4) {
         const u32x2 x = {pack_bf16(w.o[b][i] * inv, w.o[b][i + 1] * inv),
                          pack_bf16(w.o[b][i + 2] * inv, w.o[b][i + 3] * inv)};
-        *reinterpret_cast<u32x2*>(a.out + orow * kDh + 32 * b + 2 * i + 4 * half) = x;
+        *reinterpret_cast<u32x2*>(e.out + orow * kDh + 32 * b + 2 * i + 4 * half) = x;
       }
   } else if constexpr (!kCut) {
-    const int64_t rec = record_at(a, orow, split);
+    const int64_t rec = record_at(e, orow, split);
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<f32x4u*>(record_sums(a, kDh, rec) + 32 * b + 2 * i + 4 * half) =
+        *reinterpret_cast<f32x4u*>(record_sums(e, kDh, rec) + 32 * b + 2 * i + 4 * half) =
             f32x4u{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
-    if (half == 0) *record_ml(a, kDh, rec) = f32x2u{mref, lsum};
+    if (half == 0) *record_ml(e, kDh, rec) = f32x2u{mref, lsum};
   }
 }
 
@@ -1308,6 +1319,29 @@ struct Shape {
 // CUs that a call is spread over (MI355X's, also where no device is asked).
 constexpr int kCus = 256;
 
+// The split that ends soonest by a simple count: the CUs' rounds over all tiles' splits, each
+// as long as its tokens and `fixed` more (a workgroup's start and end), and the merge.  In
+// few rows, 4 KiB of K and V a token: 5 new ones over 13,000, 8 KV heads, take 18.0 us in
+// splits of 512 (208 workgroups), 20.7 of 256, 23.2 of 384 (272), 20.1 of 768; 8 requests of 4
+// over up to 12,000 70.7 of 1,536 (512), 78.7 of 1,024, 85.7 of 2,048.
+int32_t best_split(int64_t tiles, int64_t max_seq_len, int64_t fixed, int64_t most) {
+  constexpr int64_t kUnit = 128, kMerge = 150;
+  constexpr int kTried[] = {1,  2,  3,  4,  5,  6,  8,  10, 12,  16,
+                            20, 24, 32, 40, 48, 64, 96, 128, 192, 256};
+  int64_t best = 0, least = INT64_MAX;
+  for (const int n : kTried) {
+    const int64_t even = ((max_seq_len + n - 1) / n + kUnit - 1) / kUnit * kUnit;
+    const int64_t s = std::min(std::max(even, kUnit), most), k = (max_seq_len + s - 1) / s;
+    const int64_t time = (tiles * k + kCus - 1) / kCus * (s + fixed) + (k > 1 ? kMerge : 0);
+    if (time < least) {
+      least = time;
+      best = s;
+    }
+    if (s == kUnit) break;
+  }
+  return int32_t(best);
+}
+
 // The form and the split of a call, and the workspace that it takes.
 int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads,
                int32_t head_dim, int32_t max_new, int32_t max_seq_len, int32_t split_tokens,
@@ -1366,12 +1400,10 @@ int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_head
   }
   const int64_t tiles =
       std::max<int64_t>(tiles_of(n_tokens, n_req, group, max_new, kind.rows) * kv_heads, 1);
+  constexpr int32_t kAll = INT32_MAX / kSplitUnit * kSplitUnit;
   if (rule) {
-    const int64_t aim = out->kind <= 1 ? 4 * kCus : kCus, want = (aim + tiles - 1) / tiles;
-    int64_t s = (int64_t(max_seq_len) + want - 1) / want;
-    s = std::max<int64_t>((s + 127) / 128 * 128, 256);
-    if (out->kind <= 1) s = std::min<int64_t>(s, kFewSplit);
-    split_tokens = int32_t(std::min<int64_t>(s, INT32_MAX / kSplitUnit * kSplitUnit));
+    if (out->kind <= 1) split_tokens = best_split(tiles, max_seq_len, 300, kFewSplit);
+    else split_tokens = tiles < kCus ? best_split(tiles, max_seq_len, 500, kAll) : kAll;
   }
   out->split = split_tokens;
   out->splits = int32_t((int64_t(max_seq_len) + split_tokens - 1) / split_tokens);
