@@ -148,6 +148,29 @@ __device__ __forceinline__ int v_swizzle(int x) {
   return kPc == 16 ? (x & 3) * 4 : (x >> 1 & 1) * 4;
 }
 
+// ---- many rows -----------------------------------------------------------------------
+//
+// One pass over the cached tokens: with a row's reference m and x = scale log2(e) q.K,
+//   l = sum 2^(x - m),  O = sum 2^(x - m) V,  out = O / l,
+// m being the largest x so far, or up to kLazy below it: O and l are scaled only when some x
+// is more than that above m, so that most steps have no scaling (weights then reach 2^8,
+// which costs neither float32 sums nor bf16 weights any relative precision).  Weights are
+// rounded to bf16 for the matrix product, as any library's are; l sums them unrounded.
+//
+// S^T = K Q^T and O^T = V^T P^T: a query row is a lane's column in both, so that the maximum,
+// the sum and the weights stay in the lane, and P needs no exchange between the products.
+// K and V reach LDS straight from memory, the next step's while this one is worked on
+// (through registers instead: a 13,000-token prompt 3.09 ms, not 1.49); V is read transposed
+// by the LDS itself.
+//
+// What bounds it: 4 Dh operations a (row, token) on the matrix units beside an exponential
+// and some ten vector operations, on a card that lowers its clock under this load (to about
+// 1.8 of 2.4 GHz).  The 13,000-token prompt, 32 heads of 128 on 8, takes 1.32 ms, 1.05
+// PFLOP/s (a library's product of 4,096^3 reaches 1.13 there, of 16,384^3 1.34); 20,000 tokens, 8
+// heads of 64 on 4, 542 us, 0.76, where exponentials take as long as products.  A lone step
+// is bound by its load (a CU alone draws about 45 bytes a nanosecond) and its latencies:
+// 1.7 us for 256 rows x 64 tokens of 128.
+//
 // The form of a workgroup: kRw waves side by side in rows (32 each), kKw in keys; a wave
 // takes kTile cached tokens a step.
 constexpr int kTile = 64;
@@ -162,8 +185,8 @@ struct Form {
   static constexpr int kLdRows = kThreads / kPc;      // tokens of one such load
   static constexpr int kGroup = kThreads / kStep;     // steps whose places are found at once
   // (the swizzles repeat with 16 rows; a group's places are found in its predecessor's
-  // first step and read in its last)
-  static_assert(kGroup >= 2 && kLdRows % 16 == 0);
+  // first step, and read from two steps before they are used)
+  static_assert(kGroup >= 3 && kLdRows % 16 == 0);
 };
 
 // What a wave carries through the steps.
@@ -304,6 +327,7 @@ struct Source {
   uint32_t kpiece, vpiece;                       // the lane's bytes of a row,
   uint32_t row;                                  // and its first row of a step
   Places<F>* places;
+  uint32_t u[F::kLd];                            // the places of the step that is sent next
   int32_t next_block;
   uint32_t next_slot;
   bool next_in;
@@ -334,14 +358,16 @@ struct Source {
     return uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(d >> 32)))) << 32 |
            uint32_t(__builtin_amdgcn_readfirstlane(int(d)));
   }
-  // The rows of step i on their way to LDS, with no register between.  An instruction
-  // fills 64 consecutive 16-byte places, so a lane's place is fixed, and the swizzle is in
-  // which piece of the row it reads.
-  __device__ __forceinline__ void send(int i, lvec* k, lvec* v) const {
-    uint32_t u[F::kLd];
+  // The lane's places of step i.
+  __device__ __forceinline__ void look(int i) {
 #pragma unroll
     for (int e = 0; e < F::kLd; ++e)
       u[e] = places->at[i % (2 * F::kGroup) * F::kStep + row + e * F::kLdRows];
+  }
+  // The rows at the lane's places on their way to LDS, with no register between.  An
+  // instruction fills 64 consecutive 16-byte places, so a lane's place is fixed, and the
+  // swizzle is in which piece of the row it reads.
+  __device__ __forceinline__ void send(lvec* k, lvec* v) const {
 #pragma unroll
     for (int e = 0; e < F::kLd; ++e) {
       const uint64_t off = uint64_t(u[e]) * 128;
@@ -669,7 +695,7 @@ void chunk_attn(const ChunkArgs a) {
                     lvec* __restrict__ v_to) {
       const bool more = t0 + kStep < s1;
       const bool find = i % F::kGroup == 0;      // the next group's places
-      if (more) src.send(i + 1, k_to, v_to);
+      if (more) src.send(k_to, v_to);
       if (find) src.fetch(i / F::kGroup + 1);
       const int32_t t = t0 + kw * kTile;
       if (t < w.wlim && t < s1) {
@@ -679,6 +705,7 @@ void chunk_attn(const ChunkArgs a) {
         w.weigh(s, t, __builtin_expect(suspect, 0) ? src.dead(t - s0) : 0, p);
         w.add(v, p);
       }
+      src.look(i + 2);
       if (find) src.place(i / F::kGroup + 1);
       if (more) landed(v_to, t0 + kStep);
       __syncthreads();
@@ -691,7 +718,9 @@ void chunk_attn(const ChunkArgs a) {
     src.place(0);
     __syncthreads();
     suspect = src.any_dead(0);
-    src.send(0, k0, v0);
+    src.look(0);
+    src.send(k0, v0);
+    src.look(1);
     landed(v0, s0);
     __syncthreads();
     for (int32_t t0 = s0; t0 < s1; t0 += 2 * kStep) {
@@ -861,6 +890,9 @@ __global__ __launch_bounds__(2 * F::kDh) void chunk_attn_join(const ChunkArgs a)
 //   - K goes through the wave's part of LDS into the A operand, row m of half gg being
 //     token 16 gg + 4 (m % 4) + m / 4: a lane's scores are then those of the tokens whose
 //     V it holds, and P and V are operands of P.V where they are.
+// 24 requests of 2 to 8 tokens over 2,000 to 16,000, 32 heads of 128 on 8 (915 MB) take 178
+// us with the merge, 5.1 TB/s; 64 of one token over 500 to 4,000 112 us (128 rows a
+// workgroup: 137).  K and V are read once and past the caches.
 constexpr int kFewWaves = 4;
 constexpr int kFewThreads = 64 * kFewWaves;
 constexpr int kFewTile = 32;
@@ -1171,7 +1203,8 @@ void chunk_attn_few(const ChunkArgs a) {
 
 // Joins the splits' records of the rows whose tile has more than one: a wave, or the four
 // of a workgroup, per (new token, query head), Dh / 4 lanes a record, kMergeChunk records
-// of a lane group under way at once.
+// of a lane group under way at once.  A launch and three dependent loads bound it: 4.0 us for
+// 5 tokens x 32 heads x 26 splits.
 constexpr int kMergeThreads = 256;
 constexpr int kMergeChunk = 8;
 
