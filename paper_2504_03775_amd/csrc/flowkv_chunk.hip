@@ -38,6 +38,8 @@ typedef __attribute__((address_space(3))) void lvoid;
 typedef __attribute__((address_space(3))) u32x4 lvec;
 typedef __attribute__((address_space(3))) uint8_t lbyte;
 
+// CUs that a call is spread over (MI355X's, also where no device is asked).
+constexpr int kCus = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;               // log2 of the largest unnormalised weight
 
@@ -58,7 +60,7 @@ struct ChunkArgs {
   int32_t n_tokens, n_req, q_heads, kv_heads, group;
   int32_t row_shift;                    // query rows of a workgroup's tile: 2^row_shift
   int32_t tiles, split_tokens, splits;
-  int32_t pieces;                       // work by the lengths: of all tiles; 0: whole tiles
+  int32_t pieces;                       // work by the lengths: at most; 0: whole tiles
   float scale_log2;                     // scale * log2(e)
 };
 
@@ -167,7 +169,7 @@ __device__ __forceinline__ int v_swizzle(int x) {
 // and some ten vector operations, on a card that lowers its clock under this load (to about
 // 1.8 of 2.4 GHz).  The 13,000-token prompt, 32 heads of 128 on 8, takes 1.32 ms, 1.05
 // PFLOP/s (a library's product of 4,096^3 reaches 1.13 there, of 16,384^3 1.34); 20,000 tokens, 8
-// heads of 64 on 4, 542 us, 0.76, where exponentials take as long as products.  A lone step
+// heads of 64 on 4, 510 us, 0.80, where exponentials take as long as products.  A lone step
 // is bound by its load (a CU alone draws about 45 bytes a nanosecond) and its latencies:
 // 1.7 us for 256 rows x 64 tokens of 128.
 //
@@ -179,6 +181,11 @@ struct Form {
   static constexpr int kDh = kDh_, kRw = kRw_, kKw = kKw_;
   static constexpr int kWaves = kRw * kKw, kThreads = 64 * kWaves;
   static constexpr int kRows = 32 * kRw;
+  // Workgroups on a CU at once.  At 64 dims two fit into the registers (128 a lane, with the
+  // operands of one product read ahead, not of 8), and hide each other's latencies: 16
+  // prompts of 500 to 3,000 tokens, 8 heads on 4, 140 us, not 160.
+  static constexpr int kPerCu = kDh == 64 ? 2 : 1;
+  static constexpr int kAhead = kDh == 64 ? 1 : 8;
   static constexpr int kStep = kTile * kKw;         // tokens of a step
   static constexpr int kPc = kDh / 8;            // 16-byte pieces of a row
   static constexpr int kLd = kStep * kPc / kThreads;  // 16-byte loads of a step's K, or V, a lane
@@ -233,10 +240,10 @@ struct Wave {
     return u32x4{lo[0], lo[1], hi[0], hi[1]};
   }
 
-  // S^T = K Q^T: rows are tokens, columns query rows.  The operands of 8 products are read
-  // ahead.
+  // S^T = K Q^T: rows are tokens, columns query rows.  The operands of kAhead products are
+  // read ahead.
   __device__ __forceinline__ void scores(f32x16 (&s)[kN], const lvec* k) const {
-    constexpr int kM = kN * kI, kAhead = 8 < kM ? 8 : kM;
+    constexpr int kM = kN * kI, kAhead = F::kAhead;
     u32x4 w[kM];
 #pragma unroll
     for (int b = 0; b < kN; ++b) s[b] = f32x16{};
@@ -384,7 +391,7 @@ struct Source {
 // The host sees only the longest request.  Two kinds of call have every workgroup look at
 // all lengths first (about 3 us), and find what it does from them by itself:
 //   - fewer tiles than CUs, but long ones: a tile's steps are cut into pieces, one to a
-//     workgroup, no longer than need be for all tiles' to be a CU's each.  (With one length
+//     workgroup, no longer than need be for all of them to be on the CUs at once.  (With one length
 //     of split for contexts of 500 to 9,000 tokens, or under the causal diagonal, some CUs
 //     have nothing while others go round twice.)  Tiles in more than one piece are joined
 //     from their records by a second kernel.  Chunks of 100 to 700 tokens beside 20 single
@@ -396,7 +403,6 @@ struct Source {
 //     single ones over 100 to 6,600, 32 heads on 8: 255 us, in the requests' order 339.
 //     (Prompts with nothing cached gain nothing: the diagonal orders each of them.)
 constexpr int kPieceTiles = 512;           // most tile slots, and requests, of such a call
-constexpr int kPieces = 256;               // MI355X's CUs
 constexpr int kPieceLeast = 2;             // steps
 constexpr int kCutSteps = 16;              // steps a CU, were all tiles the longest, from which on
 
@@ -431,12 +437,20 @@ __device__ __forceinline__ float* piece_sums(const ChunkArgs& a, int64_t rec, in
 }
 template <class F>
 __device__ __forceinline__ f32x2u* piece_ml(const ChunkArgs& a, int64_t rec, int rw) {
-  return reinterpret_cast<f32x2u*>(a.ws + int64_t(kPieces) * F::kRows * F::kDh) +
+  return reinterpret_cast<f32x2u*>(a.ws + int64_t(F::kPerCu) * kCus * F::kRows * F::kDh) +
          (rec * F::kRw + rw) * 32;
 }
 template <class F>
 __device__ __forceinline__ int32_t* piece_first(const ChunkArgs& a) {
-  return reinterpret_cast<int32_t*>(a.ws + int64_t(kPieces) * F::kRows * (F::kDh + 2));
+  return reinterpret_cast<int32_t*>(a.ws + int64_t(F::kPerCu) * kCus * F::kRows * (F::kDh + 2));
+}
+
+// The workgroup's number.  Where two are on a CU at once and that is all there are, the
+// second ones come in reverse, the shortest beside the longest.
+template <class F>
+__device__ __forceinline__ uint32_t paired() {
+  const uint32_t id = blockIdx.x, n = gridDim.x;
+  return F::kPerCu == 2 && id >= uint32_t(kCus) && n <= 2 * kCus ? n - 1 - (id - kCus) : id;
 }
 
 // Finds the workgroup's tile, or its piece of one, and the KV head; kPieceTiles lanes, one
@@ -475,7 +489,8 @@ __device__ __forceinline__ Mine cut_tiles(const ChunkArgs& a, Cut& c, int& g, in
     const uint32_t key = uint32_t(n) * kPieceTiles + uint32_t(tid);
     c.key[tid] = key;
     __syncthreads();
-    g = int(blockIdx.x % uint32_t(a.kv_heads));
+    const uint32_t id = paired<F>();
+    g = int(id % uint32_t(a.kv_heads));
     if (n > 0) {
       int32_t before = 0;
 #pragma unroll 4
@@ -486,7 +501,7 @@ __device__ __forceinline__ Mine cut_tiles(const ChunkArgs& a, Cut& c, int& g, in
         before += x[2] > key;
         before += x[3] > key;
       }
-      if (before == int32_t(blockIdx.x / uint32_t(a.kv_heads))) {
+      if (before == int32_t(id / uint32_t(a.kv_heads))) {
         mine.split = 0;
         mine.pieces = 1;
         c.mine = mine;
@@ -554,7 +569,7 @@ __device__ __forceinline__ Mine cut_tiles(const ChunkArgs& a, Cut& c, int& g, in
       if (tid == 0) piece_first<F>(a)[0] = 0;
       if (tid < a.tiles) piece_first<F>(a)[tid + 1] = sum;
     }
-    g = total ? record / total : 0;
+    g = uniform(total ? record / total : 0);
     mine.split = record - g * total - (sum - mine.pieces);
     if (mine.split >= 0 && mine.split < mine.pieces && g < a.kv_heads) c.mine = mine;
     __syncthreads();
@@ -568,7 +583,7 @@ __device__ __forceinline__ Mine cut_tiles(const ChunkArgs& a, Cut& c, int& g, in
 }
 
 template <class F, bool kCut>
-__global__ __launch_bounds__(F::kThreads, 2)
+__global__ __launch_bounds__(F::kThreads, 2 * F::kPerCu)
 void chunk_attn(const ChunkArgs a) {
   typedef Wave<F> W;
   constexpr int kDh = F::kDh, kPc = F::kPc, kStep = F::kStep, kB = W::kB;
@@ -589,7 +604,7 @@ void chunk_attn(const ChunkArgs a) {
     split = mine.split;
     pieces = mine.pieces;
   } else {
-    const uint32_t id = blockIdx.x;
+    const uint32_t id = paired<F>();
     g = int(id % uint32_t(a.kv_heads));
     const uint32_t rest = id / uint32_t(a.kv_heads);
     split = int(rest / uint32_t(a.tiles));
@@ -728,8 +743,10 @@ void chunk_attn(const ChunkArgs a) {
       if (t0 + kStep < s1) step(t0 + kStep, k1, v1, k0, v0);
     }
   }
-  // (read again where they are used: the loop has no scalar registers left for them)
+  // (the arguments and the lane's row again: the loop has no registers left for them)
   const ChunkArgs e = late_args();
+  const int lane = int(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)));
+  const int hi = lane >> 5;
   const bool had_odd = __syncthreads_or(odd);
   float lsum = w.lsum + __shfl_xor(w.lsum, 32);
   float mref = w.mref;
@@ -739,8 +756,8 @@ void chunk_attn(const ChunkArgs a) {
     constexpr int kFit = int(sizeof(sk0)) / (F::kRw * 64 * 16 * int(sizeof(float)));
     constexpr int kR = kFit < kB ? kFit : kB;
     static_assert(kR >= 1 && kB % kR == 0 && sizeof(sk1) >= F::kRw * 2 * 64 * sizeof(float));
-    float* const sums = reinterpret_cast<float*>(sk0) + rw * (kR * 16 * 64) + ln;
-    float* const ml = reinterpret_cast<float*>(sk1) + rw * 128 + ln;
+    float* const sums = reinterpret_cast<float*>(sk0) + rw * (kR * 16 * 64) + lane;
+    float* const ml = reinterpret_cast<float*>(sk1) + rw * 128 + lane;
     for (int from = 1; from < F::kKw; ++from) {
       float c1 = 0.f, c2 = 0.f;
 #pragma unroll
@@ -782,7 +799,7 @@ void chunk_attn(const ChunkArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const uint32_t y = uint32_t(reinterpret_cast<const uint16_t*>(
-                                 v)[32 * b + 8 * (i / 4) + 4 * half + i % 4])
+                                 v)[32 * b + 8 * (i / 4) + 4 * hi + i % 4])
                              << 16;
           if ((y & 0x7f800000u) == 0x7f800000u && t < w.lim) w.o[b][i] += __uint_as_float(y);
         }
@@ -793,12 +810,15 @@ void chunk_attn(const ChunkArgs a) {
     for (int b = 0; b < kB; ++b)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<f32x4u*>(piece_sums<F>(e, record, rw, b) + (j * 64 + ln) * 4) =
+        *reinterpret_cast<f32x4u*>(piece_sums<F>(e, record, rw, b) + (j * 64 + lane) * 4) =
             f32x4u{w.o[b][4 * j], w.o[b][4 * j + 1], w.o[b][4 * j + 2], w.o[b][4 * j + 3]};
-    if (half == 0) piece_ml<F>(e, record, rw)[c32] = f32x2u{mref, lsum};
+    if (hi == 0) piece_ml<F>(e, record, rw)[lane & 31] = f32x2u{mref, lsum};
   }
-  if (!live) return;
-  const int64_t orow = token * e.q_heads + head;
+  const int32_t late_row = wrow + (lane & 31);     // of the request
+  if (late_row >= rows) return;
+  const int32_t new_token = token_of(e, late_row);
+  const int64_t orow = (int64_t(rq.begin) + new_token) * e.q_heads + g * e.group +
+                       (late_row - new_token * e.group);
   if (direct) {
     const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
 #pragma unroll
@@ -807,7 +827,7 @@ void chunk_attn(const ChunkArgs a) {
       for (int i = 0; i < 16; i += 4) {
         const u32x2 x = {pack_bf16(w.o[b][i] * inv, w.o[b][i + 1] * inv),
                          pack_bf16(w.o[b][i + 2] * inv, w.o[b][i + 3] * inv)};
-        *reinterpret_cast<u32x2*>(e.out + orow * kDh + 32 * b + 2 * i + 4 * half) = x;
+        *reinterpret_cast<u32x2*>(e.out + orow * kDh + 32 * b + 2 * i + 4 * hi) = x;
       }
   } else if constexpr (!kCut) {
     const int64_t rec = record_at(e, orow, split);
@@ -815,9 +835,9 @@ void chunk_attn(const ChunkArgs a) {
     for (int b = 0; b < kB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<f32x4u*>(record_sums(e, kDh, rec) + 32 * b + 2 * i + 4 * half) =
+        *reinterpret_cast<f32x4u*>(record_sums(e, kDh, rec) + 32 * b + 2 * i + 4 * hi) =
             f32x4u{w.o[b][i], w.o[b][i + 1], w.o[b][i + 2], w.o[b][i + 3]};
-    if (half == 0) *record_ml(e, kDh, rec) = f32x2u{mref, lsum};
+    if (hi == 0) *record_ml(e, kDh, rec) = f32x2u{mref, lsum};
   }
 }
 
@@ -1293,7 +1313,8 @@ typedef void (*ChunkFn)(ChunkArgs);
 // The forms, by how many rows a request brings and how many workgroups there are.
 struct Kind {
   int rows, threads, step;
-  ChunkFn fn[2];                                 // head_dim 64, 128
+  int per_cu[2];                                 // head_dim 64, 128, as below
+  ChunkFn fn[2];
   ChunkFn cut[2], join[2];                       // work by the lengths
 };
 template <class F64, class F128>
@@ -1303,13 +1324,14 @@ constexpr Kind kind_of(ChunkFn join64, ChunkFn join128) {
   return Kind{F64::kRows,
               F64::kThreads,
               F64::kStep,
+              {F64::kPerCu, F128::kPerCu},
               {chunk_attn<F64, false>, chunk_attn<F128, false>},
               {chunk_attn<F64, true>, chunk_attn<F128, true>},
               {join64, join128}};
 }
 const Kind kKinds[] = {
-    {16, kFewThreads, kFewTile, {chunk_attn_few<64, 1>, chunk_attn_few<128, 1>}, {}, {}},
-    {32, kFewThreads, kFewTile, {chunk_attn_few<64, 2>, chunk_attn_few<128, 2>}, {}, {}},
+    {16, kFewThreads, kFewTile, {}, {chunk_attn_few<64, 1>, chunk_attn_few<128, 1>}, {}, {}},
+    {32, kFewThreads, kFewTile, {}, {chunk_attn_few<64, 2>, chunk_attn_few<128, 2>}, {}, {}},
     kind_of<Form<64, 4, 2>, Form<128, 4, 2>>(chunk_attn_join<Form<64, 4, 2>>, nullptr),
     kind_of<Form<64, 8, 1>, Form<128, 8, 1>>(nullptr, chunk_attn_join<Form<128, 8, 1>>),
 };
@@ -1344,13 +1366,11 @@ bool by_lengths(int64_t n_tokens, int64_t n_req, int group, int64_t max_seq_len,
 
 struct Shape {
   int kind;
-  int32_t split, splits;
+  int32_t split, splits, pieces;
   bool cut, order;                               // pieces by the lengths; tiles, the longest first
   int64_t need;
 };
 
-// CUs that a call is spread over (MI355X's, also where no device is asked).
-constexpr int kCus = 256;
 
 // The split that ends soonest by a simple count: the CUs' rounds over all tiles' splits, each
 // as long as its tokens and `fixed` more (a workgroup's start and end), and the merge.  In
@@ -1424,9 +1444,10 @@ int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_head
   if (out->cut || out->order) {
     out->split = 0;
     out->splits = 1;
+    out->pieces = kind.per_cu[head_dim == 128] * kCus;
     out->need = 0;
     if (out->cut)
-      out->need = (int64_t(kPieces) * kind.rows * (head_dim + 2) +
+      out->need = (int64_t(out->pieces) * kind.rows * (head_dim + 2) +
                    tile_slots(n_tokens, n_req, group, kind.rows) + 1) *
                   int64_t(sizeof(float));
     return FLOWKV_OK;
@@ -1564,11 +1585,11 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
     return fail(FLOWKV_EINVAL, "%lld tiles of queries x %d splits: too many for one call",
                 (long long)grid, sh.splits);
   a.tiles = int32_t(tiles);
-  a.pieces = sh.cut ? kPieces : 0;
+  a.pieces = sh.cut ? sh.pieces : 0;
   void* args[] = {&a};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int d128 = head_dim == 128;
-  const int64_t groups = sh.cut ? std::max<int64_t>(grid, kPieces) : grid * sh.splits;
+  const int64_t groups = sh.cut ? std::max<int64_t>(grid, sh.pieces) : grid * sh.splits;
   hipError_t e = hipLaunchKernel(
       reinterpret_cast<const void*>(sh.cut || sh.order ? kind.cut[d128] : kind.fn[d128]),
       dim3(unsigned(groups)), dim3(unsigned(kind.threads)), args, 0, st);

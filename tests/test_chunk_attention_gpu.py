@@ -325,8 +325,8 @@ LONGEST = 400_000       # a length that the caller has to allow for, whatever th
 
 def pieces_bytes(b, hk, G, d):
     """Workspace of a call whose tiles are cut by the lengths on the device."""
-    rows = 256 if d == 128 else 128
-    return (256 * rows * (d + 2) + b.n_tokens * G // rows + len(b.new) + 1) * 4
+    rows, pieces = (256, 256) if d == 128 else (128, 512)
+    return (pieces * rows * (d + 2) + b.n_tokens * G // rows + len(b.new) + 1) * 4
 
 
 MIXED = [  # as BATCHES, with more than 32 rows of a request in every shape
