@@ -167,7 +167,7 @@ __device__ __forceinline__ int v_swizzle(int x) {
 //
 // What bounds it: 4 Dh operations a (row, token) on the matrix units beside an exponential
 // and some ten vector operations, on a card that lowers its clock under this load (to about
-// 1.8 of 2.4 GHz).  The 13,000-token prompt, 32 heads of 128 on 8, takes 1.32 ms, 1.05
+// 1.8 of 2.4 GHz).  The 13,000-token prompt, 32 heads of 128 on 8, takes 1.31 ms, 1.06
 // PFLOP/s (a library's product of 4,096^3 reaches 1.13 there, of 16,384^3 1.34); 20,000 tokens, 8
 // heads of 64 on 4, 510 us, 0.80, where exponentials take as long as products.  A lone step
 // is bound by its load (a CU alone draws about 45 bytes a nanosecond) and its latencies:
@@ -395,12 +395,12 @@ struct Source {
 //     of split for contexts of 500 to 9,000 tokens, or under the causal diagonal, some CUs
 //     have nothing while others go round twice.)  Tiles in more than one piece are joined
 //     from their records by a second kernel.  Chunks of 100 to 700 tokens beside 20 single
-//     ones over up to 8,000 cached, 8 heads of 128 on one KV head: 69 us, by even splits 84;
-//     512 tokens behind 8,000, 32 heads on 8: 87 and 94; 4,000 behind none, 8 on 1: 61 and
-//     72.  With few steps the even splits are faster: 256 behind 4,000, 32 on 8: 38 and 42.
+//     ones over up to 8,000 cached, 8 heads of 128 on one KV head: 66 us, by even splits 84;
+//     512 tokens behind 8,000, 32 heads on 8: 86 and 93; 4,000 behind none, 8 on 1: 60 and
+//     71.  With few steps the even splits are faster: 256 behind 4,000, 32 on 8: 38 and 42.
 //   - more tiles than CUs, of requests with much in the cache: whole tiles, the longest
 //     first, so that the last ones to end are short.  4 chunks of 100 to 600 tokens beside 36
-//     single ones over 100 to 6,600, 32 heads on 8: 255 us, in the requests' order 339.
+//     single ones over 100 to 6,600, 32 heads on 8: 242 us, in the requests' order 339.
 //     (Prompts with nothing cached gain nothing: the diagonal orders each of them.)
 constexpr int kPieceTiles = 512;           // most tile slots, and requests, of such a call
 constexpr int kPieceLeast = 2;             // steps

@@ -1,7 +1,7 @@
 """ctypes binding to ``libflowkv.so`` (the C ABI in ``include/flowkv.h``).
 
 Argument marshalling only: every step -- allocation, alignment, the copy,
-decode attention, the scheduler's evaluation and routing -- runs in the
+attention, appends, the scheduler's evaluation and routing -- runs in the
 native library.  PyTorch supplies device memory and streams.  The functions
 carry the C names; ``Allocator``, ``Scheduler`` and ``KVPool`` are thin
 owners of a handle or of a pool descriptor.
