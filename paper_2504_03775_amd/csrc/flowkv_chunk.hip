@@ -1381,11 +1381,13 @@ int32_t best_split(int64_t tiles, int64_t max_seq_len, int64_t fixed, int64_t mo
   constexpr int64_t kUnit = 128, kMerge = 150;
   constexpr int kTried[] = {1,  2,  3,  4,  5,  6,  8,  10, 12,  16,
                             20, 24, 32, 40, 48, 64, 96, 128, 192, 256};
-  int64_t best = 0, least = INT64_MAX;
+  int64_t best = kUnit;
+  double least = INFINITY;
   for (const int n : kTried) {
     const int64_t even = ((max_seq_len + n - 1) / n + kUnit - 1) / kUnit * kUnit;
     const int64_t s = std::min(std::max(even, kUnit), most), k = (max_seq_len + s - 1) / s;
-    const int64_t time = (tiles * k + kCus - 1) / kCus * (s + fixed) + (k > 1 ? kMerge : 0);
+    const double rounds = std::ceil(double(tiles) * double(k) / kCus);   // (past 64 bits, maybe)
+    const double time = rounds * double(s + fixed) + (k > 1 ? kMerge : 0);
     if (time < least) {
       least = time;
       best = s;
@@ -1463,9 +1465,10 @@ int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_head
   out->splits = int32_t((int64_t(max_seq_len) + split_tokens - 1) / split_tokens);
   if (out->splits < 1) out->splits = 1;
   out->need = 0;
-  if (out->splits > 1 &&
-      __builtin_mul_overflow(int64_t(n_tokens) * q_heads * (head_dim + 2) * int64_t(sizeof(float)),
-                             int64_t(out->splits), &out->need))
+  const int64_t record = (head_dim + 2) * int64_t(sizeof(float));
+  if (out->splits > 1 &&                         // (fewer than 2^62 records)
+      (__builtin_mul_overflow(int64_t(n_tokens) * q_heads, record, &out->need) ||
+       __builtin_mul_overflow(out->need, int64_t(out->splits), &out->need)))
     return fail(FLOWKV_EINVAL, "%d splits: the workspace's size overflows", out->splits);
   return FLOWKV_OK;
 }

@@ -244,6 +244,15 @@ def test_chunk_attention_workspace_is_what_the_header_says():
                 (1, 1, 8, 2, 128, 1, 10, 63), (2**31 - 1, 1, 2**30, 1, 128, 1, 2**31 - 5000, 64)):
         with pytest.raises(fk.FlowKVError):
             ws(*bad)
+    top = 2**31 - 1
+    for bad in ((top - 511, 1, 1, 1, 128, 1, 10), (2**29, 1, 32, 8, 128, 1, 10, 64),
+                (2**30, top, top, top, 64, 1, top, 64),
+                (2**26, top, 2**20, 2**20, 64, 1, top)):       # past 2^63 bytes
+        with pytest.raises(fk.FlowKVError):
+            ws(*bad)
+    for big in ((top - 512, top, top, top, 64, top, 0), (1, top, top, top, 128, 1, top),
+                (512, 512, 1, 1, 64, 1, top)):
+        assert ws(*big) >= 0
     b = ctypes.c_int64()
     assert fk.lib().flowkv_chunk_attention_workspace(1, 1, 1, 1, 64, 1, 1, 0, None) == fk.EINVAL
 
