@@ -521,10 +521,12 @@ class KVPool:
                 raise ValueError("pool tensors must be contiguous device tensors")
         self.layout, self.num_layers, self.num_blocks = layout, L, B
         self.block_size, self.kv_heads, self.head_dim = bs, hkv, dh
+        self.dtype = self.tensors[0].dtype            # (a pool's tensors have one type)
         self.elem_bytes = self.tensors[0].element_size()
         self.chunk_bytes = bs * hkv * dh * self.elem_bytes
         self.block_bytes = 2 * L * self.chunk_bytes
         self.device = self.tensors[0].device
+        self.index = self.tensors[0].get_device()
         self._bases = (ctypes.c_void_p * len(self.tensors))(*[x.data_ptr() for x in self.tensors])
         self.desc = flowkv_pool(layout, L, B, 0, self.chunk_bytes,
                                 ctypes.cast(self._bases, ctypes.POINTER(ctypes.c_void_p)))
@@ -730,7 +732,7 @@ def _on_pool_device(pool: KVPool, stream, where: str, fn, *args) -> None:
 
     if stream is not None and stream.device != pool.device:
         raise ValueError(f"{where}: the stream is on {stream.device}, the pool on {pool.device}")
-    index = pool.device.index
+    index = pool.index
     try:
         current, raw = torch._C._cuda_getDevice(), torch._C._cuda_getCurrentRawStream
     except AttributeError:
@@ -748,36 +750,41 @@ def _on_pool_device(pool: KVPool, stream, where: str, fn, *args) -> None:
         raise FlowKVError(rc, where)
 
 
-def _check_ragged(pool: KVPool, q_offsets, block_tables, seq_lens) -> int:
-    """The batch arrays of flowkv_append and flowkv_chunk_attention; the requests' count."""
+def _check_ragged(pool: KVPool, q_offsets, block_tables, seq_lens) -> tuple:
+    """The batch arrays of flowkv_append and flowkv_chunk_attention; the requests'
+    count and the blocks that each has room for.  (These checks are most of a short
+    call's host time: tensors are asked once, and for a device's index, not for the
+    device.)"""
     import torch
 
-    dev, i32 = pool.device, torch.int32
-    n = seq_lens.numel()
-    for t, dims in ((q_offsets, 1), (block_tables, 2), (seq_lens, 1)):
-        if t.dtype is not i32 or t.dim() != dims or not t.is_contiguous() or t.device != dev:
+    index, i32 = pool.index, torch.int32
+    off, tab, lens = q_offsets.shape, block_tables.shape, seq_lens.shape
+    for t, shape, dims in ((q_offsets, off, 1), (block_tables, tab, 2), (seq_lens, lens, 1)):
+        if t.dtype is not i32 or len(shape) != dims or not t.is_contiguous() \
+                or t.get_device() != index:
             raise ValueError(f"q_offsets, block_tables and seq_lens: need contiguous int32 tensors "
-                             f"of 1, 2 and 1 dimensions on {dev}, got {t.dtype} {tuple(t.shape)} "
-                             f"on {t.device}")
-    if q_offsets.numel() != n + 1 or len(block_tables) != n:
-        raise ValueError(f"{n} lengths, {q_offsets.numel()} offsets (one more is needed) and "
-                         f"{len(block_tables)} block lists")
-    return n
+                             f"of 1, 2 and 1 dimensions on {pool.device}, got {t.dtype} "
+                             f"{tuple(shape)} on {t.device}")
+    n = lens[0]
+    if off[0] != n + 1 or tab[0] != n:
+        raise ValueError(f"{n} lengths, {off[0]} offsets (one more is needed) and "
+                         f"{tab[0]} block lists")
+    return n, tab[1]
 
 
-def _token_stride(t, name: str, heads: int, dim: int, dtype, device) -> int:
+def _token_stride(t, shape, name: str, heads: int, dim: int, dtype, pool: KVPool) -> int:
     """Elements between the tokens of a (n, heads, dim) tensor whose tokens are
     each in one piece."""
-    shape, stride = t.shape, t.stride()
     if len(shape) != 3 or shape[1] != heads or shape[2] != dim or t.dtype is not dtype \
-            or t.device != device:
-        raise ValueError(f"{name}: need (tokens, {heads}, {dim}) {dtype} on {device}, got "
+            or t.get_device() != pool.index:
+        raise ValueError(f"{name}: need (tokens, {heads}, {dim}) {dtype} on {pool.device}, got "
                          f"{tuple(shape)} {t.dtype} on {t.device}")
     if shape[0] == 0:
         return heads * dim
-    if (dim > 1 and stride[2] != 1) or (heads > 1 and stride[1] != dim):
-        raise ValueError(f"{name}: a token's heads must lie together, strides are {stride}")
-    return stride[0] if shape[0] > 1 else heads * dim
+    token, head, one = t.stride()
+    if (dim > 1 and one != 1) or (heads > 1 and head != dim):
+        raise ValueError(f"{name}: a token's heads must lie together, strides are {t.stride()}")
+    return token if shape[0] > 1 else heads * dim
 
 
 def flowkv_append(pool: KVPool, layer: int, k, v, q_offsets, block_tables, seq_lens,
@@ -788,16 +795,17 @@ def flowkv_append(pool: KVPool, layer: int, k, v, q_offsets, block_tables, seq_l
     q_offsets (n_req + 1,), block_tables (n_req, max_blocks) and seq_lens
     (n_req,) int32 on the pool's device, the lengths counted with the new
     tokens."""
-    n_req = _check_ragged(pool, q_offsets, block_tables, seq_lens)
-    h, d, e, dtype = pool.kv_heads, pool.head_dim, pool.elem_bytes, pool.tensors[0].dtype
-    ks = _token_stride(k, "k", h, d, dtype, pool.device)
-    vs = _token_stride(v, "v", h, d, dtype, pool.device)
-    n = k.shape[0]
+    n_req, max_blocks = _check_ragged(pool, q_offsets, block_tables, seq_lens)
+    h, d, e, dtype = pool.kv_heads, pool.head_dim, pool.elem_bytes, pool.dtype
+    shape = k.shape
+    ks = _token_stride(k, shape, "k", h, d, dtype, pool)
+    vs = _token_stride(v, v.shape, "v", h, d, dtype, pool)
+    n = shape[0]
     if v.shape[0] != n:
         raise ValueError(f"{n} tokens of K and {v.shape[0]} of V")
     _on_pool_device(pool, stream, "flowkv_append", _lib.flowkv_append, layer, k.data_ptr(), ks * e,
                     v.data_ptr(), vs * e, h * d * e, n, n_req, q_offsets.data_ptr(),
-                    block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr())
+                    block_tables.data_ptr(), max_blocks, seq_lens.data_ptr())
 
 
 def flowkv_chunk_attention_workspace(n_tokens: int, n_req: int, q_heads: int, kv_heads: int,
@@ -822,28 +830,36 @@ def flowkv_chunk_attention(pool: KVPool, layer: int, q, q_offsets, block_tables,
     that is 0)."""
     import torch
 
-    n_req = _check_ragged(pool, q_offsets, block_tables, seq_lens)
-    if pool.tensors[0].dtype is not torch.bfloat16:      # (a pool's tensors have one type)
-        raise ValueError(f"attention reads bfloat16 K/V: the pool holds {pool.tensors[0].dtype}")
-    if q.dim() != 3:
-        raise ValueError(f"q: need (tokens, heads, head_dim), got {tuple(q.shape)}")
-    n, hq, dh = q.shape
+    n_req, max_blocks = _check_ragged(pool, q_offsets, block_tables, seq_lens)
+    bf16, shape = torch.bfloat16, q.shape
+    if pool.dtype is not bf16:
+        raise ValueError(f"attention reads bfloat16 K/V: the pool holds {pool.dtype}")
+    if len(shape) != 3:
+        raise ValueError(f"q: need (tokens, heads, head_dim), got {tuple(shape)}")
+    n, hq, dh = shape
     if dh != pool.head_dim:
         raise ValueError(f"q has a head_dim of {dh}, the pool of {pool.head_dim}")
-    qs = _token_stride(q, "q", hq, dh, torch.bfloat16, pool.device)
-    if out.shape != q.shape or out.dtype is not torch.bfloat16 or not out.is_contiguous() \
-            or out.device != pool.device:
+    qs = _token_stride(q, shape, "q", hq, dh, bf16, pool)
+    if out.shape != shape or out.dtype is not bf16 or not out.is_contiguous() \
+            or out.get_device() != pool.index:
         raise ValueError(f"out: need contiguous {(n, hq, dh)} bfloat16 on {pool.device}, got "
                          f"{tuple(out.shape)} {out.dtype} on {out.device}")
     ws, ws_bytes = 0, 0
     if workspace is not None:
-        if not workspace.is_contiguous() or workspace.device != pool.device:
+        if not workspace.is_contiguous() or workspace.get_device() != pool.index:
             raise ValueError("attention workspace: not a contiguous tensor on the pool's device")
-        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        ws, ws_bytes = workspace.data_ptr(), workspace.nbytes
     _on_pool_device(pool, stream, "flowkv_chunk_attention", _lib.flowkv_chunk_attention, layer,
                     q.data_ptr(), qs, n, n_req, hq, pool.kv_heads, dh, q_offsets.data_ptr(),
-                    block_tables.data_ptr(), block_tables.shape[1], seq_lens.data_ptr(), max_new,
+                    block_tables.data_ptr(), max_blocks, seq_lens.data_ptr(), max_new,
                     max_seq_len, scale, split_tokens, out.data_ptr(), ws, ws_bytes)
+
+
+def _address(a: np.ndarray) -> int:
+    """The array's address by its buffer, where it can be written (0.3 us; 1.1 by _ptr)."""
+    if a.size and a.flags.writeable:
+        return ctypes.addressof(ctypes.c_char.from_buffer(a))
+    return _ptr(a)
 
 
 def flowkv_copy_blocks(pool: KVPool, src_ids, dst_ids, tokens=None, stream=None) -> None:
@@ -854,8 +870,8 @@ def flowkv_copy_blocks(pool: KVPool, src_ids, dst_ids, tokens=None, stream=None)
     k = None if tokens is None else _i32(tokens)
     if s.ndim != 1 or d.shape != s.shape or (k is not None and k.shape != s.shape):
         raise ValueError("source, destination and token lists differ in length")
-    _on_pool_device(pool, stream, "flowkv_copy_blocks", _lib.flowkv_copy_blocks, _ptr(s), _ptr(d),
-                    None if k is None else _ptr(k), s.size,
+    _on_pool_device(pool, stream, "flowkv_copy_blocks", _lib.flowkv_copy_blocks, _address(s),
+                    _address(d), None if k is None else _address(k), s.size,
                     pool.kv_heads * pool.head_dim * pool.elem_bytes)
 
 

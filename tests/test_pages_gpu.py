@@ -193,6 +193,20 @@ def test_copies_too_large_for_the_caches(layout, shape, tokens):
     assert same(pool.tensors, want)
 
 
+def test_copy_blocks_by_lists_arrays_and_read_only_arrays():
+    geom = Geometry("copylists", 2, 2, 64, 16, "bfloat16")
+    pool = fk.KVPool(BM, make_device_pool(geom, BM, 20, "cuda", 2))
+    want = [t.clone() for t in pool.tensors]
+    fixed = np.array([5, 9], np.int32)
+    fixed.flags.writeable = False
+    for src, dst, tok in (([1, 2], [3, 4], None), (fixed, (10, 11), [4, 16]),
+                          (np.array([12, 99, 13], np.int64)[::2], fixed, np.array([0, 7]))):
+        copy_plain(want, BM, src, dst, tok, 16)
+        fk.flowkv_copy_blocks(pool, src, dst, tok)
+    torch.cuda.synchronize()
+    assert same(pool.tensors, want)
+
+
 def test_copy_blocks_of_2_mib_far_apart():
     geom = Geometry("copyfar", 32, 8, 128, 16, "bfloat16")
     for layout in (BM, LM):
@@ -238,6 +252,7 @@ def test_refused_by_the_binding():
         with pytest.raises(ValueError):
             fk.flowkv_copy_blocks(b.pool, src, dst, tok)
     fk.flowkv_copy_blocks(b.pool, [], [])
+    fk.flowkv_copy_blocks(b.pool, np.zeros(0, np.int32), np.zeros(0, np.int32), [])
     torch.cuda.synchronize()
     assert torch.equal(b.pool.tensors[0], before)
 
