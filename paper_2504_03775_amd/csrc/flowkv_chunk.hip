@@ -429,8 +429,8 @@ __device__ __forceinline__ float pieces_of(float steps, float inv) {
 }
 
 // The workspace of a call in pieces: a record a piece, its rows as the waves hold them:
-// register 4 j + i of lane l of dim block b at (j * 64 + l) * 4 + i; then the rows' (reference, sum); then
-// Cut::first.
+// register 4 j + i of lane l of dim block b at (j * 64 + l) * 4 + i; then the rows'
+// (reference, sum); then the pieces of one KV head before each tile slot.
 template <class F>
 __device__ __forceinline__ float* piece_sums(const ChunkArgs& a, int64_t rec, int rw, int b) {
   return a.ws + ((rec * F::kRw + rw) * (F::kDh / 32) + b) * 1024;
@@ -643,7 +643,7 @@ void chunk_attn(const ChunkArgs a) {
 #pragma unroll
   for (int i = 0; i < W::kI; ++i) {
     u32x4 x = {0, 0, 0, 0};
-    if (live) x = *(cgvec4*)(a.q + token * a.q_stride + head * kDh + 16 * i + 8 * half);
+    if (live) x = *(cgvec4*)(a.q + token * a.q_stride + int64_t(head) * kDh + 16 * i + 8 * half);
     w.q[i] = __builtin_bit_cast(bf16x8, x);
   }
 #pragma unroll
@@ -1079,7 +1079,8 @@ void chunk_attn_few(const ChunkArgs a) {
         s[c][gg] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < kI; ++i)
-          s[c][gg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[gg][i], qb[c][i], s[c][gg], 0, 0, 0);
+          s[c][gg] =
+              __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka[gg][i], qb[c][i], s[c][gg], 0, 0, 0);
       }
     __builtin_amdgcn_sched_barrier(0);
     load_k(next);

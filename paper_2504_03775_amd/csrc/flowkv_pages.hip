@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kStreamThreads) void kv_block_stream(const A a) {
   } else {
     const uint32_t i = uint32_t(uint64_t(u) * uint64_t(a.perm_mul) % uint32_t(a.n));
     const uint32_t chunk =
-        kTokens ? uint32_t(tokens_of(a.rec[i])) * uint32_t(a.slot_pieces) : uint32_t(a.chunk_pieces);
+        uint32_t(kTokens ? tokens_of(a.rec[i]) * a.slot_pieces : a.chunk_pieces);
     if (o >= chunk * 2u * uint32_t(a.num_layers)) return;
     int64_t off = int64_t(o) * 16;
     if constexpr (kTokens) off = int64_t(o / chunk) * a.chunk_bytes + int64_t(o % chunk) * 16;
@@ -328,7 +328,8 @@ extern "C" int flowkv_append(const flowkv_pool* pool, int32_t layer, const void*
                 (long long)slot_bytes);
   void* args[] = {&a};
   hipError_t e = hipLaunchKernel(
-      few ? reinterpret_cast<const void*>(kv_append<1>) : reinterpret_cast<const void*>(kv_append<2>),
+      few ? reinterpret_cast<const void*>(kv_append<1>)
+          : reinterpret_cast<const void*>(kv_append<2>),
       dim3(unsigned(groups)), dim3(kAppendThreads), args, 0, static_cast<hipStream_t>(hip_stream));
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess) return fail(FLOWKV_EHIP, "append launch: %s", hipGetErrorString(e));

@@ -437,6 +437,43 @@ def test_pieces_in_a_replayed_graph_and_on_two_streams():
         assert torch.equal(out[1][:int(b.off[-1])], once[:int(b.off[-1])])
 
 
+@pytest.mark.parametrize("max_len,split", [(LONGEST, 0), (4000, 128), (4000, 0)])
+def test_two_graphs_share_a_workspace(max_len, split):
+    """Replayed in turn on one stream, with eager work between: each call writes all of the
+    workspace that it reads."""
+    geom = Geometry("sharedws", 1, 2, 128, 16, "bfloat16")
+    runs, need = [], 0
+    for k, (new, total) in enumerate((([90, 1, 7], [300, 2000, 7]), ([2, 64], [3900, 64]))):
+        b = Batch(geom, BM, new, total, 40 + k)
+        q = queries(b, 8, 40 + k)
+        runs.append((b, q, torch.zeros_like(q)))
+        need = max(need, fk.flowkv_chunk_attention_workspace(b.n_tokens, len(new), 8, 2, 128,
+                                                             b.max_new, max_len, split))
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+
+    def call(k):
+        b, q, out = runs[k]
+        fk.flowkv_chunk_attention(b.pool, 0, q, *b.args(), b.max_new, max_len, 0.09, out, ws, split)
+
+    graphs, want = [], []
+    for k in range(2):
+        call(k)
+        torch.cuda.synchronize()
+        check_attention(runs[k][0], 0, runs[k][1], 0.09, runs[k][2], max_seq=max_len)
+        want.append(runs[k][2].clone())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[k]):
+            call(k)
+    for i in range(6):
+        k = i % 2
+        runs[k][2].fill_(float("nan"))
+        graphs[k].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(runs[k][2], want[k])
+        if i % 3 == 2:
+            ws.fill_(255)
+
+
 def test_refused_by_the_binding():
     geom = Geometry("chunkref", 2, 2, 64, 16, "bfloat16")
     b = Batch(geom, BM, [4, 3], [40, 30], 18)
