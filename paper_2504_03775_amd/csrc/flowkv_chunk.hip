@@ -365,6 +365,10 @@ struct Source {
     return uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(d >> 32)))) << 32 |
            uint32_t(__builtin_amdgcn_readfirstlane(int(d)));
   }
+  // whether token x, counted from s0, is not one of the pool: behind s1, or in a missing block
+  __device__ __forceinline__ bool lost(int32_t x) const {
+    return x >= s1 - s0 || (places->dead[x / 64 % (2 * F::kWaves)] >> (x % 64) & 1);
+  }
   // The lane's places of step i.
   __device__ __forceinline__ void look(int i) {
 #pragma unroll
@@ -686,6 +690,11 @@ void chunk_attn(const ChunkArgs a) {
     odd_from = std::min(odd_from, t0);
 #pragma unroll
     for (int e = 0; e < F::kLd; ++e) {
+      // (what lies at the place of a row that does not exist counts for nothing)
+      if (src.lost(t0 - s0 + int32_t(src.row) + e * F::kLdRows)) {
+        v[e * F::kThreads + tid] = u32x4{0, 0, 0, 0};
+        continue;
+      }
       u32x4 x = v[e * F::kThreads + tid];
       bool any = false;
 #pragma unroll

@@ -1,0 +1,75 @@
+"""What infinities and NaN in V cost attention of new tokens (GPU): nothing where no row sees
+them, and no scan of all that is cached where rows do."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2504_03775_amd import flowkv as fk
+from workloads import Geometry
+from tests.gpu_helpers import BM, LM
+from tests.paged_batch import Batch
+from tests.test_chunk_attention_gpu import queries, say
+
+pytestmark = pytest.mark.gpu
+
+
+def prepared(b, q, split, max_len=None):
+    """A call of layer 0 as a function, and its output."""
+    max_len = b.max_len if max_len is None else max_len
+    need = fk.flowkv_chunk_attention_workspace(b.n_tokens, len(b.new), q.shape[1], b.geom.kv_heads,
+                                               b.geom.head_dim, b.max_new, max_len, split)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+    out = torch.zeros(q.shape, dtype=torch.bfloat16, device="cuda")
+
+    def call():
+        fk.flowkv_chunk_attention(b.pool, 0, q, *b.args(), b.max_new, max_len, 0.09, out, ws, split)
+    return call, out
+
+
+def microseconds(call, calls=5, tries=7):
+    """The least of `tries` times of a call among others."""
+    best = float("inf")
+    for _ in range(tries):
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        begin.record()
+        for _ in range(calls):
+            call()
+        end.record()
+        torch.cuda.synchronize()
+        best = min(best, begin.elapsed_time(end) / calls * 1e3)
+    return best
+
+
+def leave_block_0_unused(b):
+    spare = np.setdiff1d(np.arange(1, b.blocks), b.tab)[0]
+    b.tab[b.tab == 0] = spare
+    b.upload()
+
+
+@pytest.mark.parametrize("d,layout,new,total,split", [
+    (128, BM, [300, 40], [1500, 1000], 0), (128, LM, [2100, 700], [2100, 1333], 1 << 20),
+    (64, LM, [1100, 300], [1100, 1333], 1 << 20), (64, BM, [300, 40], [9000, 777], 0),
+    (128, BM, [3, 1], [1500, 777], 0),
+])
+def test_a_bad_value_in_the_pools_first_row_costs_nothing(d, layout, new, total, split):
+    """Rows that do not exist (behind a length, in a block outside the pool) are read as some
+    row of the pool: what that one holds reaches no result and starts no search."""
+    b = Batch(Geometry("oddfirst", 1, 8, d, 16, "bfloat16"), layout, new, total, 50)
+    leave_block_0_unused(b)
+    b.tab[1, 3] = b.blocks + 5
+    b.upload()
+    q = queries(b, 16, 50)
+    call, out = prepared(b, q, split)
+    view = b.layer_view(0)
+    view[:, 0] = 0
+    call()
+    before = microseconds(call)
+    want = out.clone()
+    view[:, 0] = float("nan")
+    out.fill_(7)
+    call()
+    after = microseconds(call)
+    say(f"  {before:.1f} us, {after:.1f} with a NaN in block 0")
+    assert torch.equal(out, want)
+    assert after < 1.5 * before + 3
