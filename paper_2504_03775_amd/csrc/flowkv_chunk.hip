@@ -131,6 +131,20 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
 }
 
+// Takes infinities and NaN out of two bf16; whether there was one.
+__device__ __forceinline__ bool tame(uint32_t& w) {
+  bool any = false;
+  if ((w & 0x7f80u) == 0x7f80u) {
+    w &= 0xffff0000u;
+    any = true;
+  }
+  if ((w & 0x7f800000u) == 0x7f800000u) {
+    w &= 0xffffu;
+    any = true;
+  }
+  return any;
+}
+
 // What the parts of one row weigh when they are joined under reference m: a part that saw
 // no token has a reference of -inf and a sum of 0 (one whose scores are all NaN has a sum
 // of NaN, which stays).
@@ -321,6 +335,7 @@ template <class F>
 struct Places {
   uint32_t at[2 * F::kThreads];
   uint64_t dead[2 * F::kWaves];
+  int32_t odd_from;                              // first token whose V lost a value, below
 };
 
 template <class F>
@@ -681,35 +696,27 @@ void chunk_attn(const ChunkArgs a) {
 
   // Where some row does not see some token, or a block is missing, an infinity or a NaN
   // in V would reach a row as 0 x inf: such values are taken out of the step's rows by the
-  // lanes that brought them, and added at the end to the rows that see them.
-  bool odd = false, suspect = false;             // suspect: a block is missing somewhere so far
-  int32_t odd_from = s1;
+  // lanes that brought them, and added at the end to the rows that see them.  (What lies at
+  // the place of a row that does not exist counts for nothing.)
+  bool suspect = false;                          // a block is missing somewhere so far
   auto landed = [&](lvec* v, int32_t t0) {
     __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
     if (__builtin_expect(t0 + kStep <= tile_least && !suspect, 1)) return;
-    odd_from = std::min(odd_from, t0);
 #pragma unroll
     for (int e = 0; e < F::kLd; ++e) {
-      // (what lies at the place of a row that does not exist counts for nothing)
-      if (src.lost(t0 - s0 + int32_t(src.row) + e * F::kLdRows)) {
-        v[e * F::kThreads + tid] = u32x4{0, 0, 0, 0};
-        continue;
-      }
+      const int32_t t = t0 + int32_t(src.row) + e * F::kLdRows;
       u32x4 x = v[e * F::kThreads + tid];
       bool any = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if ((x[i] & 0x7f80u) == 0x7f80u) {
-          x[i] &= 0xffff0000u;
-          any = true;
-        }
-        if ((x[i] & 0x7f800000u) == 0x7f800000u) {
-          x[i] &= 0xffffu;
-          any = true;
-        }
+        uint32_t y = x[i];
+        any |= tame(y);
+        x[i] = y;
       }
-      if (any) v[e * F::kThreads + tid] = x;
-      odd |= any;
+      if (any) {
+        v[e * F::kThreads + tid] = x;
+        if (!src.lost(t - s0)) atomicMin(&places.odd_from, t);
+      }
     }
   };
 
@@ -740,6 +747,7 @@ void chunk_attn(const ChunkArgs a) {
                 *const v1 = (lvec*)sv1;
     src.fetch(0);
     src.place(0);
+    if (tid == 0) places.odd_from = s1;
     __syncthreads();
     suspect = src.any_dead(0);
     src.look(0);
@@ -756,7 +764,7 @@ void chunk_attn(const ChunkArgs a) {
   const ChunkArgs e = late_args();
   const int lane = int(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)));
   const int hi = lane >> 5;
-  const bool had_odd = __syncthreads_or(odd);
+  const int32_t odd_from = s0 < s1 ? uniform(places.odd_from) : s1;
   float lsum = w.lsum + __shfl_xor(w.lsum, 32);
   float mref = w.mref;
   if constexpr (F::kKw > 1) {
@@ -797,7 +805,7 @@ void chunk_attn(const ChunkArgs a) {
     }
     if (kw > 0) return;
   }
-  if (had_odd) {
+  if (odd_from < s1) {
     for (int32_t t = odd_from; t < s1; ++t) {
       const int32_t b = src.table[t / e.block_size];
       if (b < 0 || b >= e.pool_blocks) continue;
@@ -944,20 +952,6 @@ __device__ __forceinline__ uint32_t pair_hi(uint32_t lo, uint32_t hi) {
 }
 __device__ __forceinline__ uint32_t pair_lo(uint32_t lo, uint32_t hi) {
   return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
-}
-
-// Takes infinities and NaN out of two bf16; whether there was one.
-__device__ __forceinline__ bool tame(uint32_t& w) {
-  bool any = false;
-  if ((w & 0x7f80u) == 0x7f80u) {
-    w &= 0xffff0000u;
-    any = true;
-  }
-  if ((w & 0x7f800000u) == 0x7f800000u) {
-    w &= 0xffffu;
-    any = true;
-  }
-  return any;
 }
 
 template <int kDh, int kC>
