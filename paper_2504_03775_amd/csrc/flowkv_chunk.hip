@@ -23,6 +23,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(1))) const u32x4 cgvec4;
+typedef __attribute__((address_space(1))) const u32x2 cgvec2;
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -335,7 +336,7 @@ template <class F>
 struct Places {
   uint32_t at[2 * F::kThreads];
   uint64_t dead[2 * F::kWaves];
-  int32_t odd_from;                              // first token whose V lost a value, below
+  uint32_t odd[2];                               // where V lost a value: a bit per 64th, below
 };
 
 template <class F>
@@ -697,8 +698,12 @@ void chunk_attn(const ChunkArgs a) {
   // Where some row does not see some token, or a block is missing, an infinity or a NaN
   // in V would reach a row as 0 x inf: such values are taken out of the step's rows by the
   // lanes that brought them, and added at the end to the rows that see them.  (What lies at
-  // the place of a row that does not exist counts for nothing.)
-  bool suspect = false;                          // a block is missing somewhere so far
+  // the place of a row that does not exist counts for nothing.)  Which 64ths of the
+  // workgroup's tokens, 2^odd_shift each, such values were in, is kept: the end looks
+  // through those alone.
+  auto odd_shift = [&] { return std::max(0, 26 - __builtin_clz((s1 - s0 - 1) | 1)); };
+  bool next_dead = false, suspect = false;       // a block is missing in the next group of
+                                                 // steps; in it or in this one
   auto landed = [&](lvec* v, int32_t t0) {
     __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
     if (__builtin_expect(t0 + kStep <= tile_least && !suspect, 1)) return;
@@ -715,7 +720,8 @@ void chunk_attn(const ChunkArgs a) {
       }
       if (any) {
         v[e * F::kThreads + tid] = x;
-        if (!src.lost(t - s0)) atomicMin(&places.odd_from, t);
+        const int bit = (t - s0) >> odd_shift();
+        if (!src.lost(t - s0)) atomicOr(&places.odd[bit >> 5], 1u << (bit & 31));
       }
     }
   };
@@ -740,16 +746,20 @@ void chunk_attn(const ChunkArgs a) {
       if (find) src.place(i / F::kGroup + 1);
       if (more) landed(v_to, t0 + kStep);
       __syncthreads();
-      if (find) suspect |= src.any_dead(i / F::kGroup + 1);
+      if (find) {
+        suspect = next_dead;
+        next_dead = src.any_dead(i / F::kGroup + 1);
+        suspect |= next_dead;
+      }
       ++i;
     };
     lvec *const k0 = (lvec*)sk0, *const k1 = (lvec*)sk1, *const v0 = (lvec*)sv0,
                 *const v1 = (lvec*)sv1;
     src.fetch(0);
     src.place(0);
-    if (tid == 0) places.odd_from = s1;
+    if (tid < 2) places.odd[tid] = 0;
     __syncthreads();
-    suspect = src.any_dead(0);
+    suspect = next_dead = src.any_dead(0);
     src.look(0);
     src.send(k0, v0);
     src.look(1);
@@ -764,7 +774,10 @@ void chunk_attn(const ChunkArgs a) {
   const ChunkArgs e = late_args();
   const int lane = int(__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)));
   const int hi = lane >> 5;
-  const int32_t odd_from = s0 < s1 ? uniform(places.odd_from) : s1;
+  uint64_t odd = 0;
+  if (s0 < s1)
+    odd = uint64_t(uint32_t(uniform(int32_t(places.odd[1])))) << 32 |
+          uint32_t(uniform(int32_t(places.odd[0])));
   float lsum = w.lsum + __shfl_xor(w.lsum, 32);
   float mref = w.mref;
   if constexpr (F::kKw > 1) {
@@ -805,21 +818,54 @@ void chunk_attn(const ChunkArgs a) {
     }
     if (kw > 0) return;
   }
-  if (odd_from < s1) {
-    for (int32_t t = odd_from; t < s1; ++t) {
-      const int32_t b = src.table[t / e.block_size];
-      if (b < 0 || b >= e.pool_blocks) continue;
-      const char* v = src.base + e.voff +
-                      (int64_t(b) * e.bunits + int64_t(t % e.block_size) * e.sunits) * 128;
+  // the rows of V of the marked 64ths, 64 pieces of 16 bytes at a time
+  for (; odd; odd &= odd - 1) {
+    constexpr int kPer = 64 / kPc;
+    const int32_t from = s0 + (__builtin_ctzll(odd) << odd_shift());
+    const int32_t to = std::min(s1 - from, 1 << odd_shift()) + from;
+    for (int32_t t0 = from; t0 < to; t0 += kPer) {
+      const int32_t t = t0 + lane / kPc;
+      const int32_t blk = src.table[(t < to ? t : from) / e.block_size];
+      uint32_t at = 0;                           // in 128-byte units, as in the loop
+      bool any = false;
+      if (t < to && blk >= 0 && blk < e.pool_blocks) {
+        at = uint32_t(blk) * e.bunits + uint32_t(t % e.block_size) * e.sunits;
+        const u32x4 x = *(cgvec4*)(src.base + e.voff + uint64_t(at) * 128 + lane % kPc * 16);
 #pragma unroll
-      for (int b = 0; b < kB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t y = uint32_t(reinterpret_cast<const uint16_t*>(
-                                 v)[32 * b + 8 * (i / 4) + 4 * hi + i % 4])
-                             << 16;
-          if ((y & 0x7f800000u) == 0x7f800000u && t < w.lim) w.o[b][i] += __uint_as_float(y);
+        for (int i = 0; i < 4; ++i) {
+          uint32_t y = x[i];
+          any |= tame(y);
         }
+      }
+      for (uint64_t hit = __ballot(any); hit;) { // a token with such a value
+        const int x = __builtin_ctzll(hit) / kPc;
+        hit &= ~(((uint64_t(1) << kPc) - 1) << (x * kPc));
+        const char* v = src.base + e.voff +
+                        uint64_t(uint32_t(__builtin_amdgcn_readlane(int(at), x * kPc))) * 128;
+        const bool sees = t0 + x < w.lim;
+        bool full = true;                        // with NaN, which stays
+#pragma unroll
+        for (int b = 0; b < kB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) full &= w.o[b][i] != w.o[b][i];
+        if (!__any(sees && !full)) {             // (later tokens are seen by no other rows)
+          odd = 0;
+          t0 = to;
+          break;
+        }
+#pragma unroll
+        for (int b = 0; b < kB; ++b)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const u32x2 y = *(cgvec2*)(v + (32 * b + 8 * j + 4 * hi) * 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t z = i % 2 ? y[i / 2] & 0xffff0000u : y[i / 2] << 16;
+              if (sees && (z & 0x7f800000u) == 0x7f800000u)
+                w.o[b][4 * j + i] += __uint_as_float(z);
+            }
+          }
+      }
     }
   }
   if (kCut && !direct && any_row) {
@@ -942,9 +988,10 @@ struct FewLds {
   // K's staging, a tile per wave; after the loop the waves' weighted sums
   alignas(16) uint8_t area[kFewWaves * kRows * kDh * sizeof(float)];
   uint32_t dead[kFewSplit / kFewTile];
+  uint32_t odd[2];                         // tiles whose V lost an infinity or a NaN
   float m[kFewWaves][kRows], l[kFewWaves][kRows];
   int32_t lim[kRows];
-  static_assert(kFewWaves * kFewTile * kDh * 2 <= sizeof(area));
+  static_assert(kFewWaves * kFewTile * kDh * 2 <= sizeof(area) && kFewSplit / kFewTile <= 64);
 };
 
 __device__ __forceinline__ uint32_t pair_hi(uint32_t lo, uint32_t hi) {
@@ -1030,7 +1077,7 @@ void chunk_attn_few(const ChunkArgs a) {
 #pragma unroll
     for (int t = 0; t < kT; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  bool odd = false;
+  if (tid < 2) lds.odd[tid] = 0;
   __syncthreads();
 
   u32x4 kw[kKL];
@@ -1129,6 +1176,7 @@ void chunk_attn_few(const ChunkArgs a) {
       }
     }
     if (masked) {                                // 0 x inf is not 0
+      bool odd = false;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (dead >> (4 * e) & 1) vw[e] = VT{};
@@ -1139,6 +1187,7 @@ void chunk_attn_few(const ChunkArgs a) {
           vw[e][i] = x;
         }
       }
+      if (odd) atomicOr(&lds.odd[tile >> 5], 1u << (tile & 31));
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -1170,7 +1219,9 @@ void chunk_attn_few(const ChunkArgs a) {
       lds.l[wave][16 * c + c16] = lsum[c];
     }
   }
-  const bool had_odd = __syncthreads_or(odd);    // every wave is past the loop: the area is free
+  __syncthreads();                               // every wave is past the loop: the area is free
+  const uint64_t odd = uint64_t(uint32_t(uniform(int32_t(lds.odd[1])))) << 32 |
+                       uint32_t(uniform(int32_t(lds.odd[0])));
   float* const s_o = reinterpret_cast<float*>(lds.area);   // [wave][row][dim]
 #pragma unroll
   for (int c = 0; c < kC; ++c)
@@ -1196,17 +1247,21 @@ void chunk_attn_few(const ChunkArgs a) {
       L += lds.l[w][h] * wt;
       A += *reinterpret_cast<const f32x4*>(&s_o[(w * kFewRows + h) * kDh + d]) * wt;
     }
-    if (had_odd) {
-      for (int32_t t = s0; t < s1; ++t) {
-        const int32_t b = table[t / a.block_size];
-        if (b < 0 || b >= a.pool_blocks || t >= lds.lim[h]) continue;
-        const uint16_t* v = reinterpret_cast<const uint16_t*>(
-            a.kbase + a.voff + g * kDh * 2 +
-            (int64_t(b) * a.bunits + int64_t(t % a.block_size) * a.sunits) * 128);
+    // infinities and NaN of the tokens that the row sees, until it is all NaN
+    for (uint64_t left = odd; left; left &= left - 1) {
+      const int tile = __builtin_ctzll(left);
+      const int32_t sees = lds.lim[h] - s0 - tile * kFewTile;
+      if (sees <= 0 || (A[0] != A[0] && A[1] != A[1] && A[2] != A[2] && A[3] != A[3])) break;
+      const uint32_t gone = lds.dead[tile];
+#pragma unroll 8
+      for (int x = 0; x < kFewTile; ++x) {
+        const u32x2 y = *(cgvec2*)(a.kbase + a.voff + (g * kDh + d) * 2 +
+                                   uint64_t(lds.at[tile * kFewTile + (x & 3) * 8 + (x >> 2)]) * 128);
+        if (x >= sees || (gone >> x & 1)) continue;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t y = uint32_t(v[d + k]) << 16;
-          if ((y & 0x7f800000u) == 0x7f800000u) A[k] += __uint_as_float(y);
+          const uint32_t z = k % 2 ? y[k / 2] & 0xffff0000u : y[k / 2] << 16;
+          if ((z & 0x7f800000u) == 0x7f800000u) A[k] += __uint_as_float(z);
         }
       }
     }

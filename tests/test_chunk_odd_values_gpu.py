@@ -73,3 +73,62 @@ def test_a_bad_value_in_the_pools_first_row_costs_nothing(d, layout, new, total,
     say(f"  {before:.1f} us, {after:.1f} with a NaN in block 0")
     assert torch.equal(out, want)
     assert after < 1.5 * before + 3
+
+
+@pytest.mark.parametrize("d,layout,new,total,split", [
+    (128, BM, 200, 20000, 1 << 20), (64, LM, 200, 20000, 1 << 20), (128, LM, 200, 20000, 0),
+    (64, BM, 200, 20000, 0), (128, LM, 3, 20000, 0),
+])
+@pytest.mark.parametrize("at", [[40], [40, 15000], [15000, 19900]])
+def test_seen_infinities_behind_a_missing_block_are_not_searched_for_token_by_token(
+        d, layout, new, total, split, at):
+    """A block is missing early in a long request, and tokens behind it hold infinities that
+    every row sees: the call takes not much longer than without them."""
+    b = Batch(Geometry("oddlong", 1, 2, d, 16, "bfloat16"), layout, [new], [total], 51)
+    b.tab[0, 1] = -1                                        # tokens 16 to 31
+    b.upload()
+    q = queries(b, 8, 51)
+    call, out = prepared(b, q, split, max_len=400_000)
+    call()
+    before = microseconds(call)
+    ref = out.clone()
+    view = b.layer_view(0)
+    for i, p in enumerate(at):
+        view[1, int(b.tab[0, p // 16]), p % 16, :, 3 + i] = float("inf")
+    out.fill_(7)
+    call()
+    after = microseconds(call)
+    say(f"  {before:.1f} us, {after:.1f} with infinities at {at}")
+    sees = torch.as_tensor(total - new + np.arange(new)[:, None] >= np.asarray(at), device="cuda")
+    for i in range(len(at)):
+        got = out[:, :, 3 + i].float()
+        assert (got[sees[:, i]] == float("inf")).all()
+        assert torch.equal(out[:, :, 3 + i][~sees[:, i]], ref[:, :, 3 + i][~sees[:, i]])
+    rest = [i for i in range(d) if not 3 <= i < 3 + len(at)]
+    assert torch.equal(out[:, :, rest], ref[:, :, rest])
+    assert after < 1.5 * before + 10
+
+
+@pytest.mark.parametrize("d,layout,new,total,split", [
+    (128, BM, 600, 4000, 0), (64, LM, 600, 4000, 0), (128, LM, 3, 8000, 0), (64, BM, 8, 8000, 2048),
+    (128, LM, 2000, 2000, 0),
+])
+def test_a_request_of_nan_costs_little_more(d, layout, new, total, split):
+    """All new tokens of one request are NaN, as a diverged layer leaves them: the others of
+    the batch do not wait for it."""
+    b = Batch(Geometry("oddnan", 1, 2, d, 16, "bfloat16"), layout, [new, new], [total, total], 52)
+    q = queries(b, 8, 52)
+    call, out = prepared(b, q, split)
+    call()
+    before = microseconds(call)
+    ref = out.clone()
+    view = b.layer_view(0)
+    for p in range(total - new, total):
+        view[:, int(b.tab[0, p // 16]), p % 16] = float("nan")
+    out.fill_(7)
+    call()
+    after = microseconds(call)
+    say(f"  {before:.1f} us, {after:.1f} with NaN")
+    assert torch.isnan(out[:new].float()).all()
+    assert torch.equal(out[new:], ref[new:])
+    assert after < 1.5 * before + 10
