@@ -505,10 +505,12 @@ int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, const void* q
 
 /* Workspace bytes of flowkv_chunk_attention for these arguments.  With
    split_tokens 0 where it covers max_seq_len, else n_tokens x q_heads x
-   ceil(max_seq_len / split_tokens) x (head_dim + 2) floats; with 0, the
-   library's rule, no more than 34 MB where requests bring many tokens (0 for
-   the most part), and as above, of at most 2,048 tokens a split, where they
-   bring few. */
+   ceil(max_seq_len / split_tokens) x (head_dim + 2) floats, padding rows
+   counted.  With 0, the library's rule: where max_new x (q_heads / kv_heads) is
+   over 32, at most 34,080,772 bytes however much padding there is (0 for the
+   most part); where it is not, as above for a split of the library's own, a
+   multiple of 128 from 128 to 2,048 tokens.  EINVAL as for the call, and where
+   the size passes 2^63. */
 int flowkv_chunk_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q_heads,
                                      int32_t kv_heads, int32_t head_dim, int32_t max_new,
                                      int32_t max_seq_len, int32_t split_tokens, int64_t* bytes);

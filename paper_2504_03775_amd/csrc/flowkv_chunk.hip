@@ -474,21 +474,41 @@ __device__ __forceinline__ uint32_t paired() {
 }
 
 // Finds the workgroup's tile, or its piece of one, and the KV head; kPieceTiles lanes, one
-// to a tile slot.  The first workgroup leaves the pieces before each slot in the workspace.
+// to a tile slot (slots are counted from the first request's token here: rows before it,
+// or behind the last request, are padding and have none).  The first workgroup leaves the
+// pieces before each slot in the workspace.
 template <class F>
 __device__ __forceinline__ Mine cut_tiles(const ChunkArgs& a, Cut& c, int& g, int32_t& record) {
   static_assert(F::kThreads == kPieceTiles);
   const int tid = threadIdx.x, ln = tid & 63, wave = tid >> 6;
+  const int32_t first = a.offsets[0];
+  Mine mine;
+  mine.pieces = 0;
+  if ((int64_t(a.offsets[a.n_req]) - first) * a.group / F::kRows + a.n_req > a.tiles) {
+    // More rows than the host was told of (max_new): whole tiles, in the batch's order.
+    if (a.pieces && blockIdx.x == 0)
+      for (int32_t i = tid; i <= a.tiles; i += F::kThreads) piece_first<F>(a)[i] = 0;
+    g = int(blockIdx.x % uint32_t(a.kv_heads));
+    const int32_t slot = int32_t(blockIdx.x / uint32_t(a.kv_heads));
+    mine.rq = request_at(
+        a, flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); }));
+    const int64_t local = int64_t(slot) - first_tile(a, mine.rq.r);
+    if (local >= 0 && local * F::kRows < int64_t(mine.rq.n_new) * a.group) mine.pieces = 1;
+    mine.row0 = int32_t(local) * F::kRows;
+    mine.split = 0;
+    return mine;
+  }
+  const uint32_t id = a.pieces ? blockIdx.x : paired<F>();
+  if (id >= uint32_t(std::max(a.tiles * a.kv_heads, a.pieces))) return mine;   // (padding's)
   // (at most kPieceTiles x kRows rows: 32 bits hold what valid offsets give)
   if (tid < a.n_req)
-    c.start[tid] = int32_t(uint32_t(a.offsets[tid]) * uint32_t(a.group) / F::kRows) + tid;
+    c.start[tid] = int32_t(uint32_t(a.offsets[tid] - first) * uint32_t(a.group) / F::kRows) + tid;
   if (tid == 0) {
     c.length = INT32_MAX;
     c.mine.pieces = 0;
   }
   __syncthreads();
   int32_t n = 0;                                 // steps
-  Mine mine;
   if (tid < a.tiles) {
     int32_t r = 0, hi = a.n_req;
     while (hi - r > 1) {
@@ -509,7 +529,6 @@ __device__ __forceinline__ Mine cut_tiles(const ChunkArgs& a, Cut& c, int& g, in
     const uint32_t key = uint32_t(n) * kPieceTiles + uint32_t(tid);
     c.key[tid] = key;
     __syncthreads();
-    const uint32_t id = paired<F>();
     g = int(id % uint32_t(a.kv_heads));
     if (n > 0) {
       int32_t before = 0;
@@ -583,8 +602,8 @@ __device__ __forceinline__ Mine cut_tiles(const ChunkArgs& a, Cut& c, int& g, in
       total += c.part[0][w];
     }
     // an XCD's workgroups have pieces in a row
-    const int32_t x = int32_t(blockIdx.x) % 8, n8 = int32_t(gridDim.x) / 8;
-    record = x * n8 + std::min(x, int32_t(gridDim.x) % 8) + int32_t(blockIdx.x) / 8;
+    record = int32_t(id) < a.pieces ? int32_t(id) % 8 * (a.pieces / 8) + int32_t(id) / 8
+                                    : int32_t(id);
     if (record == 0) {
       if (tid == 0) piece_first<F>(a)[0] = 0;
       if (tid < a.tiles) piece_first<F>(a)[tid + 1] = sum;
@@ -916,10 +935,13 @@ __global__ __launch_bounds__(2 * F::kDh) void chunk_attn_join(const ChunkArgs a)
   const int32_t* first = piece_first<F>(a);
   const int32_t total = first[a.tiles], from = first[slot], to = first[slot + 1];
   if (to - from < 2) return;                     // written already
-  const int32_t r =
-      flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); });
+  const int32_t base = a.offsets[0];             // (as cut_tiles counts)
+  auto start = [&](int32_t i) {
+    return (int64_t(a.offsets[i] - base) * a.group >> a.row_shift) + i;
+  };
+  const int32_t r = flowkv::last_at_most(a.n_req, slot, start);
   const Request rq = request_at(a, r);
-  const int64_t row = (int64_t(slot) - first_tile(a, r)) * F::kRows + rw * 32 + c32;
+  const int64_t row = (int64_t(slot) - start(r)) * F::kRows + rw * 32 + c32;
   const bool live = row >= 0 && row < int64_t(rq.n_new) * a.group;
   if (!__any(live)) return;
   float m = -INFINITY, l = 0.f;
@@ -1415,12 +1437,18 @@ int64_t tiles_of(int64_t n_tokens, int64_t n_req, int group, int64_t max_new, in
                   tile_slots(n_tokens, n_req, group, rows));
 }
 
-// Whether the kernels that look at all lengths take a call: their tables' sizes, and
-// steps x kPieceTiles within 32 bits.
-bool by_lengths(int64_t n_tokens, int64_t n_req, int group, int64_t max_seq_len, const Kind& kind) {
-  const int64_t slots = tile_slots(n_tokens, n_req, group, kind.rows);
-  return slots <= kPieceTiles && n_req <= kPieceTiles &&
-         slots * ((max_seq_len + kind.step - 1) / kind.step) < 1 << 22;
+// The same without padding: of no more than max_new tokens a request.
+int64_t used_slots(int64_t n_tokens, int64_t n_req, int group, int64_t max_new, int rows) {
+  return tile_slots(std::min(n_tokens, n_req * max_new), n_req, group, rows);
+}
+
+// Whether the kernels that look at all lengths take a call: their tables' sizes, a tile's
+// steps x kPieceTiles and all steps within 31 bits.
+bool by_lengths(int64_t n_tokens, int64_t n_req, int group, int64_t max_new, int64_t max_seq_len,
+                const Kind& kind) {
+  const int64_t slots = used_slots(n_tokens, n_req, group, max_new, kind.rows);
+  const int64_t steps = (max_seq_len + kind.step - 1) / kind.step;
+  return slots <= kPieceTiles && steps < 1 << 22 && slots * steps < 1 << 30;
 }
 
 struct Shape {
@@ -1430,6 +1458,10 @@ struct Shape {
   int64_t need;
 };
 
+// The most workspace that the library's rule asks for where requests bring more than 32
+// rows: that of pieces, in which a batch's padding has no part.
+constexpr int64_t kRuleBytes =
+    int64_t(kCus) * 256 * (128 + 2) * sizeof(float) + (kPieceTiles + 1) * sizeof(float);
 
 // The split that ends soonest by a simple count: the CUs' rounds over all tiles' splits, each
 // as long as its tokens and `fixed` more (a workgroup's start and end), and the merge.  In
@@ -1482,52 +1514,80 @@ int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_head
   // 10.1; 30 behind 500, 32 of 128 on 8: 13.6 and 16.8; but 1,000 behind none, 8 on 1: 29.0
   // and 23.2.)
   const int64_t t32 = tiles_of(n_tokens, n_req, group, max_new, 32) * kv_heads;
-  const bool rule = split_tokens == 0;
+  const bool rule = split_tokens == 0, many = int64_t(max_new) * group > 32;
+  // records of even splits, past 63 bits: the most that 63 bits hold
+  auto splits_of = [&](int32_t split) {
+    return std::max<int64_t>((int64_t(max_seq_len) + split - 1) / split, 1);
+  };
+  auto bytes_of = [&](int32_t split) {
+    int64_t bytes = 0;
+    if (splits_of(split) > 1 &&                  // (fewer than 2^62 rows)
+        (__builtin_mul_overflow(int64_t(n_tokens) * q_heads,
+                                int64_t((head_dim + 2) * sizeof(float)), &bytes) ||
+         __builtin_mul_overflow(bytes, splits_of(split), &bytes)))
+      return INT64_MAX;
+    return bytes;
+  };
+  auto by_pieces = [&](int kind) {
+    out->kind = kind;
+    out->cut = true;
+    out->split = 0;
+    out->splits = 1;
+    out->pieces = kKinds[kind].per_cu[head_dim == 128] * kCus;
+    out->need = (int64_t(out->pieces) * kKinds[kind].rows * (head_dim + 2) +
+                 std::min<int64_t>(tile_slots(n_tokens, n_req, group, kKinds[kind].rows),
+                                   kPieceTiles) + 1) * int64_t(sizeof(float));
+    return FLOWKV_OK;
+  };
+  auto takes_lengths = [&](int kind) {
+    return by_lengths(n_tokens, n_req, group, max_new, max_seq_len, kKinds[kind]);
+  };
+  constexpr int32_t kAll = INT32_MAX / kSplitUnit * kSplitUnit;
+  const int cut_kind = head_dim == 128 ? 3 : 2;  // the form that has pieces
   out->cut = out->order = false;
-  if (split_tokens <= kFewSplit &&
-      (int64_t(max_new) * group <= 32 ||
-       (rule && t32 <= kCus && t32 * ((int64_t(max_seq_len) + 31) / 32) <= kFewSteps * kCus))) {
+  if (split_tokens <= kFewSplit && !many) {
     out->kind = int64_t(max_new) * group > 16;
+  } else if (rule && t32 <= kCus && t32 * ((int64_t(max_seq_len) + 31) / 32) <= kFewSteps * kCus &&
+             bytes_of(best_split(std::max<int64_t>(t32, 1), max_seq_len, 300, kFewSplit)) <=
+                 kRuleBytes) {
+    out->kind = 1;
   } else if (t256 >= kCus) {
     out->kind = 3;
   } else {
-    const int kind = head_dim == 128 ? 3 : 2;
-    const int64_t tiles = kind == 3 ? t256 : t128, step = kKinds[kind].step;
-    out->cut = rule && tiles < kCus &&
-               by_lengths(n_tokens, n_req, group, max_seq_len, kKinds[kind]) &&
-               tiles * ((max_seq_len + step - 1) / step) >= kCutSteps * kCus;
-    out->kind = out->cut ? kind : 2;
+    const int64_t tiles = cut_kind == 3 ? t256 : t128, step = kKinds[cut_kind].step;
+    if (rule && tiles < kCus && takes_lengths(cut_kind) &&
+        tiles * ((max_seq_len + step - 1) / step) >= kCutSteps * kCus)
+      return by_pieces(cut_kind);
+    out->kind = 2;
   }
   const Kind& kind = kKinds[out->kind];
-  if (rule && out->kind >= 2 && !out->cut)
-    out->order = n_req > 1 && max_seq_len / 2 >= max_new && (out->kind == 3 ? t256 : t128) > kCus &&
-                 by_lengths(n_tokens, n_req, group, max_seq_len, kind);
-  if (out->cut || out->order) {
+  if (rule && out->kind >= 2 && n_req > 1 && max_seq_len / 2 >= max_new &&
+      (out->kind == 3 ? t256 : t128) > kCus && takes_lengths(out->kind)) {
+    out->order = true;
     out->split = 0;
     out->splits = 1;
-    out->pieces = kind.per_cu[head_dim == 128] * kCus;
+    out->pieces = 0;
     out->need = 0;
-    if (out->cut)
-      out->need = (int64_t(out->pieces) * kind.rows * (head_dim + 2) +
-                   tile_slots(n_tokens, n_req, group, kind.rows) + 1) *
-                  int64_t(sizeof(float));
     return FLOWKV_OK;
   }
-  const int64_t tiles =
-      std::max<int64_t>(tiles_of(n_tokens, n_req, group, max_new, kind.rows) * kv_heads, 1);
-  constexpr int32_t kAll = INT32_MAX / kSplitUnit * kSplitUnit;
   if (rule) {
+    const int64_t tiles =
+        std::max<int64_t>(tiles_of(n_tokens, n_req, group, max_new, kind.rows) * kv_heads, 1);
     if (out->kind <= 1) split_tokens = best_split(tiles, max_seq_len, 300, kFewSplit);
     else split_tokens = tiles < kCus ? best_split(tiles, max_seq_len, 500, kAll) : kAll;
+    // padding and few steps, as a rule: pieces, or the splits that the workspace has room for
+    if (many && bytes_of(split_tokens) > kRuleBytes) {
+      if (takes_lengths(cut_kind)) return by_pieces(cut_kind);
+      while (split_tokens < kAll && bytes_of(split_tokens) > kRuleBytes)
+        split_tokens = split_tokens < kAll / 2 ? 2 * split_tokens : kAll;
+    }
   }
   out->split = split_tokens;
-  out->splits = int32_t((int64_t(max_seq_len) + split_tokens - 1) / split_tokens);
-  if (out->splits < 1) out->splits = 1;
-  out->need = 0;
-  const int64_t record = (head_dim + 2) * int64_t(sizeof(float));
-  if (out->splits > 1 &&                         // (fewer than 2^62 records)
-      (__builtin_mul_overflow(int64_t(n_tokens) * q_heads, record, &out->need) ||
-       __builtin_mul_overflow(out->need, int64_t(out->splits), &out->need)))
+  const int64_t splits = splits_of(split_tokens);
+  out->need = bytes_of(split_tokens);
+  out->splits = int32_t(splits);
+  out->pieces = 0;
+  if (out->need == INT64_MAX)
     return fail(FLOWKV_EINVAL, "%d splits: the workspace's size overflows", out->splits);
   return FLOWKV_OK;
 }
@@ -1647,7 +1707,9 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
     return fail(FLOWKV_EINVAL, "%lld tiles of queries x %d splits: too many for one call",
                 (long long)grid, sh.splits);
   a.tiles = int32_t(tiles);
-  a.pieces = sh.cut ? sh.pieces : 0;
+  if (sh.cut || sh.order)
+    a.tiles = int32_t(used_slots(n_tokens, n_req, a.group, max_new, kind.rows));
+  a.pieces = sh.pieces;
   void* args[] = {&a};
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const int d128 = head_dim == 128;
@@ -1657,7 +1719,7 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
       dim3(unsigned(groups)), dim3(unsigned(kind.threads)), args, 0, st);
   if (e == hipSuccess && sh.cut)
     e = hipLaunchKernel(reinterpret_cast<const void*>(kind.join[d128]),
-                        dim3(unsigned(grid * (kind.rows / 32))), dim3(unsigned(2 * head_dim)), args,
+                        dim3(unsigned(a.tiles * kv_heads * (kind.rows / 32))), dim3(unsigned(2 * head_dim)), args,
                         0, st);
   if (e == hipSuccess && sh.splits > 1) {
     ChunkFn fn = head_dim == 64 ? (one ? chunk_attn_merge<64, 1> : chunk_attn_merge<64, 4>)
