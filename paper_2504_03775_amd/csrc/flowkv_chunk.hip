@@ -13,6 +13,7 @@
 #include "flowkv.h"
 #include "flowkv_device.h"
 #include "flowkv_ragged.h"
+#include "flowkv_splits.h"
 #include "flowkv_status.h"
 
 using flowkv::fail;
@@ -1341,7 +1342,7 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_attn_merge(const ChunkArg
   const int32_t end = std::min(((row >> a.row_shift) + 1) << a.row_shift, rq.n_new * a.group);
   const int32_t tile_limit = seen(rq, token_of(a, end - 1));
   if (tile_limit <= a.split_tokens) return;      // written already
-  const int32_t n = (seen(rq, i) + a.split_tokens - 1) / a.split_tokens;
+  const int32_t n = flowkv::splits_of(seen(rq, i), a.split_tokens);
   const int64_t rec = record_at(a, orow, 0);
   const int tid = kWavesPer == 1 ? ln : threadIdx.x;
   const float* sums = record_sums(a, kDh, rec) + 4 * (tid % kLanes);

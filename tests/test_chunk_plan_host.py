@@ -1,11 +1,16 @@
 """The workspace that attention of new tokens asks for under the library's own rule (CPU):
 bounded as include/flowkv.h says, whatever the batch is padded to."""
 
+import os
+import shutil
+import subprocess
+
 import numpy as np
 import pytest
 
 from paper_2504_03775_amd import flowkv as fk
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 MOST = 34_080_772       # bytes, where requests bring more than 32 rows a KV head
 workspace = fk.flowkv_chunk_attention_workspace
 
@@ -61,3 +66,17 @@ def test_workspace_of_a_given_split_counts_every_row():
         for new in (1, 300):
             assert workspace(20000, 8, 8, 1, 128, new, 32768, split) == \
                 records(20000, 8, 128, 32768 // split)
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
+def test_splits_are_counted_to_the_end_of_32_bits(tmp_path):
+    """As the join of a row's splits counts them: with more than 2^30 tokens in splits of
+    about as many, the tokens and the split together pass 32 bits."""
+    exe = str(tmp_path / "splits_check")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=undefined",
+                    "-fno-sanitize-recover=all", "-I",
+                    os.path.join(ROOT, "paper_2504_03775_amd", "csrc"),
+                    os.path.join(ROOT, "tests", "native", "splits_check.cpp"), "-o", exe],
+                   check=True, capture_output=True, timeout=120)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and "counts ok" in r.stdout, r.stdout + r.stderr
