@@ -483,8 +483,12 @@ int flowkv_append(const flowkv_pool* pool, int32_t layer, const void* k_dev, int
    beyond max_seq_len are not read; a block ID outside the pool contributes
    nothing; a new token that sees nothing (a negative position among them) gets
    zeros.  A score that is NaN or +inf makes its row's output NaN; one of -inf
-   weighs nothing.  K and V of tokens that a row does not see, infinities and
-   NaN among them, do not reach it.
+   weighs nothing where its V is finite.  An infinity or a NaN in V of a token
+   that a row sees makes that element of its output infinite or NaN, however
+   small the token's weight, 0 for a score of -inf included (0 x inf is NaN in
+   float32; which of the two an element becomes may depend on split_tokens).
+   K and V of tokens that a row does not see, infinities and NaN among them, do
+   not reach it.
    max_new: the most new tokens of a request, and max_seq_len the longest
    length; both size the launch, and rows past max_new are computed all the
    same.  head_dim 64 or 128; any whole number of query heads per KV head,

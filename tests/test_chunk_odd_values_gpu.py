@@ -132,3 +132,41 @@ def test_a_request_of_nan_costs_little_more(d, layout, new, total, split):
     assert torch.isnan(out[:new].float()).all()
     assert torch.equal(out[new:], ref[new:])
     assert after < 1.5 * before + 10
+
+
+@pytest.mark.parametrize("weight", ["-inf", "underflow"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("d,new,split,longest", [
+    (128, 3, 0, False), (64, 7, 64, False), (64, 60, 0, False), (128, 200, 64, False),
+    (64, 200, 1 << 20, False), (128, 200, 0, True), (64, 200, 0, True),
+])
+def test_bad_v_of_a_seen_token_reaches_its_rows_at_any_weight(d, new, split, longest, bad, weight):
+    """A token whose score is -inf, or so low that its weight is 0, has a bad value in V: far
+    before the new tokens, among them, in the last one, and beside a missing block.  Rows
+    that see it have an element that is not finite; nothing else changes."""
+    total, far = 700, 130
+    for at in (far, total - new // 2 - 1, total - 1, 335):
+        b = Batch(Geometry("oddweight", 1, 1, d, 16, "bfloat16"), LM, [new], [total], 53)
+        if at == 335:
+            b.tab[0, 336 // 16] = -1
+            b.upload()
+        q = queries(b, 4, 53)
+        q[:, :, 3] = 1.0
+        view = b.layer_view(0)
+        slot = int(b.tab[0, at // 16]), at % 16, 0
+        view[0][slot] = 0
+        view[0][slot + (3,)] = float("-inf") if weight == "-inf" else -1e6
+        call, out = prepared(b, q, split, 400_000 if longest else None)
+        call()
+        torch.cuda.synchronize()
+        ref = out.clone()
+        assert torch.isfinite(ref[min(1, new - 1):].float()).all()
+        view[1][slot + (5,)] = bad
+        out.fill_(7)
+        call()
+        torch.cuda.synchronize()
+        sees = torch.as_tensor(total - new + np.arange(new) >= at, device="cuda")
+        assert not torch.isfinite(out[sees][:, :, 5].float()).any(), at
+        assert torch.equal(out[~sees], ref[~sees]), at
+        rest = [i for i in range(d) if i != 5]
+        assert torch.equal(out[:, :, rest], ref[:, :, rest]), at
