@@ -49,6 +49,18 @@ struct flowkv_allocator {
     by_len.erase({len, start});
   }
 
+  // Take the first n blocks, but not all, off the free run [start, start+len).  (Allocates
+  // nothing, so it cannot fail.)
+  void shorten_run(int32_t start, int32_t len, int32_t n) {
+    auto s = by_start.extract(start);
+    s.key() += n;
+    s.mapped() -= n;
+    by_start.insert(std::move(s));
+    auto l = by_len.extract({len, start});
+    l.value() = {len - n, start + n};
+    by_len.insert(std::move(l));
+  }
+
   // Insert the free run [start, start+len), merging with free neighbours.
   void release_run(int32_t start, int32_t len) {
     auto next = by_start.find(start + len);
@@ -196,8 +208,8 @@ int alloc_impl(flowkv_allocator* a, int32_t n, int32_t* out_ids) {
     auto fit = a->by_len.lower_bound({need, INT32_MIN});
     if (fit != a->by_len.end()) {
       int32_t len = fit->first, start = fit->second;
-      a->erase_run(start, len);
-      if (len > need) a->insert_run(start + need, len - need);
+      if (len > need) a->shorten_run(start, len, need);
+      else a->erase_run(start, len);
       for (int32_t i = 0; i < need; ++i) out_ids[pos++] = start + i;
       need = 0;
     } else {
@@ -312,6 +324,19 @@ int compact_impl(flowkv_allocator* a, int32_t cap, int32_t* src_ids, int32_t* ds
     return fail(FLOWKV_ECAP, "%d moves, room for %d", need, cap);
   }
   if (need > 0) {
+    // what takes memory, before anything changes
+    std::map<int32_t, int32_t> by_start;
+    std::set<std::pair<int32_t, int32_t>> by_len;
+    std::deque<int32_t> kept;
+    if (a->policy == FLOWKV_POLICY_SEGMENT) {
+      by_start.emplace(live, int32_t(a->num_blocks - live));
+      by_len.emplace(int32_t(a->num_blocks - live), live);
+    } else {
+      for (int32_t b : a->fifo)                  // (the free blocks below become destinations)
+        if (b >= live) kept.push_back(b);
+      for (int32_t b = live; b < a->num_blocks; ++b)
+        if (a->used[b]) kept.push_back(b);
+    }
     for (int32_t b = 0, i = 0; b < live; ++b)
       if (!a->used[b]) dst_ids[i++] = b;
     for (int32_t b = live, i = 0; i < need; ++b)
@@ -321,17 +346,9 @@ int compact_impl(flowkv_allocator* a, int32_t cap, int32_t* src_ids, int32_t* ds
       a->used[src_ids[i]] = 0;
       if (!a->extra.empty()) std::swap(a->extra[dst_ids[i]], a->extra[src_ids[i]]);
     }
-    if (a->policy == FLOWKV_POLICY_SEGMENT) {
-      a->by_start.clear();
-      a->by_len.clear();
-      a->insert_run(live, a->num_blocks - live);
-    } else {
-      std::deque<int32_t> kept;
-      for (int32_t b : a->fifo)
-        if (!a->used[b]) kept.push_back(b);
-      kept.insert(kept.end(), src_ids, src_ids + need);
-      a->fifo.swap(kept);
-    }
+    a->by_start.swap(by_start);
+    a->by_len.swap(by_len);
+    a->fifo.swap(kept);
   }
   *n_moves = need;
   return ok();
