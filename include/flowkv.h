@@ -492,7 +492,8 @@ int flowkv_append(const flowkv_pool* pool, int32_t layer, const void* k_dev, int
    max_new: the most new tokens of a request, and max_seq_len the longest
    length; both size the launch, and rows past max_new are computed all the
    same.  head_dim 64 or 128; any whole number of query heads per KV head,
-   n_tokens times which is under 2^31 - 512.
+   n_tokens times which is under 2^31 - 512; scale above 0 and, times log2(e),
+   finite.
    split_tokens: cached tokens per workgroup, a multiple of 64; 0 takes the
    library's rule.  One launch on hip_stream, two where the workspace is not 0:
    then workspace_dev holds at least flowkv_chunk_attention_workspace(...) bytes

@@ -1648,7 +1648,8 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   // positions are formed in 32 bits past the last tile's end
   if (max_seq_len > INT32_MAX - 4096)
     return fail(FLOWKV_EINVAL, "max_seq_len %d: need at most 2^31 - 4097", max_seq_len);
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(FLOWKV_EINVAL, "bad scale");
+  // (the kernels take it in powers of 2)
+  if (!(scale > 0.f) || !std::isfinite(scale * kLog2e)) return fail(FLOWKV_EINVAL, "bad scale");
   if (n_req == 0 || n_tokens == 0) return ok();
   if (!q_dev || !offsets_dev || !seq_lens_dev || !out_dev || (max_blocks > 0 && !block_tables_dev))
     return fail(FLOWKV_EINVAL, "NULL device pointer");

@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 
 from paper_2504_03775_amd import flowkv as fk
+from tests.test_pages_host import chunk, pool
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 MOST = 34_080_772       # bytes, where requests bring more than 32 rows a KV head
@@ -80,3 +81,11 @@ def test_splits_are_counted_to_the_end_of_32_bits(tmp_path):
                    check=True, capture_output=True, timeout=120)
     r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "counts ok" in r.stdout, r.stdout + r.stderr
+
+
+def test_a_scale_that_passes_float32_in_powers_of_two_is_refused():
+    """scale x log2(e) above float32's largest: every score would be 0 x inf."""
+    p = pool()
+    for scale in (3e38, 2.4e38):
+        assert chunk(p, n=0, scale=2.3e38) == fk.OK
+        assert chunk(p, n=0, scale=scale) == fk.EINVAL
