@@ -477,23 +477,26 @@ int flowkv_append(const flowkv_pool* pool, int32_t layer, const void* k_dev, int
        out[i][h] = sum_{t <= p} softmax_t(scale * q[i][h] . K[t][g]) * V[t][g]
    q_dev: bf16, 16-byte aligned, a token's (q_heads, head_dim) values together
    and tokens q_stride ELEMENTS apart (a multiple of 8).  out_dev: (n_tokens,
-   q_heads, head_dim) bf16, 8-byte aligned; scores, weights' sums and the output
-   are formed in float32, the weights enter the matrix product rounded to bf16,
-   and the output is rounded once.  Tokens beyond max_blocks x block_size or
-   beyond max_seq_len are not read; a block ID outside the pool contributes
-   nothing; a new token that sees nothing (a negative position among them) gets
-   zeros.  A score that is NaN or +inf makes its row's output NaN; one of -inf
-   weighs nothing where its V is finite.  An infinity or a NaN in V of a token
-   that a row sees makes that element of its output infinite or NaN, however
-   small the token's weight, 0 for a score of -inf included (0 x inf is NaN in
-   float32; which of the two an element becomes may depend on split_tokens).
-   K and V of tokens that a row does not see, infinities and NaN among them, do
-   not reach it.
+   q_heads, head_dim) bf16, 8-byte aligned.  Scores, weights' sums and the
+   output are formed in float32, the weights enter the matrix product rounded to
+   bf16 (for weights of 24 bits a single token has flowkv_decode_attention), and
+   the output is rounded once.  Weights, up to 2^8 each, are divided by their sum
+   at the end: a row's sum of them times |V| has to stay within float32.
+   Tokens beyond max_blocks x block_size or beyond max_seq_len are not read; a
+   block ID outside the pool contributes nothing; a new token that sees nothing
+   (a negative position among them) gets zeros.  A score that is NaN or +inf
+   makes its row's output NaN; one of -inf weighs nothing where its V is finite.
+   An infinity or a NaN in V of a token that a row sees makes that element of its
+   output infinite or NaN, however small the token's weight, 0 for a score of
+   -inf included (0 x inf is NaN in float32; which of the two an element becomes
+   may depend on split_tokens).  K and V of tokens that a row does not see,
+   infinities and NaN among them, do not reach it.
    max_new: the most new tokens of a request, and max_seq_len the longest
    length; both size the launch, and rows past max_new are computed all the
    same.  head_dim 64 or 128; any whole number of query heads per KV head,
    n_tokens times which is under 2^31 - 512; scale above 0 and, times log2(e),
-   finite.
+   finite; max_seq_len at most 2^31 - 4097, max_blocks x block_size 2^31 - 1;
+   blocks under 4 GiB apart in a pool under 512 GiB.
    split_tokens: cached tokens per workgroup, a multiple of 64; 0 takes the
    library's rule.  One launch on hip_stream, two where the workspace is not 0:
    then workspace_dev holds at least flowkv_chunk_attention_workspace(...) bytes
