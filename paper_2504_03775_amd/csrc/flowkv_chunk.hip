@@ -183,9 +183,10 @@ __device__ __forceinline__ int v_swizzle(int x) {
 //
 // What bounds it: 4 Dh operations a (row, token) on the matrix units beside an exponential
 // and some ten vector operations, on a card that lowers its clock under this load (to about
-// 1.8 of 2.4 GHz).  The 13,000-token prompt, 32 heads of 128 on 8, takes 1.31 ms, 1.06
-// PFLOP/s (a library's product of 4,096^3 reaches 1.13 there, of 16,384^3 1.34); 20,000 tokens, 8
-// heads of 64 on 4, 510 us, 0.80, where exponentials take as long as products.  A lone step
+// 1.8 of 2.4 GHz).  The 13,000-token prompt, 32 heads of 128 on 8, takes 1.29 to 1.38 ms by
+// the card, 1.00 to 1.07 PFLOP/s (a library's product of 4,096^3 reaches 1.13, of 16,384^3
+// 1.34); 20,000 tokens, 8 heads of 64 on 4, 524 us, 0.78, where exponentials take as long as
+// products.  A lone step
 // is bound by its load (a CU alone draws about 45 bytes a nanosecond) and its latencies:
 // 1.7 us for 256 rows x 64 tokens of 128.
 //
@@ -416,12 +417,13 @@ struct Source {
 //     of split for contexts of 500 to 9,000 tokens, or under the causal diagonal, some CUs
 //     have nothing while others go round twice.)  Tiles in more than one piece are joined
 //     from their records by a second kernel.  Chunks of 100 to 700 tokens beside 20 single
-//     ones over up to 8,000 cached, 8 heads of 128 on one KV head: 66 us, by even splits 84;
-//     512 tokens behind 8,000, 32 heads on 8: 86 and 93; 4,000 behind none, 8 on 1: 60 and
-//     71.  With few steps the even splits are faster: 256 behind 4,000, 32 on 8: 38 and 42.
+//     ones over up to 8,000 cached, 8 heads of 128 on one KV head: 67 us, by even splits 78
+//     at best; 512 tokens behind 8,000, 32 heads on 8: 86 and 92; 4,000 behind none, 8 on 1:
+//     60 and 68.  With few steps the even splits are faster: 256 behind 4,000, 32 on 8: 37,
+//     in pieces 39.
 //   - more tiles than CUs, of requests with much in the cache: whole tiles, the longest
 //     first, so that the last ones to end are short.  4 chunks of 100 to 600 tokens beside 36
-//     single ones over 100 to 6,600, 32 heads on 8: 242 us, in the requests' order 339.
+//     single ones over 100 to 6,600, 32 heads on 8: 251 us, in the requests' order 326.
 //     (Prompts with nothing cached gain nothing: the diagonal orders each of them.)
 constexpr int kPieceTiles = 512;           // most tile slots, and requests, of such a call
 constexpr int kPieceLeast = 2;             // steps
@@ -988,17 +990,17 @@ __global__ __launch_bounds__(2 * F::kDh) void chunk_attn_join(const ChunkArgs a)
 //
 // A request of a few new tokens reads every cached K and V for a handful of rows: that is
 // bound by HBM, as the decode step is, and wants many loads in flight rather than many rows
-// per byte.  A workgroup takes 16 rows, as the 16 columns of S^T, and each of its four
-// waves tiles of 32 tokens of its own, four tiles apart, with no barrier between:
+// per byte.  A workgroup takes 16 rows, as the 16 columns of S^T, or twice 16, and each of
+// its four waves tiles of 32 tokens of its own, four tiles apart, with no barrier between:
 //   - K and V rows arrive whole in registers (16 lanes a row of K; a lane of group q4 =
 //     lane / 16 has V of the tokens 4 e + q4, e = 0..7), the next tile's while this one is
 //     worked on;
 //   - K goes through the wave's part of LDS into the A operand, row m of half gg being
 //     token 16 gg + 4 (m % 4) + m / 4: a lane's scores are then those of the tokens whose
 //     V it holds, and P and V are operands of P.V where they are.
-// 24 requests of 2 to 8 tokens over 2,000 to 16,000, 32 heads of 128 on 8 (915 MB) take 178
-// us with the merge, 5.1 TB/s; 64 of one token over 500 to 4,000 112 us (128 rows a
-// workgroup: 137).  K and V are read once and past the caches.
+// 24 requests of 2 to 8 tokens over 2,000 to 16,000, 32 heads of 128 on 8 (915 MB), in 32 rows
+// take 179 us with the merge, 5.1 TB/s; 64 of one token over 500 to 4,000, in 16 rows, 115 us
+// (128 rows a workgroup, one split: 166).  K and V are read once and past the caches.
 constexpr int kFewWaves = 4;
 constexpr int kFewThreads = 64 * kFewWaves;
 constexpr int kFewTile = 32;
@@ -1466,9 +1468,9 @@ constexpr int64_t kRuleBytes =
 
 // The split that ends soonest by a simple count: the CUs' rounds over all tiles' splits, each
 // as long as its tokens and `fixed` more (a workgroup's start and end), and the merge.  In
-// few rows, 4 KiB of K and V a token: 5 new ones over 13,000, 8 KV heads, take 18.0 us in
-// splits of 512 (208 workgroups), 20.7 of 256, 23.2 of 384 (272), 20.1 of 768; 8 requests of 4
-// over up to 12,000 70.7 of 1,536 (512), 78.7 of 1,024, 85.7 of 2,048.
+// few rows, 4 KiB of K and V a token: 5 new ones over 13,000, 8 KV heads, take 18.8 us in
+// splits of 512 (208 workgroups), 21.6 of 256, 23.8 of 384 (272), 20.7 of 768; 8 requests of 4
+// over up to 12,000 70.9 of 1,536 (512), 78.5 of 1,024, 86.0 of 2,048.
 int32_t best_split(int64_t tiles, int64_t max_seq_len, int64_t fixed, int64_t most) {
   constexpr int64_t kUnit = 128, kMerge = 150;
   constexpr int kTried[] = {1,  2,  3,  4,  5,  6,  8,  10, 12,  16,
@@ -1511,9 +1513,9 @@ int plan_shape(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_head
   const int64_t t256 = tiles_of(n_tokens, n_req, group, max_new, 256) * kv_heads;
   const int64_t t128 = tiles_of(n_tokens, n_req, group, max_new, 128) * kv_heads;
   // Up to 32 rows a request, or few steps in all: 32 rows a workgroup and its waves apart in
-  // the keys end soonest.  (60 tokens behind 140, 4 heads of 64 on 2: 8.9 us, in 128 rows
-  // 10.1; 30 behind 500, 32 of 128 on 8: 13.6 and 16.8; but 1,000 behind none, 8 on 1: 29.0
-  // and 23.2.)
+  // the keys end soonest.  (60 tokens behind 140, 4 heads of 64 on 2: 7.5 us, in 128 rows
+  // 9.8; 30 behind 500, 32 of 128 on 8: 12.7 and 19.3; but 1,000 behind none, 8 on 1: 29.0
+  // and 22.7.)
   const int64_t t32 = tiles_of(n_tokens, n_req, group, max_new, 32) * kv_heads;
   const bool rule = split_tokens == 0, many = int64_t(max_new) * group > 32;
   // records of even splits, past 63 bits: the most that 63 bits hold

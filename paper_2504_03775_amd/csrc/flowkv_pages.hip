@@ -162,8 +162,9 @@ static_assert(sizeof(CopyTokensLM) + kImplicitArgBytes <= 4096, "kernel argument
 // slots (all of them without token counts) of its 2 L chunks, in 16-byte pieces.
 // Both are bound by memory.  A call that reads and writes up to 256 MiB takes the
 // first, a larger one the second: of 2 MiB blocks (32 layers of 8 x 128, block-major)
-// 60 take 37.9 us in the first and 39.4 in the second, 90 take 66.2 and 59.2, 1,000
-// take 774 and 643 (6.5 TB/s); 24 partly filled ones 9.3 and 12.0.
+// 60 take 38.0 us in the first and 40.0 in the second, 90 take 67.2 and 59.4, 1,000
+// take 775 and 645 (6.5 TB/s); 24 partly filled ones 10.0 and 12.0 (calls one after another;
+// the first kernel alone 7.1).
 //
 // The first: what it reads was written a moment ago as a rule (the block that a
 // prompt ends in) and is looked for in the caches.  A record's pieces are one span,
