@@ -1707,7 +1707,8 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   const bool one = sh.splits <= kMergeChunk * 64 * 4 / head_dim;
   const int64_t out_rows = int64_t(n_tokens) * q_heads, merge = one ? (out_rows + 3) / 4 : out_rows;
   // lanes of a launch in 32 bits
-  if (grid > UINT32_MAX / kind.threads / sh.splits || merge > UINT32_MAX / kMergeThreads)
+  if (grid > UINT32_MAX / kind.threads / sh.splits ||
+      (sh.splits > 1 && merge > UINT32_MAX / kMergeThreads))
     return fail(FLOWKV_EINVAL, "%lld tiles of queries x %d splits: too many for one call",
                 (long long)grid, sh.splits);
   a.tiles = int32_t(tiles);

@@ -82,3 +82,21 @@ def test_more_tiles_than_max_new_makes_room_for(d, hk, G, new, total, max_new, l
     out, _ = attend_as(b, q, d ** -0.5, max_new, 0, max_len)
     check_attention(b, 0, q, d ** -0.5, out, max_seq=max_len)
     assert torch.isfinite(out[3:3 + sum(new)].float()).all()
+
+
+def test_rows_past_what_a_join_could_launch():
+    """2^26 output rows and more, most of them padding, in a call that joins no splits."""
+    hq, d, n = 32, 64, (1 << 21) + 40
+    b = Batch(Geometry("padmany", 1, 2, d, 16, "bfloat16"), BM, [30, 1], [300, 40], 95,
+              pad=(n - 36, 5))
+    assert b.n_tokens == n and n * hq > 1 << 26
+    q = torch.zeros((n, hq, d), dtype=torch.bfloat16, device="cuda")
+    first = int(b.off[0])
+    q[first:] = torch.randn((n - first, hq, d), device="cuda",
+                            generator=torch.Generator("cuda").manual_seed(95)).to(torch.bfloat16)
+    out = torch.full_like(q, 7.0)
+    assert fk.flowkv_chunk_attention_workspace(n, 2, hq, 2, d, 30, 1 << 20, 1 << 20) == 0
+    fk.flowkv_chunk_attention(b.pool, 0, q, *b.args(), 30, 1 << 20, 0.1, out, None, 1 << 20)
+    torch.cuda.synchronize()
+    check_attention(b, 0, q, 0.1, out, max_seq=1 << 20)
+    assert (out[:first] == 7).all() and (out[-5:] == 7).all()
