@@ -21,7 +21,9 @@
  * Beside them: flowkv_decode_attention*, the paged decode attention that
  * reads either layout (the PagedAttention kernel section 3.3 adapts);
  * flowkv_append and flowkv_chunk_attention, which fill the pool and read it
- * for a chunk of new tokens (prefill, several tokens of a decode step);
+ * for a chunk of new tokens (prefill, several tokens of a decode step), with
+ * flowkv_append_rotated, flowkv_window_attention and flowkv_prefix_attention
+ * for rotated keys, sliding windows and shared prefixes;
  * flowkv_copy_blocks with flowkv_share, flowkv_fork and flowkv_compact, pages
  * copied within a pool, shared and moved together; and flowkv_sched*, the
  * load-aware scheduler of section 3.4 (Algorithm 1), host only.
@@ -93,6 +95,9 @@ enum {
      adjacent.  layer_base[0] points at it. */
   FLOWKV_LAYOUT_BLOCK_MAJOR = 1
 };
+
+/* ---- element types, where a call reads or rounds values ---------------------- */
+enum { FLOWKV_BF16 = 0, FLOWKV_FP16 = 1, FLOWKV_F32 = 2 };
 
 #define FLOWKV_MAX_LAYERS 128
 #define FLOWKV_INLINE_RUNS 64 /* plan records flowkv_transfer_inline carries */
@@ -469,6 +474,35 @@ int flowkv_append(const flowkv_pool* pool, int32_t layer, const void* k_dev, int
                   int32_t n_req, const int32_t* offsets_dev, const int32_t* block_tables_dev,
                   int32_t max_blocks, const int32_t* seq_lens_dev, void* hip_stream);
 
+/* flowkv_append with K, and the queries, rotated by their positions on the way
+   (rotary position embedding), one launch.  For a new token at position p and pair j of
+   the first rot_dim dims of a head, with c = cos_sin[p][j] and s = cos_sin[p][rot_dim / 2 + j]:
+       (a, b) becomes (a c - b s, a s + b c),
+   a pair being dims j and j + rot_dim / 2, or with `interleaved` 1 dims 2 j and 2 j + 1; in
+   float32, rounded once to the type; dims from rot_dim on stay as they are.  K goes to its
+   block rotated, V as it is, q rotated to q_out.  Values of a type `dtype` (FLOWKV_BF16,
+   FLOWKV_FP16, FLOWKV_F32), the pool's as well.
+   q_dev, k_dev, v_dev, q_out_dev: 16-byte aligned, a token's heads together, tokens a stride
+   in ELEMENTS apart that is a whole number of 16 bytes.  q_out_dev may be q_dev with the same
+   stride; any other overlap is undefined.  q_heads 0: no queries (both may be NULL).
+   cos_sin_dev: (n_positions, rot_dim) float32.
+   offsets, block_tables, seq_lens as for flowkv_append.  A token whose position is negative or
+   not below n_positions has nothing written, neither K and V nor q; one past its block list,
+   or whose block is outside the pool, has q written only.  Rows of no request are not written.
+   EINVAL: NULL pointers, negative sizes, bad pool (as for flowkv_transfer), layer outside it,
+   unknown dtype, head_dim not a whole number of 16 bytes, kv_heads x head_dim that does not
+   divide chunk_bytes, rot_dim not a whole number of 32 bytes from 1 to head_dim, `interleaved`
+   neither 0 nor 1, misaligned rows or strides, strides below a token's heads. */
+int flowkv_append_rotated(const flowkv_pool* pool, int32_t layer, int32_t dtype,
+                          const void* q_dev, int64_t q_stride, void* q_out_dev,
+                          int64_t q_out_stride, const void* k_dev, int64_t k_stride,
+                          const void* v_dev, int64_t v_stride, int32_t q_heads,
+                          int32_t kv_heads, int32_t head_dim, const float* cos_sin_dev,
+                          int32_t n_positions, int32_t rot_dim, int32_t interleaved,
+                          int32_t n_tokens, int32_t n_req, const int32_t* offsets_dev,
+                          const int32_t* block_tables_dev, int32_t max_blocks,
+                          const int32_t* seq_lens_dev, void* hip_stream);
+
 /* Attention of new tokens over the pool: prefill in chunks, a prompt behind a
    cached prefix, or the several tokens of a speculative decode step.  The new
    tokens' own K and V are in the pool already (flowkv_append).  For new token i
@@ -522,6 +556,69 @@ int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, const void* q
 int flowkv_chunk_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q_heads,
                                      int32_t kv_heads, int32_t head_dim, int32_t max_new,
                                      int32_t max_seq_len, int32_t split_tokens, int64_t* bytes);
+
+/* flowkv_chunk_attention through a sliding window with a few first tokens that stay visible:
+   a new token at position p attends to the tokens t <= p with t > p - window or t < sinks.
+   window >= 1 counts the token itself; sinks >= 0.  Tokens that no new token of a request sees
+   are not looked up: their entries of the block list may hold anything (their blocks freed).
+   dtype: FLOWKV_BF16 or FLOWKV_FP16, the type of q, the pool and out (weights enter the matrix
+   product rounded to it).  Split by split_tokens are the tokens that a workgroup's rows see
+   between them, the first ones and those of its window.  The rest, single tokens of a decode
+   step among it, is as for flowkv_chunk_attention: K and V of tokens that a row does not see,
+   infinities and NaN among them, do not reach it, and a row that sees nothing gets zeros.
+   EINVAL additionally for a window below 1, sinks below 0 and an unknown dtype. */
+int flowkv_window_attention(const flowkv_pool* pool, int32_t layer, int32_t dtype,
+                            const void* q_dev, int64_t q_stride, int32_t n_tokens, int32_t n_req,
+                            int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                            const int32_t* offsets_dev, const int32_t* block_tables_dev,
+                            int32_t max_blocks, const int32_t* seq_lens_dev, int32_t max_new,
+                            int32_t max_seq_len, int32_t window, int32_t sinks, float scale,
+                            int32_t split_tokens, void* out_dev, void* workspace_dev,
+                            int64_t workspace_bytes, void* hip_stream);
+
+/* Workspace bytes of flowkv_window_attention for these arguments: with split_tokens, n_tokens x
+   q_heads x splits x (head_dim + 2) floats where there is more than one split of what a
+   workgroup's rows can see between them (at most max_seq_len, and about sinks + window +
+   max_new); with 0 as for flowkv_chunk_attention.  EINVAL as for the call. */
+int flowkv_window_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q_heads,
+                                      int32_t kv_heads, int32_t head_dim, int32_t max_new,
+                                      int32_t max_seq_len, int32_t window, int32_t sinks,
+                                      int32_t split_tokens, int64_t* bytes);
+
+/* flowkv_chunk_attention for requests that share long prefixes, each prefix read once for all
+   of a group.  Group g is the requests groups[g] .. groups[g + 1] - 1 (n_groups + 1
+   non-decreasing int32 in device memory, requests outside of all groups allowed), whose first
+   prefix_lens[g] tokens are the same: their block lists name the same K and V there (blocks
+   shared by flowkv_share, a part-filled last one copied as flowkv_fork has it).  The list of
+   the group's first request is the one read for the prefix.  Every row sees all tokens up to
+   its own position, those of the prefix and those behind it: the result is that of
+   flowkv_chunk_attention, joined in another order.
+   dtype: FLOWKV_BF16 or FLOWKV_FP16, the type of q, the pool and out.
+   max_new: the most new tokens of a request, max_group: of a group; both size the launch, and
+   rows past them are computed all the same.  max_prefix: the longest prefix; max_own: the most
+   tokens of a request behind its prefix, or in all where it is in no group.  Where a prefix or
+   a request has more, its rows are of no meaning (nothing outside the pool and the lists is
+   read).  max_prefix + max_own is at most 2^31 - 4097.
+   split_tokens: cached tokens per workgroup at most, a multiple of 64; 0 takes the library's
+   rule, which may also find that requests are done sooner each by itself.  Up to three launches
+   on hip_stream.  The rest is as for flowkv_chunk_attention.  EINVAL for bad shapes or
+   pointers, ECAP for a short workspace. */
+int flowkv_prefix_attention(const flowkv_pool* pool, int32_t layer, int32_t dtype,
+                            const void* q_dev, int64_t q_stride, int32_t n_tokens, int32_t n_req,
+                            int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                            const int32_t* offsets_dev, const int32_t* block_tables_dev,
+                            int32_t max_blocks, const int32_t* seq_lens_dev, int32_t n_groups,
+                            const int32_t* groups_dev, const int32_t* prefix_lens_dev,
+                            int32_t max_new, int32_t max_group, int32_t max_own,
+                            int32_t max_prefix, float scale, int32_t split_tokens, void* out_dev,
+                            void* workspace_dev, int64_t workspace_bytes, void* hip_stream);
+
+/* Workspace bytes of flowkv_prefix_attention for these arguments.  EINVAL as for the call, and
+   where the size passes 2^63. */
+int flowkv_prefix_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q_heads,
+                                      int32_t kv_heads, int32_t head_dim, int32_t n_groups,
+                                      int32_t max_new, int32_t max_group, int32_t max_own,
+                                      int32_t max_prefix, int32_t split_tokens, int64_t* bytes);
 
 /* ---- copies of blocks within a pool --------------------------------------------- */
 

@@ -25,7 +25,7 @@ LIB = os.path.join(PKG, "libflowkv.so")
 HOST_SOURCES = ["flowkv_status.cpp", "flowkv_alloc.cpp", "flowkv_plan.cpp", "flowkv_sched.cpp",
                 "flowkv_request.cpp"]
 HIP_SOURCES = ["flowkv_transfer.hip", "flowkv_attention.hip", "flowkv_chunk.hip",
-               "flowkv_pages.hip"]
+               "flowkv_pages.hip", "flowkv_window.hip", "flowkv_prefix.hip", "flowkv_rotate.hip"]
 
 ARCH = "gfx950"
 # packed-fp32 instructions are disabled for every HIP translation unit

@@ -253,8 +253,9 @@ __global__ __launch_bounds__(kStreamThreads) void kv_block_stream(const A a) {
   __builtin_nontemporal_store(__builtin_nontemporal_load((cgvec*)src), (gvec*)dst);
 }
 
-// The pool's descriptor, as every call here checks it.
-int check_pool(const flowkv_pool* p) {
+}  // namespace
+
+int flowkv::check_pool(const flowkv_pool* p) {
   if (!p) return fail(FLOWKV_EINVAL, "NULL pool");
   if (p->layout != FLOWKV_LAYOUT_LAYER_MAJOR && p->layout != FLOWKV_LAYOUT_BLOCK_MAJOR)
     return fail(FLOWKV_EINVAL, "unknown layout %d", p->layout);
@@ -276,14 +277,12 @@ int check_pool(const flowkv_pool* p) {
   return FLOWKV_OK;
 }
 
-}  // namespace
-
 extern "C" int flowkv_append(const flowkv_pool* pool, int32_t layer, const void* k_dev,
                              int64_t k_stride, const void* v_dev, int64_t v_stride,
                              int64_t slot_bytes, int32_t n_tokens, int32_t n_req,
                              const int32_t* offsets_dev, const int32_t* block_tables_dev,
                              int32_t max_blocks, const int32_t* seq_lens_dev, void* hip_stream) {
-  int rc = check_pool(pool);
+  int rc = flowkv::check_pool(pool);
   if (rc) return rc;
   if (layer < 0 || layer >= pool->num_layers)
     return fail(FLOWKV_EINVAL, "layer %d outside the pool's %d layers", layer, pool->num_layers);
@@ -441,7 +440,7 @@ int launch_copy(const flowkv_pool* p, const int32_t* src, const int32_t* dst,
 
 int copy_impl(const flowkv_pool* pool, const int32_t* src_ids, const int32_t* dst_ids,
               const int32_t* tokens, int32_t n_blocks, int64_t slot_bytes, void* stream) {
-  int rc = check_pool(pool);
+  int rc = flowkv::check_pool(pool);
   if (rc) return rc;
   if (n_blocks < 0) return fail(FLOWKV_EINVAL, "negative block count %d", n_blocks);
   if (tokens) {

@@ -16,6 +16,10 @@ int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 // Clear the calling thread's message and return FLOWKV_OK.
 int ok();
 
+// A pool's descriptor, as the calls that write into its pages check it (flowkv_pages.hip).
+// FLOWKV_OK, or a recorded failure.
+int check_pool(const flowkv_pool* p);
+
 // Run an entry point's body so that no exception crosses the C ABI: the
 // standard containers of the host code can only raise std::bad_alloc, which
 // becomes FLOWKV_ENOMEM.

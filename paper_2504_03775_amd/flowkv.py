@@ -23,6 +23,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libflowkv.s
 OK, EINVAL, ENOSPC, ERANGE, EDUP, ECAP, EHIP, ENOMEM = 0, -1, -2, -3, -4, -5, -6, -7
 POLICY_SEGMENT, POLICY_FIFO_SORTED, POLICY_FIFO_SHUFFLED = 0, 1, 2
 LAYOUT_LAYER_MAJOR, LAYOUT_BLOCK_MAJOR = 0, 1
+BF16, FP16, F32 = 0, 1, 2
 MAX_LAYERS = 128
 INLINE_RUNS = 64  # plan records flowkv_transfer_inline carries in the kernel arguments
 INLINE_RUNS_BLOCK_MAJOR = 300  # ... between two block-major pools, in the planner's form
@@ -155,6 +156,27 @@ SIGNATURES = {
                                               ctypes.c_void_p, ctypes.c_int64,
                                               ctypes.c_void_p]),
     "flowkv_chunk_attention_workspace": (ctypes.c_int, [ctypes.c_int32] * 8 + [_I64P]),
+    "flowkv_append_rotated": (ctypes.c_int, [
+        _POOLP, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+        ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+        ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32,
+        ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+        ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]),
+    "flowkv_window_attention": (ctypes.c_int, [
+        _POOLP, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32,
+        ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+        ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32,
+        ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_int32, ctypes.c_void_p,
+        ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "flowkv_window_attention_workspace": (ctypes.c_int, [ctypes.c_int32] * 10 + [_I64P]),
+    "flowkv_prefix_attention": (ctypes.c_int, [
+        _POOLP, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32,
+        ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+        ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+        ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+        ctypes.c_float, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64,
+        ctypes.c_void_p]),
+    "flowkv_prefix_attention_workspace": (ctypes.c_int, [ctypes.c_int32] * 11 + [_I64P]),
     "flowkv_copy_blocks": (ctypes.c_int, [_POOLP, ctypes.c_void_p, ctypes.c_void_p,
                                           ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                           ctypes.c_void_p]),
@@ -522,6 +544,8 @@ class KVPool:
         self.layout, self.num_layers, self.num_blocks = layout, L, B
         self.block_size, self.kv_heads, self.head_dim = bs, hkv, dh
         self.dtype = self.tensors[0].dtype            # (a pool's tensors have one type)
+        self.type_code = {torch.bfloat16: BF16, torch.float16: FP16,
+                          torch.float32: F32}.get(self.dtype)
         self.elem_bytes = self.tensors[0].element_size()
         self.chunk_bytes = bs * hkv * dh * self.elem_bytes
         self.block_bytes = 2 * L * self.chunk_bytes
@@ -808,6 +832,47 @@ def flowkv_append(pool: KVPool, layer: int, k, v, q_offsets, block_tables, seq_l
                     block_tables.data_ptr(), max_blocks, seq_lens.data_ptr())
 
 
+def flowkv_append_rotated(pool: KVPool, layer: int, k, v, cos_sin, q_offsets, block_tables,
+                          seq_lens, q=None, q_out=None, interleaved: bool = False,
+                          stream=None) -> None:
+    """``flowkv_append`` with K, and the queries, rotated by their positions on the way.
+    cos_sin: (positions, rot_dim) float32, contiguous: a position's rot_dim / 2 cosines, then
+    its sines; q, q_out: (n, Hq, Dh) of the pool's type (bfloat16, float16 or float32), strided
+    as k and v; q_out may be q.  Pairs are dims (j, j + rot_dim / 2), or neighbours with
+    ``interleaved``."""
+    import torch
+
+    n_req, max_blocks = _check_ragged(pool, q_offsets, block_tables, seq_lens)
+    h, d, dtype = pool.kv_heads, pool.head_dim, pool.dtype
+    if pool.type_code is None:
+        raise ValueError(f"rotation of bfloat16, float16 or float32: the pool holds {dtype}")
+    shape = k.shape
+    ks = _token_stride(k, shape, "k", h, d, dtype, pool)
+    vs = _token_stride(v, v.shape, "v", h, d, dtype, pool)
+    n = shape[0]
+    if v.shape[0] != n:
+        raise ValueError(f"{n} tokens of K and {v.shape[0]} of V")
+    angles = cos_sin.shape
+    if len(angles) != 2 or cos_sin.dtype is not torch.float32 or not cos_sin.is_contiguous() \
+            or cos_sin.get_device() != pool.index:
+        raise ValueError(f"cos_sin: need contiguous (positions, rot_dim) float32 on {pool.device}, "
+                         f"got {tuple(angles)} {cos_sin.dtype} on {cos_sin.device}")
+    hq = qs = os_ = q_at = out_at = 0
+    if q is not None:
+        if q_out is None:
+            raise ValueError("q without q_out")
+        hq = q.shape[1] if q.dim() == 3 else 0
+        qs = _token_stride(q, q.shape, "q", hq, d, dtype, pool)
+        os_ = _token_stride(q_out, q_out.shape, "q_out", hq, d, dtype, pool)
+        if q.shape[0] != n or q_out.shape[0] != n:
+            raise ValueError(f"{n} tokens of K, {q.shape[0]} of q and {q_out.shape[0]} of q_out")
+        q_at, out_at = q.data_ptr(), q_out.data_ptr()
+    _on_pool_device(pool, stream, "flowkv_append_rotated", _lib.flowkv_append_rotated, layer,
+                    pool.type_code, q_at, qs, out_at, os_, k.data_ptr(), ks, v.data_ptr(), vs, hq, h,
+                    d, cos_sin.data_ptr(), angles[0], angles[1], int(interleaved), n, n_req,
+                    q_offsets.data_ptr(), block_tables.data_ptr(), max_blocks, seq_lens.data_ptr())
+
+
 def flowkv_chunk_attention_workspace(n_tokens: int, n_req: int, q_heads: int, kv_heads: int,
                                      head_dim: int, max_new: int, max_seq_len: int,
                                      split_tokens: int = 0) -> int:
@@ -853,6 +918,96 @@ def flowkv_chunk_attention(pool: KVPool, layer: int, q, q_offsets, block_tables,
                     q.data_ptr(), qs, n, n_req, hq, pool.kv_heads, dh, q_offsets.data_ptr(),
                     block_tables.data_ptr(), max_blocks, seq_lens.data_ptr(), max_new,
                     max_seq_len, scale, split_tokens, out.data_ptr(), ws, ws_bytes)
+
+
+def _check_new_tokens(pool: KVPool, q, out, workspace) -> tuple:
+    """q, out and the workspace of attention in the pool's type: (tokens, query heads, head_dim,
+    elements between q's tokens, the workspace's address and bytes)."""
+    dtype, shape = pool.dtype, q.shape
+    if pool.type_code not in (BF16, FP16):
+        raise ValueError(f"attention reads bfloat16 or float16 K/V: the pool holds {dtype}")
+    if len(shape) != 3:
+        raise ValueError(f"q: need (tokens, heads, head_dim), got {tuple(shape)}")
+    n, hq, dh = shape
+    if dh != pool.head_dim:
+        raise ValueError(f"q has a head_dim of {dh}, the pool of {pool.head_dim}")
+    qs = _token_stride(q, shape, "q", hq, dh, dtype, pool)
+    if out.shape != shape or out.dtype is not dtype or not out.is_contiguous() \
+            or out.get_device() != pool.index:
+        raise ValueError(f"out: need contiguous {(n, hq, dh)} {dtype} on {pool.device}, got "
+                         f"{tuple(out.shape)} {out.dtype} on {out.device}")
+    if workspace is None:
+        return n, hq, dh, qs, 0, 0
+    if not workspace.is_contiguous() or workspace.get_device() != pool.index:
+        raise ValueError("attention workspace: not a contiguous tensor on the pool's device")
+    return n, hq, dh, qs, workspace.data_ptr(), workspace.nbytes
+
+
+def flowkv_window_attention_workspace(n_tokens: int, n_req: int, q_heads: int, kv_heads: int,
+                                      head_dim: int, max_new: int, max_seq_len: int, window: int,
+                                      sinks: int, split_tokens: int = 0) -> int:
+    b = ctypes.c_int64()
+    _check(_lib.flowkv_window_attention_workspace(n_tokens, n_req, q_heads, kv_heads, head_dim,
+                                                  max_new, max_seq_len, window, sinks,
+                                                  split_tokens, ctypes.byref(b)),
+           "flowkv_window_attention_workspace")
+    return b.value
+
+
+def flowkv_window_attention(pool: KVPool, layer: int, q, q_offsets, block_tables, seq_lens,
+                            max_new: int, max_seq_len: int, window: int, sinks: int,
+                            scale: float, out, workspace=None, split_tokens: int = 0,
+                            stream=None) -> None:
+    """``flowkv_chunk_attention`` in which a new token sees the last ``window`` tokens up to its
+    own and the first ``sinks``, over a bfloat16 or float16 pool (q and out of its type)."""
+    n_req, max_blocks = _check_ragged(pool, q_offsets, block_tables, seq_lens)
+    n, hq, dh, qs, ws, ws_bytes = _check_new_tokens(pool, q, out, workspace)
+    _on_pool_device(pool, stream, "flowkv_window_attention", _lib.flowkv_window_attention, layer,
+                    pool.type_code, q.data_ptr(), qs, n, n_req, hq, pool.kv_heads, dh,
+                    q_offsets.data_ptr(), block_tables.data_ptr(), max_blocks,
+                    seq_lens.data_ptr(), max_new, max_seq_len, window, sinks, scale, split_tokens,
+                    out.data_ptr(), ws, ws_bytes)
+
+
+def flowkv_prefix_attention_workspace(n_tokens: int, n_req: int, q_heads: int, kv_heads: int,
+                                      head_dim: int, n_groups: int, max_new: int, max_group: int,
+                                      max_own: int, max_prefix: int,
+                                      split_tokens: int = 0) -> int:
+    b = ctypes.c_int64()
+    _check(_lib.flowkv_prefix_attention_workspace(n_tokens, n_req, q_heads, kv_heads, head_dim,
+                                                  n_groups, max_new, max_group, max_own,
+                                                  max_prefix, split_tokens, ctypes.byref(b)),
+           "flowkv_prefix_attention_workspace")
+    return b.value
+
+
+def flowkv_prefix_attention(pool: KVPool, layer: int, q, q_offsets, block_tables, seq_lens,
+                            groups, prefix_lens, max_new: int, max_group: int, max_own: int,
+                            max_prefix: int, scale: float, out, workspace=None,
+                            split_tokens: int = 0, stream=None) -> None:
+    """``flowkv_chunk_attention`` of requests that share prefixes, each read once for its group:
+    requests groups[g] .. groups[g + 1] - 1 have the same first prefix_lens[g] tokens (int32
+    tensors of n_groups + 1 and n_groups on the pool's device).  max_new and max_group: the most
+    new tokens of a request and of a group; max_own: the most tokens behind a prefix; q and out
+    of the pool's type, bfloat16 or float16."""
+    import torch
+
+    n_req, max_blocks = _check_ragged(pool, q_offsets, block_tables, seq_lens)
+    n, hq, dh, qs, ws, ws_bytes = _check_new_tokens(pool, q, out, workspace)
+    n_groups = prefix_lens.shape[0] if prefix_lens.dim() == 1 else -1
+    for t, size in ((groups, n_groups + 1), (prefix_lens, n_groups)):
+        if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != size \
+                or not t.is_contiguous() or t.get_device() != pool.index:
+            raise ValueError(f"groups and prefix_lens: need contiguous int32 tensors of n + 1 and "
+                             f"n on {pool.device}, got {tuple(groups.shape)} {groups.dtype} on "
+                             f"{groups.device} and {tuple(prefix_lens.shape)} {prefix_lens.dtype} "
+                             f"on {prefix_lens.device}")
+    _on_pool_device(pool, stream, "flowkv_prefix_attention", _lib.flowkv_prefix_attention, layer,
+                    pool.type_code, q.data_ptr(), qs, n, n_req, hq, pool.kv_heads, dh,
+                    q_offsets.data_ptr(), block_tables.data_ptr(), max_blocks,
+                    seq_lens.data_ptr(), n_groups, groups.data_ptr(), prefix_lens.data_ptr(),
+                    max_new, max_group, max_own, max_prefix, scale, split_tokens, out.data_ptr(),
+                    ws, ws_bytes)
 
 
 def _address(a: np.ndarray) -> int:
