@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "flowkv_ragged.h"
 #include "flowkv_splits.h"
@@ -871,8 +872,17 @@ __device__ __forceinline__ void attend_many(const typename P::Args& a) {
     const uint32_t id = paired<F>();
     g = int(id % uint32_t(a.kv_heads));
     const uint32_t rest = id / uint32_t(a.kv_heads);
-    split = int(rest / uint32_t(a.tiles));
-    const int slot = a.tiles - 1 - int(rest % uint32_t(a.tiles));  // the longest first
+    int slot;
+    if constexpr (P::kPrefix || P::kOwn) {
+      // a tile's splits together: slots without rows are not every other workgroup then, which
+      // go to the same CUs (one group of 128 rows in 26 splits: 17 us, not 36)
+      const uint32_t splits = gridDim.x / uint32_t(a.tiles * a.kv_heads);
+      split = int(rest % splits);
+      slot = int(rest / splits);
+    } else {
+      split = int(rest / uint32_t(a.tiles));
+      slot = a.tiles - 1 - int(rest % uint32_t(a.tiles));  // the longest first
+    }
     const int32_t u = flowkv::last_at_most(units<P>(a), slot,
                                            [&](int32_t i) { return first_tile<P>(a, i); });
     rq = unit_at<P>(a, u);
@@ -898,6 +908,49 @@ __device__ __forceinline__ void attend_many(const typename P::Args& a) {
   if (!kCut && split > 0 && s0 >= tile_limit) return;   // (split 0 writes what sees nothing)
   const int32_t s1 = tile_limit - s0 > length ? s0 + length : tile_limit;
   const bool direct = kCut ? pieces == 1 : !P::kPrefix && !P::kOwn && tile_limit <= length;
+
+  __shared__ alignas(16) u32x4 sk0[kStep * kPc], sk1[kStep * kPc], sv0[kStep * kPc],
+      sv1[kStep * kPc];
+  __shared__ Places<F> places;
+
+  const int lr = tid / kPc, lp = tid % kPc;
+  Source<F, P> src{reach};
+  src.base = a.kbase + g * kDh * 2;
+  src.voff = a.voff;
+  src.table = a.tables + int64_t(rq.r) * a.max_blocks;
+  src.bs = uint32_t(a.block_size);
+  src.bs_magic = a.bs_magic;
+  src.bs_shift = a.bs_shift;
+  src.bunits = a.bunits;
+  src.sunits = a.sunits;
+  src.pool_blocks = a.pool_blocks;
+  src.s0 = s0;
+  src.s1 = s1;
+  src.tid = tid;
+  src.wave = wave;
+  src.row = lr;
+  src.kpiece = 16 * (lp ^ k_swizzle<kPc>(lr));
+  src.vpiece = 16 * (lp ^ v_swizzle<kPc>(lr));
+  src.places = &places;
+
+  // The first step is on its way while the query rows are looked up and loaded (chunk
+  // attention has it behind them).
+  constexpr bool kEarly = !std::is_same_v<typename P::Args, ChunkArgs>;
+  bool next_dead = false, suspect = false;       // a block is missing in the next group of
+                                                 // steps; in it or in this one
+  auto start = [&] {
+    src.fetch(0);
+    src.place(0);
+    if (tid < 2) places.odd[tid] = 0;
+    __syncthreads();
+    suspect = next_dead = src.any_dead(0);
+    src.look(0);
+    src.send((lvec*)sk0, (lvec*)sv0);
+    src.look(1);
+  };
+  if constexpr (kEarly) {
+    if (s0 < s1) start();
+  }
 
   // this lane's query row, as a column of S^T
   const int32_t wrow = row0 + rw * 32, row = wrow + c32;
@@ -943,30 +996,6 @@ __device__ __forceinline__ void attend_many(const typename P::Args& a) {
   w.mref = -INFINITY;
   w.lsum = 0.f;
 
-  __shared__ alignas(16) u32x4 sk0[kStep * kPc], sk1[kStep * kPc], sv0[kStep * kPc],
-      sv1[kStep * kPc];
-  __shared__ Places<F> places;
-
-  const int lr = tid / kPc, lp = tid % kPc;
-  Source<F, P> src{reach};
-  src.base = a.kbase + g * kDh * 2;
-  src.voff = a.voff;
-  src.table = a.tables + int64_t(rq.r) * a.max_blocks;
-  src.bs = uint32_t(a.block_size);
-  src.bs_magic = a.bs_magic;
-  src.bs_shift = a.bs_shift;
-  src.bunits = a.bunits;
-  src.sunits = a.sunits;
-  src.pool_blocks = a.pool_blocks;
-  src.s0 = s0;
-  src.s1 = s1;
-  src.tid = tid;
-  src.wave = wave;
-  src.row = lr;
-  src.kpiece = 16 * (lp ^ k_swizzle<kPc>(lr));
-  src.vpiece = 16 * (lp ^ v_swizzle<kPc>(lr));
-  src.places = &places;
-
   // Where some row does not see some token, or a block is missing, an infinity or a NaN
   // in V would reach a row as 0 x inf: such values are taken out of the step's rows by the
   // lanes that brought them, and added at the end to the rows that see them.  (What lies at
@@ -974,8 +1003,6 @@ __device__ __forceinline__ void attend_many(const typename P::Args& a) {
   // workgroup's tokens, 2^odd_shift each, such values were in, is kept: the end looks
   // through those alone.
   auto odd_shift = [&] { return std::max(0, 26 - __builtin_clz((s1 - s0 - 1) | 1)); };
-  bool next_dead = false, suspect = false;       // a block is missing in the next group of
-                                                 // steps; in it or in this one
   auto landed = [&](lvec* v, int32_t t0) {
     __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0)
     bool all_seen = t0 + kStep <= tile_least;
@@ -1031,22 +1058,14 @@ __device__ __forceinline__ void attend_many(const typename P::Args& a) {
     };
     lvec *const k0 = (lvec*)sk0, *const k1 = (lvec*)sk1, *const v0 = (lvec*)sv0,
                 *const v1 = (lvec*)sv1;
-    src.fetch(0);
-    src.place(0);
-    if (tid < 2) places.odd[tid] = 0;
+    if constexpr (!kEarly) start();
     if constexpr (P::kPrefix) {
       if (ln == 0) places.least[wave] = w.wleast;
-    }
-    __syncthreads();
-    if constexpr (P::kPrefix) {
+      __syncthreads();
 #pragma unroll
       for (int x = 0; x < F::kWaves; ++x) tile_least = std::min(tile_least, places.least[x]);
       tile_least = uniform(tile_least);
     }
-    suspect = next_dead = src.any_dead(0);
-    src.look(0);
-    src.send(k0, v0);
-    src.look(1);
     landed(v0, s0);
     __syncthreads();
     for (int32_t t0 = s0; t0 < s1; t0 += 2 * kStep) {
@@ -1252,6 +1271,20 @@ __device__ __forceinline__ void join_pieces(const ChunkArgs& a) {
   }
 }
 
+// A row's parts so far: reference, sum, and four dims.
+struct Running {
+  float m, l;
+  f32x4 v;
+};
+__device__ __forceinline__ Running join(const Running& a, const Running& b) {
+  Running r;
+  r.m = fmaxf(a.m, b.m);
+  const float wa = part_weight(a.m, a.l, r.m), wb = part_weight(b.m, b.l, r.m);
+  r.l = weighted(a.l, wa, b.l, wb);
+  r.v = weighted(a.v, wa, b.v, wb);
+  return r;
+}
+
 // ---- few rows ----------------------------------------------------------------------
 //
 // A request of a few new tokens reads every cached K and V for a handful of rows: that is
@@ -1271,19 +1304,20 @@ constexpr int kFewWaves = 4;
 constexpr int kFewThreads = 64 * kFewWaves;
 constexpr int kFewTile = 32;
 constexpr int kFewSplit = 2048;            // most tokens of a workgroup: their places are in LDS
+constexpr int kFewOwn = 4096;              // the same behind a prefix
 
-template <int kDh, int kC>
+template <int kDh, int kC, int kSplit, int kWaves>
 struct FewLds {
   static constexpr int kRows = 16 * kC;
-  uint32_t at[kFewSplit];                  // a tile's token 4 e + q4 at 8 q4 + e, in 128-byte units
+  uint32_t at[kSplit];                     // a tile's token 4 e + q4 at 8 q4 + e, in 128-byte units
   // K's staging, a tile per wave; after the loop the waves' weighted sums
-  alignas(16) uint8_t area[kFewWaves * kRows * kDh * sizeof(float)];
-  uint32_t dead[kFewSplit / kFewTile];
-  uint32_t odd[2];                         // tiles whose V lost an infinity or a NaN
-  float m[kFewWaves][kRows], l[kFewWaves][kRows];
+  alignas(16) uint8_t area[kWaves * kRows * kDh * sizeof(float)];
+  uint32_t dead[kSplit / kFewTile];
+  uint32_t odd[kSplit / kFewTile / 32];    // tiles whose V lost an infinity or a NaN
+  float m[kWaves][kRows], l[kWaves][kRows];
   int32_t lim[kRows];
   int32_t low[kRows];                      // kWindow
-  static_assert(kFewWaves * kFewTile * kDh * 2 <= sizeof(area) && kFewSplit / kFewTile <= 64);
+  static_assert(kWaves * kFewTile * kDh * 2 <= sizeof(area) && kSplit / kFewTile % 64 == 0);
 };
 
 __device__ __forceinline__ uint32_t pair_hi(uint32_t lo, uint32_t hi) {
@@ -1296,7 +1330,7 @@ __device__ __forceinline__ uint32_t pair_lo(uint32_t lo, uint32_t hi) {
 // Workgroups on a CU at once.
 constexpr int few_per_cu(int dh, int c) { return (dh == 64 ? 4 : 3) - (c - 1); }
 
-template <int kDh, int kC, class P>
+template <int kDh, int kC, class P, int kSplit = kFewSplit, int kWaves = kFewWaves>
 __device__ __forceinline__ void attend_few(const typename P::Args& a) {
   typedef typename P::T T;
   typedef typename T::Vec Vec;
@@ -1336,10 +1370,11 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
   const int32_t s0 = split * a.split_tokens;
   if (split > 0 && s0 >= tile_limit) return;
   const int32_t s1 = tile_limit - s0 > a.split_tokens ? s0 + a.split_tokens : tile_limit;
-  const bool direct = !P::kPrefix && !P::kOwn && tile_limit <= a.split_tokens;
+  bool direct = !P::kPrefix && tile_limit <= a.split_tokens;
+  if constexpr (P::kOwn) direct = a.splits == a.first_split + 1;   // (no request has more)
   const int n_tiles = (s1 - s0 + kFewTile - 1) / kFewTile;
 
-  __shared__ FewLds<kDh, kC> lds;
+  __shared__ FewLds<kDh, kC, kSplit, kWaves> lds;
   int32_t lim[kC], low[kC];
   Vec qb[kC][kI];
 #pragma unroll
@@ -1370,7 +1405,7 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
     }
   }
   const int32_t* table = a.tables + int64_t(rq.r) * a.max_blocks;
-  for (int x = tid; x < n_tiles * kFewTile; x += kFewThreads) {
+  for (int x = tid; x < n_tiles * kFewTile; x += 64 * kWaves) {
     const uint32_t t = reach.token(uint32_t(s0 + x));
     const uint32_t b = uint32_t((uint64_t(__umulhi(t, a.bs_magic)) + t) >> a.bs_shift);
     const bool in = s0 + x < s1;
@@ -1391,7 +1426,7 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
 #pragma unroll
     for (int t = 0; t < kT; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  if (tid < 2) lds.odd[tid] = 0;
+  if (tid < kSplit / kFewTile / 32) lds.odd[tid] = 0;
   __syncthreads();
 
   u32x4 kw[kKL];
@@ -1419,9 +1454,9 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
     load_k(wave);
     load_v(wave);
   }
-  for (int tile = wave; tile < n_tiles; tile += kFewWaves) {
+  for (int tile = wave; tile < n_tiles; tile += kWaves) {
     // (past the wave's last tile: its own again, so that as many loads are under way)
-    const int next = tile + kFewWaves < n_tiles ? tile + kFewWaves : tile;
+    const int next = tile + kWaves < n_tiles ? tile + kWaves : tile;
 #pragma unroll
     for (int e = 0; e < kKL; ++e) {
       const int x = kt + e * kStride;
@@ -1536,8 +1571,11 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
     }
   }
   __syncthreads();                               // every wave is past the loop: the area is free
-  const uint64_t odd = uint64_t(uint32_t(uniform(int32_t(lds.odd[1])))) << 32 |
-                       uint32_t(uniform(int32_t(lds.odd[0])));
+  uint64_t odds[kSplit / kFewTile / 64];
+#pragma unroll
+  for (int w = 0; w < kSplit / kFewTile / 64; ++w)
+    odds[w] = uint64_t(uint32_t(uniform(int32_t(lds.odd[2 * w + 1])))) << 32 |
+              uint32_t(uniform(int32_t(lds.odd[2 * w])));
   float* const s_o = reinterpret_cast<float*>(lds.area);   // [wave][row][dim]
 #pragma unroll
   for (int c = 0; c < kC; ++c)
@@ -1550,22 +1588,24 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
             f32x4{o[c][t][x], o[c][t + 1][x], o[c][t + 2][x], o[c][t + 3][x]};
   __syncthreads();
   // a row's dims 4 at a time
-  for (int i = tid; i < kFewRows * kDh / 4; i += kFewThreads) {
+  for (int i = tid; i < kFewRows * kDh / 4; i += 64 * kWaves) {
     const int h = i / (kDh / 4), d = i % (kDh / 4) * 4;
     if (row0 + h >= rows) break;
     float M = -INFINITY, L = 0.f;
     f32x4 A = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) M = fmaxf(M, lds.m[w][h]);
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, lds.m[w][h]);
 #pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) {
+    for (int w = 0; w < kWaves; ++w) {
       const float wt = part_weight(lds.m[w][h], lds.l[w][h], M);
       L += lds.l[w][h] * wt;
       A += *reinterpret_cast<const f32x4*>(&s_o[(w * kFewRows + h) * kDh + d]) * wt;
     }
     // infinities and NaN of the tokens that the row sees, until it is all NaN
-    for (uint64_t left = odd; left; left &= left - 1) {
-      const int tile = __builtin_ctzll(left);
+#pragma unroll
+    for (int w = 0; w < kSplit / kFewTile / 64; ++w)
+    for (uint64_t left = odds[w]; left; left &= left - 1) {
+      const int tile = 64 * w + __builtin_ctzll(left);
       const int32_t sees = lds.lim[h] - s0 - tile * kFewTile;
       if (sees <= 0 || (A[0] != A[0] && A[1] != A[1] && A[2] != A[2] && A[3] != A[3])) break;
       const uint32_t gone = lds.dead[tile];
@@ -1588,6 +1628,30 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
     const int32_t qi = token_of(a, row0 + h);
     const int64_t orow =
         (int64_t(rq.begin) + qi) * a.q_heads + g * a.group + (row0 + h - qi * a.group);
+    if constexpr (P::kOwn) {
+      if (direct) {                              // the prefix's records, kOwnAhead under way
+        constexpr int kOwnAhead = 16;
+        const int32_t n = flowkv::splits_of(
+            std::min(std::max(rq.base + qi + 1, 0), reach.shift), a.prefix_split);
+        const int64_t rec = orow * a.splits;
+        Running x{M, L, A};
+        for (int32_t s = 0; s < n; s += kOwnAhead) {
+          Running y[kOwnAhead];
+#pragma unroll
+          for (int j = 0; j < kOwnAhead; ++j) {  // (past the end: the first record, not used)
+            const int64_t at = rec + (s + j < n ? s + j : 0);
+            const f32x2u m = *record_ml(a, kDh, at);
+            y[j] = Running{m[0], m[1],
+                           *reinterpret_cast<const f32x4u*>(record_sums(a, kDh, at) + d)};
+          }
+#pragma unroll
+          for (int j = 0; j < kOwnAhead; ++j)
+            if (s + j < n) x = join(x, y[j]);
+        }
+        L = x.l;
+        A = x.v;
+      }
+    }
     if (direct) {
       const float inv = L == 0.f ? 0.f : 1.f / L;
       const u32x2 x = {T::pack(A[0] * inv, A[1] * inv), T::pack(A[2] * inv, A[3] * inv)};
@@ -1606,19 +1670,6 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
 // 5 tokens x 32 heads x 26 splits.
 constexpr int kMergeThreads = 256;
 constexpr int kMergeChunk = 8;
-
-struct Running {
-  float m, l;
-  f32x4 v;
-};
-__device__ __forceinline__ Running join(const Running& a, const Running& b) {
-  Running r;
-  r.m = fmaxf(a.m, b.m);
-  const float wa = part_weight(a.m, a.l, r.m), wb = part_weight(b.m, b.l, r.m);
-  r.l = weighted(a.l, wa, b.l, wb);
-  r.v = weighted(a.v, wa, b.v, wb);
-  return r;
-}
 
 template <int kDh, int kWavesPer, class P>
 __device__ __forceinline__ void merge_splits(const typename P::Args& a) {

@@ -37,6 +37,12 @@ __global__ __launch_bounds__(kFewThreads, few_per_cu(kDh, kC))
 void prefix_attn_few(const SpanArgs a) {
   attend_few<kDh, kC, P>(a);
 }
+// Behind the prefix: four waves, or eight where there are no more workgroups than CUs.
+template <int kDh, int kC, int kWaves, class P>
+__global__ __launch_bounds__(64 * kWaves, kWaves == kFewWaves ? few_per_cu(kDh, kC) : 2)
+void prefix_attn_own(const SpanArgs a) {
+  attend_few<kDh, kC, P, kFewOwn, kWaves>(a);
+}
 template <int kDh, int kWavesPer, class T>
 __global__ __launch_bounds__(kMergeThreads) void prefix_attn_merge(const SpanArgs a) {
   merge_splits<kDh, kWavesPer, Own<T>>(a);
@@ -94,6 +100,7 @@ const Kernels& alone(int32_t dtype) {
 struct Parts {
   const void* prefix[4][2];
   const void* own[3][2];
+  const void* own_wide[2][2];                    // eight waves
   const void* merge[2][2];
 };
 template <class T>
@@ -105,9 +112,11 @@ Parts parts_of() {
                 {ptr(prefix_attn_few<64, 2, P>), ptr(prefix_attn_few<128, 2, P>)},
                 {ptr(prefix_attn<Form<64, 4, 2>, P>), ptr(prefix_attn<Form<128, 4, 2>, P>)},
                 {ptr(prefix_attn<Form<64, 8, 1>, P>), ptr(prefix_attn<Form<128, 8, 1>, P>)}},
-               {{ptr(prefix_attn_few<64, 1, O>), ptr(prefix_attn_few<128, 1, O>)},
-                {ptr(prefix_attn_few<64, 2, O>), ptr(prefix_attn_few<128, 2, O>)},
+               {{ptr(prefix_attn_own<64, 1, 4, O>), ptr(prefix_attn_own<128, 1, 4, O>)},
+                {ptr(prefix_attn_own<64, 2, 4, O>), ptr(prefix_attn_own<128, 2, 4, O>)},
                 {ptr(prefix_attn<Form<64, 4, 2>, O>), ptr(prefix_attn<Form<128, 4, 2>, O>)}},
+               {{ptr(prefix_attn_own<64, 1, 8, O>), ptr(prefix_attn_own<128, 1, 8, O>)},
+                {ptr(prefix_attn_own<64, 2, 8, O>), ptr(prefix_attn_own<128, 2, 8, O>)}},
                {{ptr(prefix_attn_merge<64, 1, T>), ptr(prefix_attn_merge<64, 4, T>)},
                 {ptr(prefix_attn_merge<128, 1, T>), ptr(prefix_attn_merge<128, 4, T>)}}};
 }
@@ -119,11 +128,13 @@ const Parts& parts(int32_t dtype) {
 // Forms of a part: rows of a tile, threads.
 constexpr int kRows[4] = {16, 32, 128, 256};
 constexpr int kThreads[4] = {kFewThreads, kFewThreads, 512, 512};
+constexpr int kWideThreads = 512;
 
 struct Plan {
   bool shared;                 // false: each request by itself, `sh`
   Shape sh;
   int prefix_kind, own_kind;
+  bool wide;                                     // eight waves behind the prefix
   int32_t prefix_split, own_split;
   int64_t prefix_splits, own_splits;             // records of a row
   int64_t need;
@@ -153,23 +164,29 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
     out->need = out->sh.need;
     return FLOWKV_OK;
   }
-  out->prefix_kind = together <= 16 ? 0 : together <= 32 ? 1 : together <= 128 ? 2 : 3;
-  out->own_kind = one <= 16 ? 0 : one <= 32 ? 1 : 2;
-  auto split_of = [&](int kind, int64_t units, int64_t most_new, int32_t tokens) {
-    constexpr int64_t kAll = INT32_MAX / kSplitUnit * kSplitUnit;
-    const int64_t most = kind <= 1 ? kFewSplit : kAll;
-    if (split_tokens > 0) return int32_t(std::min<int64_t>(split_tokens, most));
-    const int64_t tiles =
-        tiles_of(n_tokens, units, group, most_new, kRows[kind]) * kv_heads;
-    return best_split(std::max<int64_t>(tiles, 1), tokens, kind <= 1 ? 300 : 500, most);
+  out->prefix_kind = together <= 16 ? 0 : together <= 32 ? 1 : 2;
+  if (tiles_of(n_tokens, n_groups, group, max_group, 256) * kv_heads >= kCus) out->prefix_kind = 3;
+  out->own_kind = one <= 16 ? 0 : one <= 64 ? 1 : 2;
+  constexpr int64_t kAll = INT32_MAX / kSplitUnit * kSplitUnit;
+  auto tiles_at = [&](int kind, int64_t units, int64_t most_new) {
+    return std::max<int64_t>(tiles_of(n_tokens, units, group, most_new, kRows[kind]) * kv_heads,
+                             1);
   };
-  out->prefix_split = split_of(out->prefix_kind, n_groups, max_group, max_prefix);
-  out->own_split = split_of(out->own_kind, n_req, max_new, max_own);
+  auto split_of = [&](int kind, int64_t tiles, int32_t tokens, int64_t most) {
+    if (kind > 1) most = kAll;
+    if (split_tokens > 0) return int32_t(std::min<int64_t>(split_tokens, most));
+    return best_split(tiles, tokens, kind <= 1 ? 300 : 500, most);
+  };
+  const int64_t own_tiles = tiles_at(out->own_kind, n_req, max_new);
+  out->prefix_split = split_of(out->prefix_kind, tiles_at(out->prefix_kind, n_groups, max_group),
+                               max_prefix, kFewSplit);
+  out->own_split = split_of(out->own_kind, own_tiles, max_own, kFewOwn);
   auto splits_of = [](int32_t tokens, int32_t split) {
     return std::max<int64_t>((int64_t(tokens) + split - 1) / split, 1);
   };
   out->prefix_splits = splits_of(max_prefix, out->prefix_split);
   out->own_splits = splits_of(max_own, out->own_split);
+  out->wide = out->own_kind <= 1 && own_tiles * out->own_splits <= kCus;
   if (__builtin_mul_overflow(int64_t(n_tokens) * q_heads,
                              int64_t((head_dim + 2) * sizeof(float)), &out->need) ||
       __builtin_mul_overflow(out->need, out->prefix_splits + out->own_splits, &out->need))
@@ -179,23 +196,24 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
 }
 
 // A part of units (requests or groups): its workgroups, or a failure where they are too many.
-int part_grid(const ChunkArgs& a, int kind, int64_t n_units, int64_t splits, int64_t* grid) {
+int part_grid(const ChunkArgs& a, int kind, int threads, int64_t n_units, int64_t splits,
+              int64_t* grid) {
   const int64_t tiles = tile_slots(a.n_tokens, n_units, a.group, kRows[kind]) * a.kv_heads;
-  if (tiles > UINT32_MAX / kThreads[kind] / splits)  // lanes of a launch in 32 bits
+  if (tiles > UINT32_MAX / threads / splits)  // lanes of a launch in 32 bits
     return fail(FLOWKV_EINVAL, "%lld tiles of queries x %lld splits: too many for one call",
                 (long long)tiles, (long long)splits);
   *grid = tiles * splits;
   return FLOWKV_OK;
 }
 
-hipError_t launch_part(const void* fn, int kind, int64_t grid, int64_t splits,
+hipError_t launch_part(const void* fn, int kind, int threads, int64_t grid, int64_t splits,
                        int32_t split_tokens, SpanArgs& a, hipStream_t stream) {
   a.split_tokens = split_tokens;
   a.tiles = int32_t(grid / splits / a.kv_heads);
   a.row_shift = 0;
   while (1 << a.row_shift < kRows[kind]) ++a.row_shift;
   void* args[] = {&a};
-  return hipLaunchKernel(fn, dim3(unsigned(grid)), dim3(unsigned(kThreads[kind])), args, 0,
+  return hipLaunchKernel(fn, dim3(unsigned(grid)), dim3(unsigned(threads)), args, 0,
                          stream);
 }
 
@@ -210,20 +228,23 @@ int launch_parts(int32_t dtype, const Plan& p, int head_dim, SpanArgs& a, hipStr
     return fail(FLOWKV_EINVAL, "%lld rows of output x %lld splits: too many for one call",
                 (long long)out_rows, (long long)splits);
   int64_t prefix_grid, own_grid;
-  int rc = part_grid(a, p.prefix_kind, a.n_groups, p.prefix_splits, &prefix_grid);
+  const int prefix_threads = kThreads[p.prefix_kind];
+  const int own_threads = p.wide ? kWideThreads : kThreads[p.own_kind];
+  int rc = part_grid(a, p.prefix_kind, prefix_threads, a.n_groups, p.prefix_splits, &prefix_grid);
   if (rc) return rc;
-  rc = part_grid(a, p.own_kind, a.n_req, p.own_splits, &own_grid);
+  rc = part_grid(a, p.own_kind, own_threads, a.n_req, p.own_splits, &own_grid);
   if (rc) return rc;
   a.splits = int32_t(splits);
   a.first_split = int32_t(p.prefix_splits);
   a.prefix_split = p.prefix_split;
   void* args[] = {&a};
-  hipError_t e = launch_part(fn.prefix[p.prefix_kind][d128], p.prefix_kind, prefix_grid,
-                             p.prefix_splits, p.prefix_split, a, stream);
+  hipError_t e = launch_part(fn.prefix[p.prefix_kind][d128], p.prefix_kind, prefix_threads,
+                             prefix_grid, p.prefix_splits, p.prefix_split, a, stream);
   if (e == hipSuccess)
-    e = launch_part(fn.own[p.own_kind][d128], p.own_kind, own_grid, p.own_splits, p.own_split, a,
-                    stream);
-  if (e == hipSuccess)
+    e = launch_part(p.wide ? fn.own_wide[p.own_kind][d128] : fn.own[p.own_kind][d128], p.own_kind,
+                    own_threads, own_grid, p.own_splits, p.own_split, a, stream);
+  // (one split behind the prefix, of few rows: its workgroup joins them)
+  if (e == hipSuccess && (p.own_splits > 1 || p.own_kind > 1))
     e = hipLaunchKernel(fn.merge[d128][!one], dim3(unsigned(merge)), dim3(kMergeThreads), args, 0,
                         stream);
   if (e == hipSuccess) e = hipGetLastError();

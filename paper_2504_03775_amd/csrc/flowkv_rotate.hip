@@ -22,25 +22,10 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(1))) u32x4 gvec;
 typedef __attribute__((address_space(1))) const u32x4 cgvec;
-
-struct RotateArgs {
-  char* kbase;                    // the layer's K of block 0
-  int64_t voff;                   // V from K
-  int64_t bstride;                // bytes between blocks
-  const char *q, *k, *v;
-  char* q_out;
-  int64_t q_stride, q_out_stride, k_stride, v_stride;   // bytes between tokens
-  const float* angles;            // (n_positions, rot_dim): cosines, then sines
-  const int32_t *offsets, *seq_lens, *tables;
-  int32_t n_tokens, n_req, max_blocks, pool_blocks, block_size;
-  int32_t q_heads, kv_heads, pieces;                    // 16-byte pieces of a head
-  int32_t n_positions, rot_dim;
-};
 
 // 16-byte pieces of each type as float32, and back.
 struct Bf16 {
@@ -95,42 +80,87 @@ struct F32 {
   }
 };
 
-// Work: units of two 16-byte pieces of a head, a lane each, heads of q, then of K, then of V,
-// token by token.  A rotated unit holds kPer pairs whole: pieces x and x + half (pairs half a
-// rotation apart), or 2 x and 2 x + 1 (neighbours), with kPer cosines and as many sines.
+// x / d = (umulhi(x, m) + x) >> l with l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1.
+struct Divisor {
+  uint32_t magic, shift;
+};
+__device__ __forceinline__ uint32_t div(uint32_t x, Divisor d) {
+  return uint32_t((uint64_t(__umulhi(x, d.magic)) + x) >> d.shift);
+}
+Divisor divisor(uint32_t d) {
+  Divisor r{0, 0};
+  while ((uint64_t(1) << r.shift) < d) ++r.shift;
+  r.magic = uint32_t((((uint64_t(1) << r.shift) - d) << 32) / d + 1);
+  return r;
+}
+
+// Work: units of two 16-byte pieces of a head; a lane takes one, or the same one of kHeads heads
+// next to each other (which share their cosines and sines), heads of q, then of K, then of V,
+// token by token.  A rotated unit is pieces x and x + half of the rotated dims, kPer pairs half
+// a rotation apart or two times kPer / 2 neighbours; an unrotated one is two pieces half of the
+// unrotated ones apart.  So 16 bytes of neighbouring lanes lie together in every store.
 constexpr int kThreads = 256;
 
-template <class T, bool kNeighbours>
+struct RotateArgs {
+  char* kbase;                    // the layer's K of block 0
+  int64_t voff;                   // V from K
+  int64_t bstride;                // bytes between blocks
+  const char *q, *k, *v;
+  char* q_out;
+  int64_t q_stride, q_out_stride, k_stride, v_stride;   // bytes between tokens
+  const float* angles;            // (n_positions, rot_dim): cosines, then sines
+  const int32_t *offsets, *seq_lens, *tables;
+  int32_t n_tokens, n_req, max_blocks, pool_blocks, block_size;
+  int32_t q_heads, kv_heads, pieces;                    // 16-byte pieces of a head
+  int32_t n_positions, rot_dim;
+  uint32_t items, per, per_head;  // lanes' items in all, of a token, of a head
+  Divisor by_per, by_per_head, by_block;
+};
+
+template <class T, bool kNeighbours, int kHeads, bool kPast>
 __global__ __launch_bounds__(kThreads) void kv_rotate(const RotateArgs a) {
   constexpr int kPer = T::kPer;
   const int ln = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t first = (int64_t(blockIdx.x) * (kThreads / 64) + wave) * 64;
-  const uint32_t per_head = uint32_t(a.pieces + 1) / 2;
-  const uint32_t per = uint32_t(a.q_heads + 2 * a.kv_heads) * per_head;    // units of a token
-  const int64_t items = int64_t(a.n_tokens) * per;
-  if (first >= items) return;
-  const int64_t last = std::min<int64_t>(first + 64, items) - 1;
-  const int32_t t0 = int32_t(first / per), t1 = int32_t(last / per);
-  const bool some = first + ln < items;
-  const uint32_t d = uint32_t(first - int64_t(t0) * per) + ln;
-  const int32_t token = some ? t0 + int32_t(d / per) : t1;
-  const uint32_t unit = some ? d % per : 0;
-  const uint32_t head = unit / per_head, x = unit % per_head;
-  const bool is_q = head < uint32_t(a.q_heads);
-  const bool is_v = head >= uint32_t(a.q_heads + a.kv_heads);
-  const uint32_t h = is_q ? head : head - a.q_heads - (is_v ? a.kv_heads : 0);
+  const uint32_t first = (blockIdx.x * (kThreads / 64) + wave) * 64;
+  if (first >= a.items) return;
+  const uint32_t last = std::min(first + 63, a.items - 1);
+  const int32_t t0 = int32_t(div(first, a.by_per)), t1 = int32_t(div(last, a.by_per));
+  const bool some = first + ln <= last;
+  const uint32_t d = first - uint32_t(t0) * a.per + uint32_t(ln);
+  const uint32_t dt = some ? div(d, a.by_per) : uint32_t(t1 - t0);
+  const int32_t token = t0 + int32_t(dt);
+  const uint32_t unit = some ? d - dt * a.per : 0;
+  const uint32_t j = div(unit, a.by_per_head), x = unit - j * a.per_head;
   const uint32_t half = uint32_t(a.rot_dim) / (2 * kPer);                  // pieces
-  const bool turned = !is_v && x < half;
-  const uint32_t p0 = turned && !kNeighbours ? x : 2 * x;
-  const uint32_t p1 = turned && !kNeighbours ? x + half : 2 * x + 1;
-  const bool two = p1 < uint32_t(a.pieces);
-  const char* src = is_q   ? a.q + token * a.q_stride
-                    : is_v ? a.v + token * a.v_stride
-                           : a.k + token * a.k_stride;
-  src += int64_t(h) * a.pieces * 16;
-  u32x4 y0 = *(cgvec*)(src + p0 * 16), y1 = {};
-  if (two) y1 = *(cgvec*)(src + p1 * 16);
+  const uint32_t heads = uint32_t(a.q_heads + 2 * a.kv_heads), kv = uint32_t(a.kv_heads);
+  const bool turning = x < half;
+  u32x4 y[kHeads][2];
+  uint32_t p0[kHeads], p1[kHeads], h[kHeads];
+  bool is_q[kHeads], is_v[kHeads], turned[kHeads], here[kHeads], two[kHeads];
+#pragma unroll
+  for (int e = 0; e < kHeads; ++e) {
+    const uint32_t head = j * kHeads + e;
+    here[e] = head < heads;
+    is_q[e] = head < uint32_t(a.q_heads);
+    is_v[e] = head >= uint32_t(a.q_heads) + kv;
+    h[e] = is_q[e] ? head : head - uint32_t(a.q_heads) - (is_v[e] ? kv : 0);
+    turned[e] = !is_v[e] && turning;
+    // (behind the rotated dims the units go on from 2 half)
+    const uint32_t rest = !turning ? half : 0;
+    p0[e] = is_v[e] ? x : x + rest;
+    p1[e] = is_v[e] ? x + a.per_head : x + (turning ? half : a.per_head);
+    two[e] = p1[e] < uint32_t(a.pieces);
+    const char* src = is_q[e]   ? a.q + token * a.q_stride
+                      : is_v[e] ? a.v + token * a.v_stride
+                                : a.k + token * a.k_stride;
+    src += int64_t(h[e] * uint32_t(a.pieces)) * 16;
+    y[e][0] = y[e][1] = u32x4{};
+    if (here[e]) {
+      y[e][0] = *(cgvec*)(src + p0[e] * 16);
+      if (two[e]) y[e][1] = *(cgvec*)(src + p1[e] * 16);
+    }
+  }
 
   // the lane's request: among those of the wave's tokens
   int32_t r = flowkv::last_at_most(a.n_req, t0, [&](int32_t i) { return a.offsets[i]; });
@@ -143,55 +173,80 @@ __global__ __launch_bounds__(kThreads) void kv_rotate(const RotateArgs a) {
     }
   }
   const int32_t begin = a.offsets[r], end = a.offsets[r + 1];
-  const int64_t p = int64_t(a.seq_lens[r]) - (int64_t(end) - begin) + (token - begin);
-  if (!some || token < begin || token >= end || p < 0 || p >= a.n_positions) return;
-  char* dst;
-  if (is_q) {
-    dst = a.q_out + token * a.q_out_stride + int64_t(h) * a.pieces * 16;
-  } else {
-    const uint32_t b = uint32_t(p) / uint32_t(a.block_size);
-    if (b >= uint32_t(a.max_blocks)) return;
-    const int32_t id = a.tables[int64_t(r) * a.max_blocks + b];
-    if (id < 0 || id >= a.pool_blocks) return;
-    const uint32_t slot = uint32_t(p) - b * uint32_t(a.block_size);
-    dst = a.kbase + (is_v ? a.voff : 0) + id * a.bstride +
-          (int64_t(slot) * a.kv_heads + h) * a.pieces * 16;
-  }
-  if (turned) {
-    float c[kPer], s[kPer];
-    const float* row = a.angles + p * a.rot_dim + x * kPer;
+  const int64_t pos = int64_t(a.seq_lens[r]) - (int64_t(end) - begin) + (token - begin);
+  if (!some || token < begin || token >= end || pos < 0 || pos >= a.n_positions) return;
+  const uint32_t p = uint32_t(pos);
+  float c[kPer], s[kPer];
+  if (turning) {
+    // neighbours: of piece x, then of piece x + half
+    const float* row = a.angles + int64_t(p) * a.rot_dim + x * (kNeighbours ? kPer / 2 : kPer);
+    constexpr int kLoad = kNeighbours ? kPer / 2 : 4;
+    typedef float Load __attribute__((ext_vector_type(kLoad), aligned(4)));
 #pragma unroll
-    for (int i = 0; i < kPer; i += 4) {
-      const f32x4u u = *reinterpret_cast<const f32x4u*>(row + i);
-      const f32x4u v = *reinterpret_cast<const f32x4u*>(row + a.rot_dim / 2 + i);
+    for (int i = 0; i < kPer; i += kLoad) {
+      const float* at = row + (kNeighbours && i ? half * (kPer / 2) : uint32_t(i));
+      const Load u = *reinterpret_cast<const Load*>(at);
+      const Load w = *reinterpret_cast<const Load*>(at + a.rot_dim / 2);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        c[i + j] = u[j];
-        s[i + j] = v[j];
+      for (int k = 0; k < kLoad; ++k) {
+        c[i + k] = u[k];
+        s[i + k] = w[k];
       }
     }
-    float f0[kPer], f1[kPer];
-    T::widen(y0, f0);
-    T::widen(y1, f1);
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      float& u = kNeighbours ? (i < kPer / 2 ? f0[2 * i] : f1[2 * i - kPer]) : f0[i];
-      float& w = kNeighbours ? (i < kPer / 2 ? f0[2 * i + 1] : f1[2 * i + 1 - kPer]) : f1[i];
-      const float turned_u = u * c[i] - w * s[i];
-      w = u * s[i] + w * c[i];
-      u = turned_u;
-    }
-    y0 = T::round(f0);
-    y1 = T::round(f1);
   }
-  *(gvec*)(dst + p0 * 16) = y0;
-  if (two) *(gvec*)(dst + p1 * 16) = y1;
+  const uint32_t b = div(p, a.by_block);
+  int32_t id = -1;                                       // of the token's block
+  if (b < uint32_t(a.max_blocks)) id = a.tables[int64_t(r) * a.max_blocks + b];
+  const bool kept = id >= 0 && id < a.pool_blocks;
+  char* const slot = a.kbase + id * a.bstride +
+                     int64_t((p - b * uint32_t(a.block_size)) * kv) * a.pieces * 16;
+#pragma unroll
+  for (int e = 0; e < kHeads; ++e) {
+    if (!here[e] || !(is_q[e] || kept)) continue;
+    if (turned[e]) {
+      float f0[kPer], f1[kPer];
+      T::widen(y[e][0], f0);
+      T::widen(y[e][1], f1);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        float& u = kNeighbours ? (i < kPer / 2 ? f0[2 * i] : f1[2 * i - kPer]) : f0[i];
+        float& w = kNeighbours ? (i < kPer / 2 ? f0[2 * i + 1] : f1[2 * i + 1 - kPer]) : f1[i];
+        const float turned_u = u * c[i] - w * s[i];
+        w = u * s[i] + w * c[i];
+        u = turned_u;
+      }
+      y[e][0] = T::round(f0);
+      y[e][1] = T::round(f1);
+    }
+    char* dst = is_q[e] ? a.q_out + token * a.q_out_stride : slot + (is_v[e] ? a.voff : 0);
+    dst += int64_t(h[e] * uint32_t(a.pieces)) * 16;
+    if constexpr (!kPast) {
+      *(gvec*)(dst + p0[e] * 16) = y[e][0];
+      if (two[e]) *(gvec*)(dst + p1[e] * 16) = y[e][1];
+    } else {
+      __builtin_nontemporal_store(y[e][0], (gvec*)(dst + p0[e] * 16));
+      if (two[e]) __builtin_nontemporal_store(y[e][1], (gvec*)(dst + p1[e] * 16));
+    }
+  }
 }
 
+// Units up to which a lane takes one: they then are on the CUs at once.  And bytes written from
+// which on they go past the caches: 45 MB (17,679 tokens of 10 heads of 128) take 17.9 us past
+// them, 5.6 TB/s, and 20.8 through; 17 MB (8,484 tokens of 16 heads of 64) 11.9 and 10.5.
+constexpr int64_t kRotateFew = 1 << 17;
+constexpr int64_t kRotatePast = int64_t(32) << 20;
+
+enum Variant { kOneHead, kTwoHeads, kTwoHeadsPast };
+
+template <class T, bool kNeighbours>
+const void* kernel(Variant v) {
+  return v == kOneHead    ? reinterpret_cast<const void*>(kv_rotate<T, kNeighbours, 1, false>)
+         : v == kTwoHeads ? reinterpret_cast<const void*>(kv_rotate<T, kNeighbours, 2, false>)
+                          : reinterpret_cast<const void*>(kv_rotate<T, kNeighbours, 2, true>);
+}
 template <class T>
-const void* kernel(bool neighbours) {
-  return neighbours ? reinterpret_cast<const void*>(kv_rotate<T, true>)
-                    : reinterpret_cast<const void*>(kv_rotate<T, false>);
+const void* kernel(bool neighbours, Variant v) {
+  return neighbours ? kernel<T, true>(v) : kernel<T, false>(v);
 }
 
 }  // namespace
@@ -224,8 +279,8 @@ extern "C" int flowkv_append_rotated(
     return fail(FLOWKV_EINVAL, "interleaved %d: need 0 or 1", interleaved);
   if (n_tokens < 0 || n_req < 0 || max_blocks < 0 || n_positions < 0)
     return fail(FLOWKV_EINVAL, "negative sizes");
-  const int64_t per = (int64_t(q_heads) + 2 * int64_t(kv_heads)) * ((head / 16 + 1) / 2);
-  if (per > INT32_MAX / 2)
+  const int64_t heads = int64_t(q_heads) + 2 * int64_t(kv_heads), per_head = (head / 16 + 1) / 2;
+  if (heads * per_head > INT32_MAX / 2)
     return fail(FLOWKV_EINVAL, "%d query and %d KV heads: too many", q_heads, kv_heads);
   if (n_tokens == 0 || n_req == 0 || n_positions == 0) return ok();
   if (!k_dev || !v_dev || !cos_sin_dev || !offsets_dev || !seq_lens_dev ||
@@ -246,7 +301,11 @@ extern "C" int flowkv_append_rotated(
   }
   if (reinterpret_cast<uintptr_t>(cos_sin_dev) % 4)
     return fail(FLOWKV_EINVAL, "cosines not 4-byte aligned");
-  const int64_t items = int64_t(n_tokens) * per;
+  const Variant variant = n_tokens * heads * per_head <= kRotateFew ? kOneHead
+                          : n_tokens * heads * head <= kRotatePast  ? kTwoHeads
+                                                                    : kTwoHeadsPast;
+  const int64_t per = (variant == kOneHead ? heads : (heads + 1) / 2) * per_head;
+  const int64_t items = n_tokens * per;
   const int64_t groups = (items + kThreads - 1) / kThreads;
   if (groups * kThreads > UINT32_MAX)                // lanes of a launch
     return fail(FLOWKV_EINVAL, "%d tokens of %lld units: too many for one call", n_tokens,
@@ -279,10 +338,16 @@ extern "C" int flowkv_append_rotated(
   a.pieces = int32_t(head / 16);
   a.n_positions = n_positions;
   a.rot_dim = rot_dim;
+  a.items = uint32_t(items);
+  a.per = uint32_t(per);
+  a.per_head = uint32_t(per_head);
+  a.by_per = divisor(a.per);
+  a.by_per_head = divisor(a.per_head);
+  a.by_block = divisor(uint32_t(a.block_size));
   void* args[] = {&a};
-  const void* fn = dtype == FLOWKV_BF16   ? kernel<Bf16>(interleaved)
-                   : dtype == FLOWKV_FP16 ? kernel<Fp16>(interleaved)
-                                          : kernel<F32>(interleaved);
+  const void* fn = dtype == FLOWKV_BF16   ? kernel<Bf16>(interleaved, variant)
+                   : dtype == FLOWKV_FP16 ? kernel<Fp16>(interleaved, variant)
+                                          : kernel<F32>(interleaved, variant);
   hipError_t rc2 = hipLaunchKernel(fn, dim3(unsigned(groups)), dim3(kThreads), args, 0,
                                    static_cast<hipStream_t>(hip_stream));
   if (rc2 == hipSuccess) rc2 = hipGetLastError();

@@ -41,7 +41,7 @@ def test_attention_kernels(tmp_path_factory, name, many, few, rest):
 
 def test_rotated_append_kernels(tmp_path_factory):
     entries = kernel_entries(compiled("flowkv_rotate", tmp_path_factory), "kv_rotate")
-    assert len(entries) == 6
+    assert len(entries) == 18
     check_all(entries)
     for n, e in entries.items():        # 32 waves a CU
         assert number(e, "vgpr_count") <= 64, n
