@@ -114,6 +114,7 @@ struct SpanArgs : ChunkArgs {
   int32_t max_own;                      // tokens of a request behind its prefix
   int32_t first_split;                  // records of a row: [0, first_split) of its prefix,
   int32_t prefix_split;                 // this many tokens each, the others its own
+  uint32_t prefix_items;                // Shared: workgroups of prefixes, of a KV head
 };
 
 // The kernel's arguments, loaded here and not before.
@@ -131,30 +132,31 @@ __device__ __forceinline__ A late_args() {
 //   Causal    a request's rows, over all tokens up to each row's own
 //   Windowed  the same, over the last `window` of them and the first `sinks`
 //   Prefixed  the rows of a whole group of requests, over the prefix that they share
-//   Own       a request's rows, over what is behind its group's prefix
+//   Shared    (few rows) the same in some workgroups, and in the others a request's rows, over
+//             what is behind its group's prefix; what joins the two
 template <class T_>
 struct Causal {
   typedef T_ T;
   typedef ChunkArgs Args;
-  static constexpr bool kWindow = false, kPrefix = false, kOwn = false;
+  static constexpr bool kWindow = false, kPrefix = false, kShared = false;
 };
 template <class T_>
 struct Windowed {
   typedef T_ T;
   typedef SpanArgs Args;
-  static constexpr bool kWindow = true, kPrefix = false, kOwn = false;
+  static constexpr bool kWindow = true, kPrefix = false, kShared = false;
 };
 template <class T_>
 struct Prefixed {
   typedef T_ T;
   typedef SpanArgs Args;
-  static constexpr bool kWindow = false, kPrefix = true, kOwn = false;
+  static constexpr bool kWindow = false, kPrefix = true, kShared = false;
 };
 template <class T_>
-struct Own {
+struct Shared {
   typedef T_ T;
   typedef SpanArgs Args;
-  static constexpr bool kWindow = false, kPrefix = false, kOwn = true;
+  static constexpr bool kWindow = false, kPrefix = false, kShared = true;
 };
 
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -166,31 +168,59 @@ __device__ __forceinline__ int32_t group_at(const SpanArgs& a, int32_t g) {
   return r < 0 ? 0 : r < a.n_req ? r : a.n_req;
 }
 
-// A tile's rows are those of a unit: a request, or a group of them.
-template <class P>
-__device__ __forceinline__ int32_t units(const typename P::Args& a) {
-  if constexpr (P::kPrefix) return a.n_groups;
-  else return a.n_req;
-}
-template <class P>
-__device__ __forceinline__ int32_t begin_of(const typename P::Args& a, int32_t r) {
-  if constexpr (P::kPrefix) return a.offsets[group_at(a, r)];
-  else return a.offsets[r];
-}
-
-// The rows of a unit are its (new token, query head of the group) pairs,
-// token by token; a tile is 2^row_shift of them.  Tile slot x of the batch: unit r
-// has the slots from floor(its first token * G / rows) + r, which are enough for its
-// rows whatever the offsets are, and at most n_tokens * G / rows + units in all:
-// the grid needs no lengths on the host.
-template <class P>
-__device__ __forceinline__ int64_t first_tile(const typename P::Args& a, int32_t r) {
-  return (int64_t(begin_of<P>(a, r)) * a.group >> a.row_shift) + r;
+// A tile's rows are those of a unit: a request, or a group of them.  The rows of a unit are its
+// (new token, query head of the KV head's group) pairs, token by token; a tile is 2^row_shift of
+// them.  Tile slot x of the batch: request r has the slots from floor(offsets[r] * G / rows) + r,
+// which are enough for its rows whatever the offsets are, and at most n_tokens * G / rows +
+// n_req in all: the grid needs no lengths on the host.
+__device__ __forceinline__ int64_t first_tile(const ChunkArgs& a, int32_t r) {
+  return (int64_t(a.offsets[r]) * a.group >> a.row_shift) + r;
 }
 
 // The token of a unit's row x (0 <= x < 2^31).
 __device__ __forceinline__ int32_t token_of(const ChunkArgs& a, int32_t x) {
   return int32_t((__umulhi(uint32_t(x), a.g_magic) + uint32_t(x)) >> a.g_shift);
+}
+
+// Item `want` of the tiles of all groups, each tile in splits of its group's prefix: which group,
+// which of its items (-1: there are fewer).  The lanes count 64 groups at a time, so that the
+// workgroups with something to do are the first of a launch, next to each other.  (With a slot
+// for every split of the longest prefix, the empty ones between them left some XCDs' CUs idle
+// and others with two in turn: 48 requests in 6 groups of 500 to 9,000 tokens took 53 us in
+// splits of 384, not 36.)
+struct Item {
+  int32_t unit;
+  int64_t at;
+};
+__device__ __forceinline__ int32_t group_at(const SpanArgs& a, int32_t g);
+__device__ __forceinline__ int32_t prefix_of(const SpanArgs& a, int32_t g);
+__device__ __forceinline__ Item find_item(const SpanArgs& a, int64_t want) {
+  const int ln = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int32_t g0 = 0; g0 < a.n_groups; g0 += 64) {
+    const int32_t g = g0 + ln;
+    int64_t count = 0;
+    if (g < a.n_groups) {
+      const int64_t rows =
+          (int64_t(a.offsets[group_at(a, g + 1)]) - a.offsets[group_at(a, g)]) * a.group;
+      const int64_t tiles = rows > 0 ? (rows + (int64_t(1) << a.row_shift) - 1) >> a.row_shift : 0;
+      count = tiles * splits_of(prefix_of(a, g), a.prefix_split);
+    }
+    int64_t sum = count;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      const int64_t y = __shfl_up(sum, off);
+      if (ln >= off) sum += y;
+    }
+    const uint64_t hit = __ballot(want < before + sum);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      const int64_t first = __shfl(sum - count, l);
+      return Item{g0 + l, want - before - first};
+    }
+    before += __shfl(sum, 63);
+  }
+  return Item{0, -1};
 }
 
 struct Request {
@@ -227,23 +257,60 @@ __device__ __forceinline__ int32_t prefix_before(const SpanArgs& a, int32_t r) {
   return group_at(a, g) <= r && r < group_at(a, g + 1) ? prefix_of(a, g) : 0;
 }
 
-// A unit: of a group, r is the first request, whose block list is read, and base the one
-// behind the last.
-template <class P>
-__device__ __forceinline__ Request unit_at(const typename P::Args& a, int32_t u) {
-  if constexpr (P::kPrefix) {
-    Request q;
-    q.r = group_at(a, u);
-    q.base = group_at(a, u + 1);
-    q.begin = a.offsets[q.r];
-    const int64_t n = int64_t(a.offsets[q.base]) - q.begin;
-    q.limit = prefix_of(a, u);
-    q.n_new = q.r < q.base && q.begin >= 0 && n > 0 && q.begin + n <= a.n_tokens && q.limit > 0
-                  ? int32_t(n) : 0;
-    return q;
-  } else {
-    return request_at(a, u);
+// A group as a unit of rows: r is its first request, whose block list is read, and base the one
+// behind its last.
+__device__ __forceinline__ Request group_unit(const SpanArgs& a, int32_t g) {
+  Request q;
+  q.r = group_at(a, g);
+  q.base = group_at(a, g + 1);
+  q.begin = a.offsets[q.r];
+  const int64_t n = int64_t(a.offsets[q.base]) - q.begin;
+  q.limit = prefix_of(a, g);
+  q.n_new = q.r < q.base && q.begin >= 0 && n > 0 && q.begin + n <= a.n_tokens && q.limit > 0
+                ? int32_t(n) : 0;
+  return q;
+}
+
+// Item `at` of a group's: 8 splits of all tiles, tile by tile, then the next 8.  So the tiles of
+// a split are 8 workgroups (of a KV head) apart, on one XCD and at the same time, and all but
+// the first find its K and V in that XCD's L2.
+__device__ __forceinline__ void place_item(const SpanArgs& a, const Request& q, int32_t at,
+                                           int64_t* tile, int* split) {
+  const uint32_t splits = uint32_t(splits_of(q.limit, a.prefix_split));
+  const int64_t rows = int64_t(q.n_new) * a.group;
+  const uint32_t tiles = uint32_t((rows + (int64_t(1) << a.row_shift) - 1) >> a.row_shift);
+  if (tiles == 0 || splits == 0) {
+    *tile = -1;
+    return;
   }
+  const uint32_t block = uint32_t(at) / (8 * tiles), rest = uint32_t(at) - block * 8 * tiles;
+  const uint32_t wide = splits - 8 * block < 8 ? splits - 8 * block : 8;
+  *tile = rest / wide;
+  *split = int(8 * block + (rest - uint32_t(*tile) * wide));
+}
+
+// What new token i of a group sees of the prefix: all of it, unless the token lies in it.
+__device__ __forceinline__ int32_t seen_of_prefix(const SpanArgs& a, const Request& q, int32_t i) {
+  const int32_t token = q.begin + i;
+  // its request: where it would be if all had as many, or between
+  int32_t r = q.r, hi = q.base;
+  const int32_t guess =
+      std::min(r + int32_t(float(i) * float(hi - r) / float(q.n_new)), hi - 1);
+  const int32_t from = a.offsets[guess], to = a.offsets[guess + 1];
+  if (from > token) {
+    hi = guess;
+  } else {
+    r = to > token ? guess : std::min(guess + 1, hi - 1);
+    if (to > token) hi = guess + 1;
+  }
+  while (hi - r > 1) {
+    const int32_t mid = r + (hi - r) / 2;
+    if (a.offsets[mid] <= token) r = mid;
+    else hi = mid;
+  }
+  const Request one = request_at(a, r);
+  const int32_t n = one.base + (token - one.begin) + 1;
+  return n < 0 ? 0 : n < q.limit ? n : q.limit;
 }
 
 // Tokens that new token i of a request sees: those up to its own position.
@@ -257,9 +324,10 @@ __device__ __forceinline__ int32_t seen(const Request& q, int32_t i) {
 // splits and steps of a tile are in this count.
 template <class P>
 struct Reach {
+  __device__ __forceinline__ Reach() {}
   int32_t sinks = 0, shift = 0;
   int32_t window = 0;                    // kWindow
-  int32_t most = 0;                      // kOwn
+  int32_t most = 0;                      // kShared
   __device__ __forceinline__ Reach(const typename P::Args& a, const Request& rq, int32_t row0) {
     if constexpr (P::kWindow) {
       // the window of the tile's first row on
@@ -268,7 +336,7 @@ struct Reach {
       sinks = a.sinks;
       shift = low > sinks ? low - sinks : 0;
     }
-    if constexpr (P::kOwn) {
+    if constexpr (P::kShared) {              // (behind the prefix)
       shift = prefix_before(a, rq.r);
       most = a.max_own;
     }
@@ -276,12 +344,12 @@ struct Reach {
   // how many are below token n of the request
   __device__ __forceinline__ int32_t below(int32_t n) const {
     if constexpr (P::kWindow) return n <= sinks ? n : std::max(sinks, n - shift);
-    else if constexpr (P::kOwn) return std::min(std::max(n - shift, 0), most);
+    else if constexpr (P::kShared) return std::min(std::max(n - shift, 0), most);
     else return n;
   }
   __device__ __forceinline__ uint32_t token(uint32_t x) const {
     if constexpr (P::kWindow) return x < uint32_t(sinks) ? x : x + uint32_t(shift);
-    else if constexpr (P::kOwn) return x + uint32_t(shift);
+    else if constexpr (P::kShared) return x + uint32_t(shift);
     else return x;
   }
   // the first that new token i sees, but for those below `sinks`
@@ -299,30 +367,14 @@ struct Reach {
 template <class P>
 __device__ __forceinline__ int32_t end_of(const typename P::Args& a, const Request& rq,
                                           const Reach<P>& reach, int32_t i) {
-  if constexpr (P::kPrefix) {
-    // (all of the prefix, unless the new token lies in it)
-    const int32_t token = rq.begin + i;
-    int32_t r = rq.r, hi = rq.base;
-    while (hi - r > 1) {
-      const int32_t mid = r + (hi - r) / 2;
-      if (a.offsets[mid] <= token) r = mid;
-      else hi = mid;
-    }
-    const Request one = request_at(a, r);
-    const int32_t n = one.base + (token - one.begin) + 1;
-    return n < 0 ? 0 : n < rq.limit ? n : rq.limit;
-  } else {
-    return reach.below(seen(rq, i));
-  }
+  if constexpr (P::kPrefix) return seen_of_prefix(a, rq, i);
+  else return reach.below(seen(rq, i));
 }
-
 
 // The workspace holds a record per (new token, query head, split): the weighted V
 // (Dh floats) of all records first, then all records' (reference max, sum).
-template <class P>
-__device__ __forceinline__ int64_t record_at(const typename P::Args& a, int64_t row, int split) {
-  if constexpr (P::kOwn) return row * a.splits + a.first_split + split;
-  else return row * a.splits + split;
+__device__ __forceinline__ int64_t record_at(const ChunkArgs& a, int64_t row, int split) {
+  return row * a.splits + split;
 }
 __device__ __forceinline__ float* record_sums(const ChunkArgs& a, int dh, int64_t rec) {
   return a.ws + rec * dh;
@@ -716,8 +768,8 @@ __device__ __forceinline__ Mine cut_tiles(const typename P::Args& a, Cut& c, int
     g = int(blockIdx.x % uint32_t(a.kv_heads));
     const int32_t slot = int32_t(blockIdx.x / uint32_t(a.kv_heads));
     mine.rq = request_at(
-        a, flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile<P>(a, i); }));
-    const int64_t local = int64_t(slot) - first_tile<P>(a, mine.rq.r);
+        a, flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); }));
+    const int64_t local = int64_t(slot) - first_tile(a, mine.rq.r);
     if (local >= 0 && local * F::kRows < int64_t(mine.rq.n_new) * a.group) mine.pieces = 1;
     mine.row0 = int32_t(local) * F::kRows;
     mine.split = 0;
@@ -872,21 +924,19 @@ __device__ __forceinline__ void attend_many(const typename P::Args& a) {
     const uint32_t id = paired<F>();
     g = int(id % uint32_t(a.kv_heads));
     const uint32_t rest = id / uint32_t(a.kv_heads);
-    int slot;
-    if constexpr (P::kPrefix || P::kOwn) {
-      // a tile's splits together: slots without rows are not every other workgroup then, which
-      // go to the same CUs (one group of 128 rows in 26 splits: 17 us, not 36)
-      const uint32_t splits = gridDim.x / uint32_t(a.tiles * a.kv_heads);
-      split = int(rest % splits);
-      slot = int(rest / splits);
+    int64_t local;
+    if constexpr (P::kPrefix) {
+      const Item item = find_item(a, rest);
+      if (item.at < 0) return;
+      rq = group_unit(a, uniform(item.unit));
+      place_item(a, rq, uniform(int32_t(item.at)), &local, &split);
     } else {
       split = int(rest / uint32_t(a.tiles));
-      slot = a.tiles - 1 - int(rest % uint32_t(a.tiles));  // the longest first
+      const int slot = a.tiles - 1 - int(rest % uint32_t(a.tiles));  // the longest first
+      rq = request_at(
+          a, flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); }));
+      local = int64_t(slot) - first_tile(a, rq.r);
     }
-    const int32_t u = flowkv::last_at_most(units<P>(a), slot,
-                                           [&](int32_t i) { return first_tile<P>(a, i); });
-    rq = unit_at<P>(a, u);
-    const int64_t local = int64_t(slot) - first_tile<P>(a, u);
     if (local < 0 || local * F::kRows >= int64_t(rq.n_new) * a.group) return;
     row0 = int32_t(local) * F::kRows;
   }
@@ -907,7 +957,7 @@ __device__ __forceinline__ void attend_many(const typename P::Args& a) {
   const int32_t s0 = split * length;
   if (!kCut && split > 0 && s0 >= tile_limit) return;   // (split 0 writes what sees nothing)
   const int32_t s1 = tile_limit - s0 > length ? s0 + length : tile_limit;
-  const bool direct = kCut ? pieces == 1 : !P::kPrefix && !P::kOwn && tile_limit <= length;
+  const bool direct = kCut ? pieces == 1 : !P::kPrefix && tile_limit <= length;
 
   __shared__ alignas(16) u32x4 sk0[kStep * kPc], sk1[kStep * kPc], sv0[kStep * kPc],
       sv1[kStep * kPc];
@@ -1201,7 +1251,7 @@ __device__ __forceinline__ void attend_many(const typename P::Args& a) {
         *reinterpret_cast<u32x2*>(e.out + orow * kDh + 32 * b + 2 * i + 4 * hi) = x;
       }
   } else if constexpr (!kCut) {
-    const int64_t rec = record_at<P>(e, orow, split);
+    const int64_t rec = record_at(e, orow, split);
 #pragma unroll
     for (int b = 0; b < kB; ++b)
 #pragma unroll
@@ -1271,20 +1321,6 @@ __device__ __forceinline__ void join_pieces(const ChunkArgs& a) {
   }
 }
 
-// A row's parts so far: reference, sum, and four dims.
-struct Running {
-  float m, l;
-  f32x4 v;
-};
-__device__ __forceinline__ Running join(const Running& a, const Running& b) {
-  Running r;
-  r.m = fmaxf(a.m, b.m);
-  const float wa = part_weight(a.m, a.l, r.m), wb = part_weight(b.m, b.l, r.m);
-  r.l = weighted(a.l, wa, b.l, wb);
-  r.v = weighted(a.v, wa, b.v, wb);
-  return r;
-}
-
 // ---- few rows ----------------------------------------------------------------------
 //
 // A request of a few new tokens reads every cached K and V for a handful of rows: that is
@@ -1304,20 +1340,19 @@ constexpr int kFewWaves = 4;
 constexpr int kFewThreads = 64 * kFewWaves;
 constexpr int kFewTile = 32;
 constexpr int kFewSplit = 2048;            // most tokens of a workgroup: their places are in LDS
-constexpr int kFewOwn = 4096;              // the same behind a prefix
 
-template <int kDh, int kC, int kSplit, int kWaves>
+template <int kDh, int kC>
 struct FewLds {
   static constexpr int kRows = 16 * kC;
-  uint32_t at[kSplit];                     // a tile's token 4 e + q4 at 8 q4 + e, in 128-byte units
+  uint32_t at[kFewSplit];                  // a tile's token 4 e + q4 at 8 q4 + e, in 128-byte units
   // K's staging, a tile per wave; after the loop the waves' weighted sums
-  alignas(16) uint8_t area[kWaves * kRows * kDh * sizeof(float)];
-  uint32_t dead[kSplit / kFewTile];
-  uint32_t odd[kSplit / kFewTile / 32];    // tiles whose V lost an infinity or a NaN
-  float m[kWaves][kRows], l[kWaves][kRows];
+  alignas(16) uint8_t area[kFewWaves * kRows * kDh * sizeof(float)];
+  uint32_t dead[kFewSplit / kFewTile];
+  uint32_t odd[2];                         // tiles whose V lost an infinity or a NaN
+  float m[kFewWaves][kRows], l[kFewWaves][kRows];
   int32_t lim[kRows];
   int32_t low[kRows];                      // kWindow
-  static_assert(kWaves * kFewTile * kDh * 2 <= sizeof(area) && kSplit / kFewTile % 64 == 0);
+  static_assert(kFewWaves * kFewTile * kDh * 2 <= sizeof(area) && kFewSplit / kFewTile <= 64);
 };
 
 __device__ __forceinline__ uint32_t pair_hi(uint32_t lo, uint32_t hi) {
@@ -1330,7 +1365,7 @@ __device__ __forceinline__ uint32_t pair_lo(uint32_t lo, uint32_t hi) {
 // Workgroups on a CU at once.
 constexpr int few_per_cu(int dh, int c) { return (dh == 64 ? 4 : 3) - (c - 1); }
 
-template <int kDh, int kC, class P, int kSplit = kFewSplit, int kWaves = kFewWaves>
+template <int kDh, int kC, class P>
 __device__ __forceinline__ void attend_few(const typename P::Args& a) {
   typedef typename P::T T;
   typedef typename T::Vec Vec;
@@ -1349,32 +1384,47 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
   const uint32_t id = blockIdx.x;
   const int g = int(id % uint32_t(a.kv_heads));
   const uint32_t rest = id / uint32_t(a.kv_heads);
-  const int split = int(rest / uint32_t(a.tiles));
-  const int slot = int(rest % uint32_t(a.tiles));
-  const int32_t u = flowkv::last_at_most(units<P>(a), slot,
-                                         [&](int32_t i) { return first_tile<P>(a, i); });
-  const Request rq = unit_at<P>(a, u);
-  const int64_t local = int64_t(slot) - first_tile<P>(a, u);
+  int split = 0;
+  int32_t length = a.split_tokens;
+  Request rq{};
+  int64_t local = -1;
+  bool of_prefix = false;                        // kShared: a group's rows, over its prefix
+  if constexpr (P::kShared) of_prefix = rest < a.prefix_items;
+  if (of_prefix) {
+    if constexpr (P::kShared) {
+      const Item item = find_item(a, rest);
+      if (item.at < 0) return;
+      length = a.prefix_split;
+      rq = group_unit(a, uniform(item.unit));
+      place_item(a, rq, uniform(int32_t(item.at)), &local, &split);
+    }
+  } else {
+    uint32_t at = rest;
+    if constexpr (P::kShared) at -= a.prefix_items;
+    split = int(at / uint32_t(a.tiles));
+    const int slot = int(at % uint32_t(a.tiles));
+    rq = request_at(
+        a, flowkv::last_at_most(a.n_req, slot, [&](int32_t i) { return first_tile(a, i); }));
+    local = int64_t(slot) - first_tile(a, rq.r);
+  }
   if (local < 0 || local * kFewRows >= int64_t(rq.n_new) * a.group) return;
   const int32_t row0 = int32_t(local) * kFewRows, rows = rq.n_new * a.group;
-  const Reach<P> reach(a, rq, row0);
-  int32_t tile_limit, tile_least;
-  if constexpr (P::kPrefix) {
-    tile_limit = tile_least = rq.limit;
-  } else {
+  Reach<P> reach;
+  int32_t tile_limit = rq.limit, tile_least = rq.limit;
+  if (!of_prefix) {
+    reach = Reach<P>(a, rq, row0);
     tile_limit = end_of<P>(a, rq, reach, token_of(a, std::min(row0 + kFewRows, rows) - 1));
     tile_least = end_of<P>(a, rq, reach, token_of(a, row0));
   }
   const int32_t tile_low =
       P::kWindow ? reach.low(rq, token_of(a, std::min(row0 + kFewRows, rows) - 1)) : 0;
-  const int32_t s0 = split * a.split_tokens;
+  const int32_t s0 = split * length;
   if (split > 0 && s0 >= tile_limit) return;
-  const int32_t s1 = tile_limit - s0 > a.split_tokens ? s0 + a.split_tokens : tile_limit;
-  bool direct = !P::kPrefix && tile_limit <= a.split_tokens;
-  if constexpr (P::kOwn) direct = a.splits == a.first_split + 1;   // (no request has more)
+  const int32_t s1 = tile_limit - s0 > length ? s0 + length : tile_limit;
+  const bool direct = !P::kShared && tile_limit <= length;
   const int n_tiles = (s1 - s0 + kFewTile - 1) / kFewTile;
 
-  __shared__ FewLds<kDh, kC, kSplit, kWaves> lds;
+  __shared__ FewLds<kDh, kC> lds;
   int32_t lim[kC], low[kC];
   Vec qb[kC][kI];
 #pragma unroll
@@ -1383,13 +1433,16 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
     const bool live = row < rows;
     const int32_t qi = live ? token_of(a, row) : 0;
     const int32_t qh = live ? row - qi * a.group : 0;
-    lim[c] = live ? end_of<P>(a, rq, reach, qi) : 0;
+    if constexpr (P::kShared)
+      lim[c] = !live ? 0 : of_prefix ? seen_of_prefix(a, rq, qi) : end_of<P>(a, rq, reach, qi);
+    else
+      lim[c] = live ? end_of<P>(a, rq, reach, qi) : 0;
     if (tid < 16) lds.lim[16 * c + tid] = lim[c];
     if constexpr (P::kWindow) {
       low[c] = reach.low(rq, qi);
       if (tid < 16) lds.low[16 * c + tid] = low[c];
     }
-    if constexpr (P::kPrefix) {
+    if (of_prefix) {
       int32_t least = live ? lim[c] : rq.limit;
 #pragma unroll
       for (int off = 1; off < 16; off *= 2) least = std::min(least, __shfl_xor(least, off));
@@ -1405,7 +1458,7 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
     }
   }
   const int32_t* table = a.tables + int64_t(rq.r) * a.max_blocks;
-  for (int x = tid; x < n_tiles * kFewTile; x += 64 * kWaves) {
+  for (int x = tid; x < n_tiles * kFewTile; x += kFewThreads) {
     const uint32_t t = reach.token(uint32_t(s0 + x));
     const uint32_t b = uint32_t((uint64_t(__umulhi(t, a.bs_magic)) + t) >> a.bs_shift);
     const bool in = s0 + x < s1;
@@ -1426,7 +1479,7 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
 #pragma unroll
     for (int t = 0; t < kT; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  if (tid < kSplit / kFewTile / 32) lds.odd[tid] = 0;
+  if (tid < 2) lds.odd[tid] = 0;
   __syncthreads();
 
   u32x4 kw[kKL];
@@ -1436,27 +1489,40 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
   const char* const kbase = a.kbase + g * kDh * 2 + 16 * kp;
   const char* const vbase = a.kbase + a.voff + g * kDh * 2 + c16 * (kVW * 4);
   auto swz = [](int token) { return (token * kPc >> 4) & (kPc - 1); };
+  // (rows of a prefix are read again, by its other tiles; others once, past the caches)
   auto load_k = [&](int tile) {
-#pragma unroll
-    for (int e = 0; e < kKL; ++e) {
+    auto at = [&](int e) {
       const int x = kt + e * kStride;            // token of the tile
-      kw[e] = __builtin_nontemporal_load(
-          (cgvec4*)(kbase + uint64_t(lds.at[tile * kFewTile + (x & 3) * 8 + (x >> 2)]) * 128));
+      return (cgvec4*)(kbase +
+                       uint64_t(lds.at[tile * kFewTile + (x & 3) * 8 + (x >> 2)]) * 128);
+    };
+    if (of_prefix) {
+#pragma unroll
+      for (int e = 0; e < kKL; ++e) kw[e] = *at(e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kKL; ++e) kw[e] = __builtin_nontemporal_load(at(e));
     }
   };
   auto load_v = [&](int tile) {
+    auto at = [&](int e) {
+      return (cgv*)(vbase + uint64_t(lds.at[tile * kFewTile + 8 * q4 + e]) * 128);
+    };
+    if (of_prefix) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      vw[e] = __builtin_nontemporal_load(
-          (cgv*)(vbase + uint64_t(lds.at[tile * kFewTile + 8 * q4 + e]) * 128));
+      for (int e = 0; e < 8; ++e) vw[e] = *at(e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vw[e] = __builtin_nontemporal_load(at(e));
+    }
   };
   if (wave < n_tiles) {
     load_k(wave);
     load_v(wave);
   }
-  for (int tile = wave; tile < n_tiles; tile += kWaves) {
+  for (int tile = wave; tile < n_tiles; tile += kFewWaves) {
     // (past the wave's last tile: its own again, so that as many loads are under way)
-    const int next = tile + kWaves < n_tiles ? tile + kWaves : tile;
+    const int next = tile + kFewWaves < n_tiles ? tile + kFewWaves : tile;
 #pragma unroll
     for (int e = 0; e < kKL; ++e) {
       const int x = kt + e * kStride;
@@ -1571,11 +1637,8 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
     }
   }
   __syncthreads();                               // every wave is past the loop: the area is free
-  uint64_t odds[kSplit / kFewTile / 64];
-#pragma unroll
-  for (int w = 0; w < kSplit / kFewTile / 64; ++w)
-    odds[w] = uint64_t(uint32_t(uniform(int32_t(lds.odd[2 * w + 1])))) << 32 |
-              uint32_t(uniform(int32_t(lds.odd[2 * w])));
+  const uint64_t odd = uint64_t(uint32_t(uniform(int32_t(lds.odd[1])))) << 32 |
+                       uint32_t(uniform(int32_t(lds.odd[0])));
   float* const s_o = reinterpret_cast<float*>(lds.area);   // [wave][row][dim]
 #pragma unroll
   for (int c = 0; c < kC; ++c)
@@ -1588,24 +1651,22 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
             f32x4{o[c][t][x], o[c][t + 1][x], o[c][t + 2][x], o[c][t + 3][x]};
   __syncthreads();
   // a row's dims 4 at a time
-  for (int i = tid; i < kFewRows * kDh / 4; i += 64 * kWaves) {
+  for (int i = tid; i < kFewRows * kDh / 4; i += kFewThreads) {
     const int h = i / (kDh / 4), d = i % (kDh / 4) * 4;
     if (row0 + h >= rows) break;
     float M = -INFINITY, L = 0.f;
     f32x4 A = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, lds.m[w][h]);
+    for (int w = 0; w < kFewWaves; ++w) M = fmaxf(M, lds.m[w][h]);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < kFewWaves; ++w) {
       const float wt = part_weight(lds.m[w][h], lds.l[w][h], M);
       L += lds.l[w][h] * wt;
       A += *reinterpret_cast<const f32x4*>(&s_o[(w * kFewRows + h) * kDh + d]) * wt;
     }
     // infinities and NaN of the tokens that the row sees, until it is all NaN
-#pragma unroll
-    for (int w = 0; w < kSplit / kFewTile / 64; ++w)
-    for (uint64_t left = odds[w]; left; left &= left - 1) {
-      const int tile = 64 * w + __builtin_ctzll(left);
+    for (uint64_t left = odd; left; left &= left - 1) {
+      const int tile = __builtin_ctzll(left);
       const int32_t sees = lds.lim[h] - s0 - tile * kFewTile;
       if (sees <= 0 || (A[0] != A[0] && A[1] != A[1] && A[2] != A[2] && A[3] != A[3])) break;
       const uint32_t gone = lds.dead[tile];
@@ -1628,36 +1689,13 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
     const int32_t qi = token_of(a, row0 + h);
     const int64_t orow =
         (int64_t(rq.begin) + qi) * a.q_heads + g * a.group + (row0 + h - qi * a.group);
-    if constexpr (P::kOwn) {
-      if (direct) {                              // the prefix's records, kOwnAhead under way
-        constexpr int kOwnAhead = 16;
-        const int32_t n = flowkv::splits_of(
-            std::min(std::max(rq.base + qi + 1, 0), reach.shift), a.prefix_split);
-        const int64_t rec = orow * a.splits;
-        Running x{M, L, A};
-        for (int32_t s = 0; s < n; s += kOwnAhead) {
-          Running y[kOwnAhead];
-#pragma unroll
-          for (int j = 0; j < kOwnAhead; ++j) {  // (past the end: the first record, not used)
-            const int64_t at = rec + (s + j < n ? s + j : 0);
-            const f32x2u m = *record_ml(a, kDh, at);
-            y[j] = Running{m[0], m[1],
-                           *reinterpret_cast<const f32x4u*>(record_sums(a, kDh, at) + d)};
-          }
-#pragma unroll
-          for (int j = 0; j < kOwnAhead; ++j)
-            if (s + j < n) x = join(x, y[j]);
-        }
-        L = x.l;
-        A = x.v;
-      }
-    }
     if (direct) {
       const float inv = L == 0.f ? 0.f : 1.f / L;
       const u32x2 x = {T::pack(A[0] * inv, A[1] * inv), T::pack(A[2] * inv, A[3] * inv)};
       *reinterpret_cast<u32x2*>(a.out + orow * kDh + d) = x;
     } else {
-      const int64_t rec = record_at<P>(a, orow, split);
+      int64_t rec = record_at(a, orow, split);
+      if constexpr (P::kShared) rec += of_prefix ? 0 : a.first_split;
       *reinterpret_cast<f32x4u*>(record_sums(a, kDh, rec) + d) = A;
       if (d == 0) *record_ml(a, kDh, rec) = f32x2u{M, L};
     }
@@ -1670,6 +1708,19 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
 // 5 tokens x 32 heads x 26 splits.
 constexpr int kMergeThreads = 256;
 constexpr int kMergeChunk = 8;
+
+struct Running {
+  float m, l;
+  f32x4 v;
+};
+__device__ __forceinline__ Running join(const Running& a, const Running& b) {
+  Running r;
+  r.m = fmaxf(a.m, b.m);
+  const float wa = part_weight(a.m, a.l, r.m), wb = part_weight(b.m, b.l, r.m);
+  r.l = weighted(a.l, wa, b.l, wb);
+  r.v = weighted(a.v, wa, b.v, wb);
+  return r;
+}
 
 template <int kDh, int kWavesPer, class P>
 __device__ __forceinline__ void merge_splits(const typename P::Args& a) {
@@ -1689,21 +1740,21 @@ __device__ __forceinline__ void merge_splits(const typename P::Args& a) {
   // the tile that the row was in, as its workgroups saw it
   const int32_t row = i * a.group + int32_t(uint32_t(head) % uint32_t(a.group));
   const Reach<P> reach(a, rq, row >> a.row_shift << a.row_shift);
-  if constexpr (!P::kOwn) {
+  if constexpr (!P::kShared) {
     const int32_t end = std::min(((row >> a.row_shift) + 1) << a.row_shift, rq.n_new * a.group);
     const int32_t tile_limit = end_of<P>(a, rq, reach, token_of(a, end - 1));
     if (tile_limit <= a.split_tokens) return;    // written already
   }
   int32_t n = flowkv::splits_of(end_of<P>(a, rq, reach, i), a.split_tokens);
-  int32_t before = 0;                            // kOwn: the prefix's records
-  if constexpr (P::kOwn) {
+  int32_t before = 0;                            // kShared: the prefix's records
+  if constexpr (P::kShared) {
     before = flowkv::splits_of(std::min(std::max(rq.base + i + 1, 0), reach.shift), a.prefix_split);
     n += before;
   }
   const int64_t rec = orow * a.splits;
   // record s: those of the prefix, then those behind them
   auto at_of = [&](int32_t s) {
-    if constexpr (P::kOwn) return s < before ? s : s - before + a.first_split;
+    if constexpr (P::kShared) return s < before ? s : s - before + a.first_split;
     else return s;
   };
   const int tid = kWavesPer == 1 ? ln : threadIdx.x;

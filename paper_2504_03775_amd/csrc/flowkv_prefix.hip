@@ -27,25 +27,22 @@ using namespace flowkv::chunk;
 
 // ---- over a group's prefix, over what is behind it, and their join ----------------------
 
-template <class F, class P>
-__global__ __launch_bounds__(F::kThreads, 2 * F::kPerCu)
-void prefix_attn(const SpanArgs a) {
-  attend_many<F, false, P>(a);
-}
-template <int kDh, int kC, class P>
+// Few rows: both in one launch.  A tile of 16 or 32 rows of a group reads the prefix through its
+// XCD's L2, which brings some 14 TB/s of it.
+template <int kDh, int kC, class T>
 __global__ __launch_bounds__(kFewThreads, few_per_cu(kDh, kC))
 void prefix_attn_few(const SpanArgs a) {
-  attend_few<kDh, kC, P>(a);
+  attend_few<kDh, kC, Shared<T>>(a);
 }
-// Behind the prefix: four waves, or eight where there are no more workgroups than CUs.
-template <int kDh, int kC, int kWaves, class P>
-__global__ __launch_bounds__(64 * kWaves, kWaves == kFewWaves ? few_per_cu(kDh, kC) : 2)
-void prefix_attn_own(const SpanArgs a) {
-  attend_few<kDh, kC, P, kFewOwn, kWaves>(a);
+// Many rows: prefixes alone.
+template <class F, class T>
+__global__ __launch_bounds__(F::kThreads, 2 * F::kPerCu)
+void prefix_attn(const SpanArgs a) {
+  attend_many<F, false, Prefixed<T>>(a);
 }
 template <int kDh, int kWavesPer, class T>
 __global__ __launch_bounds__(kMergeThreads) void prefix_attn_merge(const SpanArgs a) {
-  merge_splits<kDh, kWavesPer, Own<T>>(a);
+  merge_splits<kDh, kWavesPer, Shared<T>>(a);
 }
 
 // ---- each request by itself ----------------------------------------------------------------
@@ -96,27 +93,17 @@ const Kernels& alone(int32_t dtype) {
 
 // ---- the host's part -----------------------------------------------------------------------
 
-// The forms of the parts, as Kernels has them; 256 rows for prefixes alone.
 struct Parts {
-  const void* prefix[4][2];
-  const void* own[3][2];
-  const void* own_wide[2][2];                    // eight waves
-  const void* merge[2][2];
+  const void* few[2][2];       // 16, 32 rows; head_dim
+  const void* many[2];         // 128 rows; head_dim
+  const void* merge[2][2];     // head_dim; a wave or four a row
 };
 template <class T>
 Parts parts_of() {
   auto ptr = [](void (*fn)(SpanArgs)) { return reinterpret_cast<const void*>(fn); };
-  typedef Prefixed<T> P;
-  typedef Own<T> O;
-  return Parts{{{ptr(prefix_attn_few<64, 1, P>), ptr(prefix_attn_few<128, 1, P>)},
-                {ptr(prefix_attn_few<64, 2, P>), ptr(prefix_attn_few<128, 2, P>)},
-                {ptr(prefix_attn<Form<64, 4, 2>, P>), ptr(prefix_attn<Form<128, 4, 2>, P>)},
-                {ptr(prefix_attn<Form<64, 8, 1>, P>), ptr(prefix_attn<Form<128, 8, 1>, P>)}},
-               {{ptr(prefix_attn_own<64, 1, 4, O>), ptr(prefix_attn_own<128, 1, 4, O>)},
-                {ptr(prefix_attn_own<64, 2, 4, O>), ptr(prefix_attn_own<128, 2, 4, O>)},
-                {ptr(prefix_attn<Form<64, 4, 2>, O>), ptr(prefix_attn<Form<128, 4, 2>, O>)}},
-               {{ptr(prefix_attn_own<64, 1, 8, O>), ptr(prefix_attn_own<128, 1, 8, O>)},
-                {ptr(prefix_attn_own<64, 2, 8, O>), ptr(prefix_attn_own<128, 2, 8, O>)}},
+  return Parts{{{ptr(prefix_attn_few<64, 1, T>), ptr(prefix_attn_few<128, 1, T>)},
+                {ptr(prefix_attn_few<64, 2, T>), ptr(prefix_attn_few<128, 2, T>)}},
+               {ptr(prefix_attn<Form<64, 4, 2>, T>), ptr(prefix_attn<Form<128, 4, 2>, T>)},
                {{ptr(prefix_attn_merge<64, 1, T>), ptr(prefix_attn_merge<64, 4, T>)},
                 {ptr(prefix_attn_merge<128, 1, T>), ptr(prefix_attn_merge<128, 4, T>)}}};
 }
@@ -125,19 +112,27 @@ const Parts& parts(int32_t dtype) {
   return dtype == FLOWKV_BF16 ? bf16 : fp16;
 }
 
-// Forms of a part: rows of a tile, threads.
-constexpr int kRows[4] = {16, 32, 128, 256};
-constexpr int kThreads[4] = {kFewThreads, kFewThreads, 512, 512};
-constexpr int kWideThreads = 512;
+// Bytes of prefixes that tiles of 32 rows of a group read less than its requests would, each by
+// itself, from which on the join's launch is worth it.  (8 KV heads of 128: 2 requests behind
+// 8,000 tokens, 33 MB saved, 13.3 us shared and 12.8 by themselves; 16 behind 500, 29 MB, 12.7
+// and 13.6; 4 behind 8,000, 98 MB, 14.4 and 23.3; one KV head: 16 behind 2,000, 12 MB, 12.4 and
+// 10.9; 48, 37 MB, 13.5 and 14.2.)
+constexpr int64_t kLeastSaved = int64_t(24) << 20;
+// Bytes that they read, through their L2s, from which on tiles of 128 rows in a launch of their
+// own are sooner done: they are bound by the matrix units, at less than half of the time.  (64
+// requests behind 13,000 tokens, 426 MB: 45.0 and 44.7 us; 128: 81 and 65; 250: 152 and 108; 250
+// behind 2,000, 260 MB: 54 and 62.)
+constexpr int64_t kMostRead = int64_t(400) << 20;
 
 struct Plan {
   bool shared;                 // false: each request by itself, `sh`
   Shape sh;
-  int prefix_kind, own_kind;
-  bool wide;                                     // eight waves behind the prefix
+  int few_rows;                // of a tile behind a prefix, 16 or 32
+  int many_rows;               // of a tile over a prefix, in a launch of its own; 0: few_rows
   int32_t prefix_split, own_split;
   int64_t prefix_splits, own_splits;             // records of a row
   int64_t need;
+  int prefix_rows() const { return many_rows ? many_rows : few_rows; }
 };
 
 int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
@@ -157,36 +152,39 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
     return fail(FLOWKV_EINVAL, "split_tokens %d: need 0 or a multiple of %d", split_tokens,
                 kSplitUnit);
   const int group = q_heads / kv_heads;
-  const int64_t together = int64_t(max_group) * group, one = int64_t(max_new) * group;
+  const int64_t one = int64_t(max_new) * group;  // rows of a request
+  auto tiles_at = [&](int64_t units, int64_t most_new, int rows) {
+    return std::max<int64_t>(tiles_of(n_tokens, units, group, most_new, rows) * kv_heads, 1);
+  };
+  const int64_t tiles32 = tiles_of(n_tokens, n_groups, group, max_group, 32);
+  const int64_t prefix_bytes = int64_t(max_prefix) * kv_heads * head_dim * 4;
   out->shared = n_groups > 0 && max_prefix > 0 &&
-                (split_tokens > 0 || (n_req > n_groups && one <= 128 && max_prefix >= 512));
+                (split_tokens > 0 ||
+                 (one <= 64 && (n_req * ((one + 31) / 32) - tiles32) * prefix_bytes >=
+                                   kLeastSaved));
+  // Tiles of 32 rows halve what a prefix is read, with two workgroups a CU instead of three.
+  const bool many = split_tokens > kFewSplit ||
+                    (split_tokens == 0 && tiles32 * prefix_bytes >= kMostRead);
+  out->few_rows = (many || int64_t(max_group) * group <= 16) && one <= 16 ? 16 : 32;
+  out->many_rows = many ? 128 : 0;
   if (!out->shared) {
     out->need = out->sh.need;
     return FLOWKV_OK;
   }
-  out->prefix_kind = together <= 16 ? 0 : together <= 32 ? 1 : 2;
-  if (tiles_of(n_tokens, n_groups, group, max_group, 256) * kv_heads >= kCus) out->prefix_kind = 3;
-  out->own_kind = one <= 16 ? 0 : one <= 64 ? 1 : 2;
   constexpr int64_t kAll = INT32_MAX / kSplitUnit * kSplitUnit;
-  auto tiles_at = [&](int kind, int64_t units, int64_t most_new) {
-    return std::max<int64_t>(tiles_of(n_tokens, units, group, most_new, kRows[kind]) * kv_heads,
-                             1);
-  };
-  auto split_of = [&](int kind, int64_t tiles, int32_t tokens, int64_t most) {
-    if (kind > 1) most = kAll;
+  auto split_of = [&](int64_t tiles, int32_t tokens, int64_t fixed, int64_t most) {
     if (split_tokens > 0) return int32_t(std::min<int64_t>(split_tokens, most));
-    return best_split(tiles, tokens, kind <= 1 ? 300 : 500, most);
+    return best_split(tiles, tokens, fixed, most);
   };
-  const int64_t own_tiles = tiles_at(out->own_kind, n_req, max_new);
-  out->prefix_split = split_of(out->prefix_kind, tiles_at(out->prefix_kind, n_groups, max_group),
-                               max_prefix, kFewSplit);
-  out->own_split = split_of(out->own_kind, own_tiles, max_own, kFewOwn);
+  const int64_t prefix_tiles = tiles_at(n_groups, max_group, out->prefix_rows());
+  out->prefix_split = split_of(prefix_tiles, max_prefix, out->many_rows ? 500 : 300,
+                               out->many_rows ? kAll : kFewSplit);
+  out->own_split = split_of(tiles_at(n_req, max_new, out->few_rows), max_own, 300, kFewSplit);
   auto splits_of = [](int32_t tokens, int32_t split) {
     return std::max<int64_t>((int64_t(tokens) + split - 1) / split, 1);
   };
   out->prefix_splits = splits_of(max_prefix, out->prefix_split);
   out->own_splits = splits_of(max_own, out->own_split);
-  out->wide = out->own_kind <= 1 && own_tiles * out->own_splits <= kCus;
   if (__builtin_mul_overflow(int64_t(n_tokens) * q_heads,
                              int64_t((head_dim + 2) * sizeof(float)), &out->need) ||
       __builtin_mul_overflow(out->need, out->prefix_splits + out->own_splits, &out->need))
@@ -195,56 +193,53 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
   return FLOWKV_OK;
 }
 
-// A part of units (requests or groups): its workgroups, or a failure where they are too many.
-int part_grid(const ChunkArgs& a, int kind, int threads, int64_t n_units, int64_t splits,
-              int64_t* grid) {
-  const int64_t tiles = tile_slots(a.n_tokens, n_units, a.group, kRows[kind]) * a.kv_heads;
-  if (tiles > UINT32_MAX / threads / splits)  // lanes of a launch in 32 bits
-    return fail(FLOWKV_EINVAL, "%lld tiles of queries x %lld splits: too many for one call",
-                (long long)tiles, (long long)splits);
-  *grid = tiles * splits;
-  return FLOWKV_OK;
-}
-
-hipError_t launch_part(const void* fn, int kind, int threads, int64_t grid, int64_t splits,
-                       int32_t split_tokens, SpanArgs& a, hipStream_t stream) {
-  a.split_tokens = split_tokens;
-  a.tiles = int32_t(grid / splits / a.kv_heads);
-  a.row_shift = 0;
-  while (1 << a.row_shift < kRows[kind]) ++a.row_shift;
-  void* args[] = {&a};
-  return hipLaunchKernel(fn, dim3(unsigned(grid)), dim3(unsigned(threads)), args, 0,
-                         stream);
+int row_shift(int rows) {
+  int shift = 0;
+  while (1 << shift < rows) ++shift;
+  return shift;
 }
 
 int launch_parts(int32_t dtype, const Plan& p, int head_dim, SpanArgs& a, hipStream_t stream) {
   const Parts& fn = parts(dtype);
-  const int d128 = head_dim == 128;
+  const int d128 = head_dim == 128, kv = a.kv_heads;
   const int64_t splits = p.prefix_splits + p.own_splits;
   const int64_t out_rows = int64_t(a.n_tokens) * a.q_heads;
   const bool one = splits <= kMergeChunk * 64 * 4 / head_dim;
   const int64_t merge = one ? (out_rows + 3) / 4 : out_rows;
-  if (merge > UINT32_MAX / kMergeThreads || splits > INT32_MAX)
-    return fail(FLOWKV_EINVAL, "%lld rows of output x %lld splits: too many for one call",
-                (long long)out_rows, (long long)splits);
-  int64_t prefix_grid, own_grid;
-  const int prefix_threads = kThreads[p.prefix_kind];
-  const int own_threads = p.wide ? kWideThreads : kThreads[p.own_kind];
-  int rc = part_grid(a, p.prefix_kind, prefix_threads, a.n_groups, p.prefix_splits, &prefix_grid);
-  if (rc) return rc;
-  rc = part_grid(a, p.own_kind, own_threads, a.n_req, p.own_splits, &own_grid);
-  if (rc) return rc;
+  const int64_t prefix_items =
+      tile_slots(a.n_tokens, a.n_groups, a.group, p.prefix_rows());
+  const int64_t own_tiles = tile_slots(a.n_tokens, a.n_req, a.group, p.few_rows);
+  // lanes of a launch in 32 bits; workgroups of prefixes and behind them, of a KV head
+  auto fits = [&](int64_t items, int64_t each, int threads) {
+    return each <= UINT32_MAX / threads / kv && items <= UINT32_MAX / threads / kv / each;
+  };
+  if (splits > INT32_MAX || merge > UINT32_MAX / kMergeThreads ||
+      !fits(prefix_items, p.prefix_splits, 1024) || !fits(own_tiles, p.own_splits, 1024))
+    return fail(FLOWKV_EINVAL,
+                "%lld tiles of prefixes x %lld splits, %lld behind them x %lld: too many for one "
+                "call", (long long)prefix_items, (long long)p.prefix_splits, (long long)own_tiles,
+                (long long)p.own_splits);
   a.splits = int32_t(splits);
   a.first_split = int32_t(p.prefix_splits);
   a.prefix_split = p.prefix_split;
   void* args[] = {&a};
-  hipError_t e = launch_part(fn.prefix[p.prefix_kind][d128], p.prefix_kind, prefix_threads,
-                             prefix_grid, p.prefix_splits, p.prefix_split, a, stream);
+  hipError_t e = hipSuccess;
+  if (p.many_rows) {
+    a.split_tokens = p.prefix_split;
+    a.row_shift = row_shift(p.many_rows);
+    e = hipLaunchKernel(fn.many[d128],
+                        dim3(unsigned(prefix_items * p.prefix_splits * kv)), dim3(512), args, 0,
+                        stream);
+  }
+  a.prefix_items = p.many_rows ? 0 : uint32_t(prefix_items * p.prefix_splits);
+  a.split_tokens = p.own_split;
+  a.row_shift = row_shift(p.few_rows);
+  a.tiles = int32_t(own_tiles);
   if (e == hipSuccess)
-    e = launch_part(p.wide ? fn.own_wide[p.own_kind][d128] : fn.own[p.own_kind][d128], p.own_kind,
-                    own_threads, own_grid, p.own_splits, p.own_split, a, stream);
-  // (one split behind the prefix, of few rows: its workgroup joins them)
-  if (e == hipSuccess && (p.own_splits > 1 || p.own_kind > 1))
+    e = hipLaunchKernel(fn.few[p.few_rows == 32][d128],
+                        dim3(unsigned((a.prefix_items + own_tiles * p.own_splits) * kv)),
+                        dim3(kFewThreads), args, 0, stream);
+  if (e == hipSuccess)
     e = hipLaunchKernel(fn.merge[d128][!one], dim3(unsigned(merge)), dim3(kMergeThreads), args, 0,
                         stream);
   if (e == hipSuccess) e = hipGetLastError();

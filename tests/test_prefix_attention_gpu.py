@@ -82,7 +82,7 @@ def test_against_the_formula(shape, groups, dtype):
     b, bounds, prefixes = group_batch(Geometry(f"pre{shape}", L, hk, d, bs, dtype), layout,
                                       GROUPS[groups], seed, pad=(seed % 3, seed % 4))
     q = queries(b, hk * G, seed, lead=(0, 8, 2 * d)[seed % 3])
-    for split in (0, [64, 128, 1024, 4096][seed % 4]):
+    for split in (0, [64, 128, 1024][seed % 3], 4096):
         say(f"prefix {dtype} {NAMES[layout]} shape {SHAPES[shape]} groups {groups} split {split}")
         out = attend(b, L - 1, q, d ** -0.5, bounds, prefixes, split)
         rel, worst = check_span(b, L - 1, q, d ** -0.5, out)
@@ -100,7 +100,22 @@ def test_llama8b_geometry(layout, groups):
     check_span(b, 2, q, 128 ** -0.5, attend(b, 2, q, 128 ** -0.5, bounds, prefixes))
 
 
-@pytest.mark.parametrize("split", [0, 64, 1024])
+@pytest.mark.parametrize("hk,d,G,dtype,groups", [
+    (8, 128, 4, "bfloat16", [(13000, [(1, 1 + i) for i in range(130)])]),
+    (4, 64, 4, "float16", [(9000, [(4, 5 + i) for i in range(60)]),
+                           (11000, [(3, 9 + 20 * i) for i in range(55)])]),
+])
+def test_prefixes_in_tiles_of_128_rows(hk, d, G, dtype, groups):
+    """So much of prefixes that the library's rule takes wide tiles, in several splits."""
+    b, bounds, prefixes = group_batch(Geometry("prewide", 1, hk, d, 16, dtype), BM, groups, 21)
+    most = sizes(b, bounds, prefixes)
+    rows, slot = b.n_tokens * G, hk * d * 4
+    assert (rows // 32) * most[3] * slot >= 400 << 20
+    q = queries(b, hk * G, 21)
+    check_span(b, 0, q, d ** -0.5, attend(b, 0, q, d ** -0.5, bounds, prefixes))
+
+
+@pytest.mark.parametrize("split", [0, 64, 1024, 4096])
 def test_rows_past_the_sizes_that_the_host_tells(split):
     """max_new and max_group below the requests' own, and sizes far above them."""
     groups = [(700, [(30, 40), (3, 33), (1, 900)]), (129, [(12, 12)] * 12)]
@@ -113,7 +128,7 @@ def test_rows_past_the_sizes_that_the_host_tells(split):
         check_span(b, 0, q, 0.09, attend(b, 0, q, 0.09, bounds, prefixes, split, most))
 
 
-@pytest.mark.parametrize("split", [0, 64])
+@pytest.mark.parametrize("split", [0, 64, 4096])
 def test_requests_of_no_group_and_new_tokens_within_a_prefix(split):
     groups = [(0, [(3, 90), (1, 5)]), (800, [(2, 5), (40, 41), (1, 1)]), (0, [(1, 300)] * 3)]
     b, bounds, prefixes = group_batch(Geometry("prenone", 1, 2, 64, 16, "float16"), LM, groups, 5)
@@ -142,12 +157,13 @@ def test_group_arrays_that_make_no_sense_touch_nothing_else():
     for bad, lens in (([-5, 9, 100], [600, 300]), ([9, 0, 13], [600, 300]), ([0, 9, 13], [-3, 2**31 - 1]),
                       ([13, 13, 13], [600, 600]), ([2**31 - 1, -2**31, 5], [5, 5]),
                       ([0, 13, 13], [10**6, 0])):
-        attend(b, 0, q, 0.1, bad, lens, 64, most)
+        for split in (64, 4096):
+            attend(b, 0, q, 0.1, bad, lens, split, most)
     attend(b, 0, q, 0.1, bounds, prefixes, 64, (1, 9, 3, 100))      # less than there is
     check_span(b, 0, q, 0.1, attend(b, 0, q, 0.1, bounds, prefixes, 64, most))
 
 
-@pytest.mark.parametrize("split", [64, 1024])
+@pytest.mark.parametrize("split", [64, 1024, 4096])
 def test_blocks_outside_the_pool_contribute_nothing(split):
     groups = [(400, [(1, 60), (2, 30), (70, 90)])]
     b, bounds, prefixes = group_batch(Geometry("prebad", 1, 2, 128, 16, "bfloat16"), LM, groups, 7)
@@ -160,7 +176,8 @@ def test_blocks_outside_the_pool_contribute_nothing(split):
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("d,dtype,n,split", [(64, "bfloat16", 3, 64), (128, "float16", 3, 1024),
-                                             (128, "bfloat16", 40, 64), (64, "float16", 40, 1024)])
+                                             (128, "bfloat16", 40, 64), (64, "float16", 40, 1024),
+                                             (128, "bfloat16", 40, 4096), (64, "float16", 3, 4096)])
 def test_odd_values_reach_only_the_rows_that_see_them(d, dtype, n, split, bad):
     """In the prefix: every row of the group, none of another.  Behind it: its request's.  In
     slots behind a prefix's part-filled last block, and behind the last token: none."""
@@ -200,7 +217,7 @@ def test_odd_values_reach_only_the_rows_that_see_them(d, dtype, n, split, bad):
             view[:, x, y] = z
 
 
-@pytest.mark.parametrize("split", [64, 0])
+@pytest.mark.parametrize("split", [64, 0, 4096])
 def test_large_scores_and_rising_maxima(split):
     groups = [(600, [(1, 40), (5, 30)] * 6)]
     b, bounds, prefixes = group_batch(Geometry("prebig", 1, 1, 64, 16, "float16"), BM, groups, 9)
@@ -223,7 +240,7 @@ def test_many_groups_and_blocks_beyond_4_gib():
         b, bounds, prefixes = group_batch(Geometry("premany", 1, hk, 128, 16, "bfloat16"), LM, groups,
                                           15, spare=spare)
         q = queries(b, 2 * hk, 15)
-        for split in (64, 0):
+        for split in (64, 0, 4096):
             check_span(b, 0, q, 0.1, attend(b, 0, q, 0.1, bounds, prefixes, split))
 
 
