@@ -39,6 +39,21 @@ def test_attention_kernels(tmp_path_factory, name, many, few, rest):
     check_occupancy({**manys, **fews})
 
 
+def body(asm, name):
+    return re.search(rf"^{re.escape(name)}:.*?^\.Lfunc_end", asm, re.S | re.M).group(0)
+
+
+def test_few_rows_read_k_and_v_past_the_caches(tmp_path_factory):
+    """(A branch round the two kinds of load once cost the hint, and 8% of a decode step.)"""
+    for name, kernel in (("flowkv_chunk", "chunk_attn_few"), ("flowkv_window", "window_attn_few"),
+                         ("flowkv_prefix", "alone_attn_few")):
+        asm = compiled(name, tmp_path_factory)
+        for n in kernel_entries(asm, kernel):
+            d = int(re.search(r"fewILi(64|128)E", n).group(1))
+            past = len(re.findall(r"^\s+global_load_dword\S*\s.*\bnt\b", body(asm, n), re.M))
+            assert past >= 2 * (d // 16 + 4), (n, past)
+
+
 def test_rotated_append_kernels(tmp_path_factory):
     entries = kernel_entries(compiled("flowkv_rotate", tmp_path_factory), "kv_rotate")
     assert len(entries) == 18
