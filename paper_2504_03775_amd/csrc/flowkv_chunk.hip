@@ -61,12 +61,12 @@ struct Table {
   }
 };
 
-}  // namespace
-
-const Kernels& flowkv::chunk::causal_bf16() {
+const Kernels& kernels() {
   static const Kernels k = kernels_of<Table>();
   return k;
 }
+
+}  // namespace
 
 extern "C" int flowkv_chunk_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q_heads,
                                                 int32_t kv_heads, int32_t head_dim,
@@ -74,8 +74,8 @@ extern "C" int flowkv_chunk_attention_workspace(int32_t n_tokens, int32_t n_req,
                                                 int32_t split_tokens, int64_t* bytes) {
   if (!bytes) return fail(FLOWKV_EINVAL, "NULL output");
   Shape sh;
-  const int rc = plan_shape(causal_bf16(), n_tokens, n_req, q_heads, kv_heads, head_dim, max_new,
-                            Span{max_seq_len}, split_tokens, &sh);
+  const int rc = plan_shape(kernels(), n_tokens, n_req, q_heads, kv_heads, head_dim, max_new,
+                            Span{max_seq_len}, split_tokens, false, &sh);
   if (rc) return rc;
   *bytes = sh.need;
   return ok();
@@ -97,8 +97,8 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   int rc = check_pool(c);
   if (rc) return rc;
   Shape sh;
-  rc = plan_shape(causal_bf16(), n_tokens, n_req, q_heads, kv_heads, head_dim, max_new,
-                  Span{max_seq_len}, split_tokens, &sh);
+  rc = plan_shape(kernels(), n_tokens, n_req, q_heads, kv_heads, head_dim, max_new,
+                  Span{max_seq_len}, split_tokens, false, &sh);
   if (rc) return rc;
   rc = check_sizes(c);
   if (rc) return rc;
@@ -107,5 +107,5 @@ extern "C" int flowkv_chunk_attention(const flowkv_pool* pool, int32_t layer, co
   if (rc) return rc;
   ChunkArgs a{};
   fill(c, &a);
-  return launch(causal_bf16(), sh, max_new, head_dim, a, c.stream);
+  return launch(kernels(), sh, max_new, head_dim, a, c.stream);
 }

@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "flowkv.h"
 #include "flowkv_chunk_kernels.h"
@@ -41,6 +42,8 @@ struct Kernels {
   const void* merge[2][2];                       // head_dim; a wave or four a row
 };
 constexpr int kSplitUnit = 64;
+constexpr int kTailRounds = 4;             // most rounds of tiles that have a tail,
+constexpr int kTailSteps = 32;             // and the least steps
 constexpr int kFewSteps = 8;               // of 32 tokens, a CU
 
 // x / d = (umulhi(x, m) + x) >> l with l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1.
@@ -49,9 +52,6 @@ inline void by_product(uint32_t d, uint32_t* magic, uint32_t* shift) {
   while ((uint64_t(1) << *shift) < d) ++*shift;
   *magic = uint32_t((((uint64_t(1) << *shift) - d) << 32) / d + 1);
 }
-
-// Those of attention over all of a bf16 cache (flowkv_chunk.hip).
-const Kernels& causal_bf16();
 
 // From a table of the kernels: many<F>(cut), join<F>(), few<kDh, kC>(), merge<kDh, kWavesPer>().
 template <class Table>
@@ -104,6 +104,7 @@ struct Shape {
   int kind;
   int32_t split, splits, pieces;
   bool cut, order;                               // pieces by the lengths; tiles, the longest first
+  bool tail;                                     // whole tiles, then pieces
   int64_t need;
 };
 
@@ -152,7 +153,7 @@ struct Span {
 // The form and the split of a call, and the workspace that it takes.
 inline int plan_shape(const Kernels& kernels, int32_t n_tokens, int32_t n_req, int32_t q_heads,
                       int32_t kv_heads, int32_t head_dim, int32_t max_new, const Span& span,
-                      int32_t split_tokens, Shape* out) {
+                      int32_t split_tokens, bool tail, Shape* out) {
   const Kind* kKinds = kernels.kind;
   if (n_tokens < 0 || n_req < 0 || max_new < 0 || span.max_seq_len < 0)
     return fail(FLOWKV_EINVAL, "negative sizes");
@@ -191,9 +192,10 @@ inline int plan_shape(const Kernels& kernels, int32_t n_tokens, int32_t n_req, i
       return INT64_MAX;
     return bytes;
   };
-  auto by_pieces = [&](int kind) {
+  auto by_pieces = [&](int kind, bool behind_whole) {
     out->kind = kind;
-    out->cut = true;
+    out->cut = !behind_whole;
+    out->tail = behind_whole;
     out->split = 0;
     out->splits = 1;
     out->pieces = kKinds[kind].per_cu[head_dim == 128] * kCus;
@@ -207,7 +209,7 @@ inline int plan_shape(const Kernels& kernels, int32_t n_tokens, int32_t n_req, i
   };
   constexpr int32_t kAll = INT32_MAX / kSplitUnit * kSplitUnit;
   const int cut_kind = head_dim == 128 ? 3 : 2;  // the form that has pieces
-  out->cut = out->order = false;
+  out->cut = out->order = out->tail = false;
   if (split_tokens <= kFewSplit && !many) {
     out->kind = int64_t(max_new) * group > 16;
   } else if (rule && t32 <= kCus && t32 * ((length(1) + 31) / 32) <= kFewSteps * kCus &&
@@ -220,10 +222,16 @@ inline int plan_shape(const Kernels& kernels, int32_t n_tokens, int32_t n_req, i
     const int64_t tiles = cut_kind == 3 ? t256 : t128, step = kKinds[cut_kind].step;
     if (rule && tiles < kCus && takes_lengths(cut_kind) &&
         tiles * ((length(cut_kind) + step - 1) / step) >= kCutSteps * kCus)
-      return by_pieces(cut_kind);
+      return by_pieces(cut_kind, false);
     out->kind = 2;
   }
   const Kind& kind = kKinds[out->kind];
+  if (tail && rule && out->kind == cut_kind && head_dim == 128 && takes_lengths(cut_kind)) {
+    const int64_t round = int64_t(kind.per_cu[1]) * kCus;
+    if (t256 > round && t256 <= kTailRounds * round &&
+        length(cut_kind) >= int64_t(kTailSteps) * kind.step)
+      return by_pieces(cut_kind, true);
+  }
   if (rule && out->kind >= 2 && n_req > 1 && span.max_seq_len / 2 >= max_new &&
       (out->kind == 3 ? t256 : t128) > kCus && takes_lengths(out->kind)) {
     out->order = true;
@@ -240,7 +248,7 @@ inline int plan_shape(const Kernels& kernels, int32_t n_tokens, int32_t n_req, i
     else split_tokens = tiles < kCus ? best_split(tiles, length(out->kind), 500, kAll) : kAll;
     // padding and few steps, as a rule: pieces, or the splits that the workspace has room for
     if (many && bytes_of(out->kind, split_tokens) > kRuleBytes) {
-      if (takes_lengths(cut_kind)) return by_pieces(cut_kind);
+      if (takes_lengths(cut_kind)) return by_pieces(cut_kind, false);
       while (split_tokens < kAll && bytes_of(out->kind, split_tokens) > kRuleBytes)
         split_tokens = split_tokens < kAll / 2 ? 2 * split_tokens : kAll;
     }
@@ -404,16 +412,20 @@ int launch(const Kernels& kernels, const Shape& sh, int32_t max_new, int head_di
     return fail(FLOWKV_EINVAL, "%lld tiles of queries x %d splits: too many for one call",
                 (long long)grid, sh.splits);
   a.tiles = int32_t(tiles);
-  if (sh.cut || sh.order)
+  if (sh.cut || sh.order || sh.tail)
     a.tiles = int32_t(used_slots(a.n_tokens, a.n_req, a.group, max_new, kind.rows));
   a.pieces = sh.pieces;
+  if constexpr (std::is_same_v<Args, SpanArgs>) a.tail = sh.tail;
   void* args[] = {&a};
   const int d128 = head_dim == 128;
-  const int64_t groups = sh.cut ? std::max<int64_t>(grid, sh.pieces) : grid * sh.splits;
-  hipError_t e = hipLaunchKernel(sh.cut || sh.order ? kind.cut[d128] : kind.fn[d128],
+  const int64_t groups =
+      sh.tail  ? std::max(grid, int64_t(a.tiles) * a.kv_heads + sh.pieces)
+      : sh.cut ? std::max<int64_t>(grid, sh.pieces)
+               : grid * sh.splits;
+  hipError_t e = hipLaunchKernel(sh.cut || sh.order || sh.tail ? kind.cut[d128] : kind.fn[d128],
                                  dim3(unsigned(groups)), dim3(unsigned(kind.threads)), args, 0,
                                  stream);
-  if (e == hipSuccess && sh.cut)
+  if (e == hipSuccess && (sh.cut || sh.tail))
     e = hipLaunchKernel(kind.join[d128], dim3(unsigned(a.tiles * a.kv_heads * (kind.rows / 32))),
                         dim3(unsigned(2 * head_dim)), args, 0, stream);
   if (e == hipSuccess && sh.splits > 1)

@@ -111,6 +111,7 @@ struct SpanArgs : ChunkArgs {
   const int32_t* groups;                // (n_groups + 1) requests of shared prefixes
   const int32_t* prefix_lens;           // (n_groups)
   int32_t n_groups, max_prefix;
+  int32_t tail;                         // the tiles behind the last whole round in pieces
   int32_t max_own;                      // tokens of a request behind its prefix
   int32_t first_split;                  // records of a row: [0, first_split) of its prefix,
   int32_t prefix_split;                 // this many tokens each, the others its own
@@ -129,7 +130,7 @@ __device__ __forceinline__ A late_args() {
 
 // What the calls differ in: the element type, which tokens a row sees, and whose rows make
 // up a tile.
-//   Causal    a request's rows, over all tokens up to each row's own
+//   Causal    a request's rows, over all tokens up to each row's own (Alone: with a tail)
 //   Windowed  the same, over the last `window` of them and the first `sinks`
 //   Prefixed  the rows of a whole group of requests, over the prefix that they share
 //   Shared    (few rows) the same in some workgroups, and in the others a request's rows, over
@@ -138,25 +139,31 @@ template <class T_>
 struct Causal {
   typedef T_ T;
   typedef ChunkArgs Args;
-  static constexpr bool kWindow = false, kPrefix = false, kShared = false;
+  static constexpr bool kWindow = false, kPrefix = false, kShared = false, kTail = false;
+};
+template <class T_>
+struct Alone {
+  typedef T_ T;
+  typedef SpanArgs Args;
+  static constexpr bool kWindow = false, kPrefix = false, kShared = false, kTail = true;
 };
 template <class T_>
 struct Windowed {
   typedef T_ T;
   typedef SpanArgs Args;
-  static constexpr bool kWindow = true, kPrefix = false, kShared = false;
+  static constexpr bool kWindow = true, kPrefix = false, kShared = false, kTail = true;
 };
 template <class T_>
 struct Prefixed {
   typedef T_ T;
   typedef SpanArgs Args;
-  static constexpr bool kWindow = false, kPrefix = true, kShared = false;
+  static constexpr bool kWindow = false, kPrefix = true, kShared = false, kTail = false;
 };
 template <class T_>
 struct Shared {
   typedef T_ T;
   typedef SpanArgs Args;
-  static constexpr bool kWindow = false, kPrefix = false, kShared = true;
+  static constexpr bool kWindow = false, kPrefix = false, kShared = true, kTail = false;
 };
 
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -698,6 +705,10 @@ struct Source {
 //     first, so that the last ones to end are short.  4 chunks of 100 to 600 tokens beside 36
 //     single ones over 100 to 6,600, 32 heads on 8: 251 us, in the requests' order 326.
 //     (Prompts with nothing cached gain nothing: the diagonal orders each of them.)
+// A third kind, where tiles are long and a few rounds of the CUs (kTail): as many whole tiles as
+// fill rounds, the longest first, and the rest of them in pieces, one round more.  (16 prompts of
+// 50 to 700 tokens behind 3,000 and 5,000, 20 heads of 128 on 4, 533 tiles on 256 CUs: 446 us in
+// whole tiles, three rounds.)
 constexpr int kPieceTiles = 512;           // most tile slots, and requests, of such a call
 constexpr int kPieceLeast = 2;             // steps
 constexpr int kCutSteps = 16;              // steps a CU, were all tiles the longest, from which on
@@ -775,8 +786,12 @@ __device__ __forceinline__ Mine cut_tiles(const typename P::Args& a, Cut& c, int
     mine.split = 0;
     return mine;
   }
-  const uint32_t id = a.pieces ? blockIdx.x : paired<F>();
-  if (id >= uint32_t(std::max(a.tiles * a.kv_heads, a.pieces))) return mine;   // (padding's)
+  uint32_t id = a.pieces ? blockIdx.x : paired<F>();
+  bool tail = false;
+  if constexpr (P::kTail) tail = a.tail != 0;
+  const uint32_t slots = uint32_t(a.tiles * a.kv_heads);
+  // (padding's; with a tail, fewer than `pieces` whole tiles and as many pieces are behind)
+  if (id >= (tail ? slots + uint32_t(a.pieces) : std::max(slots, uint32_t(a.pieces)))) return mine;
   // (at most kPieceTiles x kRows rows: 32 bits hold what valid offsets give)
   if (tid < a.n_req)
     c.start[tid] = int32_t(uint32_t(a.offsets[tid] - first) * uint32_t(a.group) / F::kRows) + tid;
@@ -803,10 +818,21 @@ __device__ __forceinline__ Mine cut_tiles(const typename P::Args& a, Cut& c, int
       n = limit > F::kStep ? (limit + F::kStep - 1) / F::kStep : 1;
     }
   }
-  if (a.pieces == 0) {                           // each counts the longer ones
+  int32_t whole = INT32_MAX;                     // with a tail: whole tiles of a KV head
+  if (a.pieces == 0 || tail) {                   // each counts the longer ones
     const uint32_t key = uint32_t(n) * kPieceTiles + uint32_t(tid);
     c.key[tid] = key;
+    if (tail) {
+      const int32_t some = __popcll(__ballot(n > 0));
+      if (ln == 0) c.part[0][wave] = some;
+    }
     __syncthreads();
+    if (tail) {
+      int32_t all = 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) all += c.part[0][w];
+      whole = all * a.kv_heads / a.pieces * a.pieces / a.kv_heads;
+    }
     g = int(id % uint32_t(a.kv_heads));
     if (n > 0) {
       int32_t before = 0;
@@ -818,14 +844,17 @@ __device__ __forceinline__ Mine cut_tiles(const typename P::Args& a, Cut& c, int
         before += x[2] > key;
         before += x[3] > key;
       }
-      if (before == int32_t(id / uint32_t(a.kv_heads))) {
+      if (tail && before < whole) n = 0;         // (not one of the tail's)
+      if (before < whole && before == int32_t(id / uint32_t(a.kv_heads))) {
         mine.split = 0;
         mine.pieces = 1;
         c.mine = mine;
       }
     }
     __syncthreads();
-  } else {
+  }
+  if (a.pieces != 0 && (!tail || id >= uint32_t(whole * a.kv_heads))) {
+    if (tail) id -= uint32_t(whole * a.kv_heads);
     c.steps[tid] = float(n);
     int32_t sum = n, most = n;
 #pragma unroll

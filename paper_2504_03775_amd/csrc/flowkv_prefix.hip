@@ -47,48 +47,50 @@ __global__ __launch_bounds__(kMergeThreads) void prefix_attn_merge(const SpanArg
 
 // ---- each request by itself ----------------------------------------------------------------
 
-template <class F, bool kCut>
+template <class F, bool kCut, class T>
 __global__ __launch_bounds__(F::kThreads, 2 * F::kPerCu)
-void alone_attn(const ChunkArgs a) {
-  attend_many<F, kCut, Causal<Fp16>>(a);
+void alone_attn(const SpanArgs a) {
+  attend_many<F, kCut, Alone<T>>(a);
 }
-template <class F>
-__global__ __launch_bounds__(2 * F::kDh) void alone_attn_join(const ChunkArgs a) {
-  join_pieces<F, Fp16>(a);
+template <class F, class T>
+__global__ __launch_bounds__(2 * F::kDh) void alone_attn_join(const SpanArgs a) {
+  join_pieces<F, T>(a);
 }
-template <int kDh, int kC>
+template <int kDh, int kC, class T>
 __global__ __launch_bounds__(kFewThreads, few_per_cu(kDh, kC))
-void alone_attn_few(const ChunkArgs a) {
-  attend_few<kDh, kC, Causal<Fp16>>(a);
+void alone_attn_few(const SpanArgs a) {
+  attend_few<kDh, kC, Alone<T>>(a);
 }
-template <int kDh, int kWavesPer>
-__global__ __launch_bounds__(kMergeThreads) void alone_attn_merge(const ChunkArgs a) {
-  merge_splits<kDh, kWavesPer, Causal<Fp16>>(a);
+template <int kDh, int kWavesPer, class T>
+__global__ __launch_bounds__(kMergeThreads) void alone_attn_merge(const SpanArgs a) {
+  merge_splits<kDh, kWavesPer, Alone<T>>(a);
 }
 
-struct Alone {
+template <class T>
+struct AloneTable {
   template <class F>
   static const void* many(bool cut) {
-    return cut ? reinterpret_cast<const void*>(alone_attn<F, true>)
-               : reinterpret_cast<const void*>(alone_attn<F, false>);
+    return cut ? reinterpret_cast<const void*>(alone_attn<F, true, T>)
+               : reinterpret_cast<const void*>(alone_attn<F, false, T>);
   }
   template <class F>
   static const void* join() {
-    return reinterpret_cast<const void*>(alone_attn_join<F>);
+    return reinterpret_cast<const void*>(alone_attn_join<F, T>);
   }
   template <int kDh, int kC>
   static const void* few() {
-    return reinterpret_cast<const void*>(alone_attn_few<kDh, kC>);
+    return reinterpret_cast<const void*>(alone_attn_few<kDh, kC, T>);
   }
   template <int kDh, int kWavesPer>
   static const void* merge() {
-    return reinterpret_cast<const void*>(alone_attn_merge<kDh, kWavesPer>);
+    return reinterpret_cast<const void*>(alone_attn_merge<kDh, kWavesPer, T>);
   }
 };
 
 const Kernels& alone(int32_t dtype) {
-  static const Kernels fp16 = kernels_of<Alone>();
-  return dtype == FLOWKV_BF16 ? causal_bf16() : fp16;
+  static const Kernels bf16 = kernels_of<AloneTable<Bf16>>(),
+                       fp16 = kernels_of<AloneTable<Fp16>>();
+  return dtype == FLOWKV_BF16 ? bf16 : fp16;
 }
 
 // ---- the host's part -----------------------------------------------------------------------
@@ -146,7 +148,7 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
                 (long long)longest);
   // (its checks of the sizes hold for either way)
   const int rc = plan_shape(alone(FLOWKV_BF16), n_tokens, n_req, q_heads, kv_heads, head_dim,
-                            max_new, Span{int32_t(longest)}, 0, &out->sh);
+                            max_new, Span{int32_t(longest)}, 0, true, &out->sh);
   if (rc) return rc;
   if (split_tokens < 0 || split_tokens % kSplitUnit)
     return fail(FLOWKV_EINVAL, "split_tokens %d: need 0 or a multiple of %d", split_tokens,
@@ -302,5 +304,5 @@ extern "C" int flowkv_prefix_attention(
   a.max_prefix = max_prefix;
   a.max_own = max_own;
   if (p.shared) return launch_parts(dtype, p, head_dim, a, c.stream);
-  return launch<ChunkArgs>(alone(dtype), p.sh, max_new, head_dim, a, c.stream);
+  return launch(alone(dtype), p.sh, max_new, head_dim, a, c.stream);
 }

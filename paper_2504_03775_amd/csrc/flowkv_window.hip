@@ -75,7 +75,7 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
     return fail(FLOWKV_EINVAL, "window of %d tokens and %d first ones: need 1 and 0 at least",
                 window, sinks);
   return plan_shape(kernels(FLOWKV_BF16), n_tokens, n_req, q_heads, kv_heads, head_dim, max_new,
-                    Span{max_seq_len, window, sinks}, split_tokens, out);
+                    Span{max_seq_len, window, sinks}, split_tokens, true, out);
 }
 
 }  // namespace

@@ -92,6 +92,8 @@ def span_plain(b, layer, q, scale, window=0, sinks=0, max_seq=None):
                     for i in range(p.shape[0]):
                         c = see[sl][i]
                         o[sl.start + i, h] = (p[i, c, None] * v[c]).sum(0)
+                        w1[sl.start + i, h] = (p[i, c, None] * v[c].abs()).sum(0)
+                        vs[sl.start + i, h] = v[c].abs().sum(0)
                 s1[sl, h] = torch.where(see[sl], (x[sl, h].abs() @ kt.abs()) * scale, 0.).amax(1)
         res.append((o, w1, s1, vs))
         rows += range(int(b.off[r]), int(b.off[r]) + m)

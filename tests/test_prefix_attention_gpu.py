@@ -115,6 +115,16 @@ def test_prefixes_in_tiles_of_128_rows(hk, d, G, dtype, groups):
     check_span(b, 0, q, d ** -0.5, attend(b, 0, q, d ** -0.5, bounds, prefixes))
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_prompts_behind_prefixes_each_by_itself(dtype):
+    """Many rows a request: whole tiles, and a tail of them in pieces."""
+    groups = [(2100, [(300, 300), (130, 130), (64, 90)]), (3000, [(500, 500), (90, 90)])]
+    b, bounds, prefixes = group_batch(Geometry("prealone", 1, 8, 128, 16, dtype), LM, groups, 22)
+    q = queries(b, 64, 22)
+    out = attend(b, 0, q, 0.09, bounds, prefixes)
+    check_span(b, 0, q, 0.09, out)
+
+
 @pytest.mark.parametrize("split", [0, 64, 1024, 4096])
 def test_rows_past_the_sizes_that_the_host_tells(split):
     """max_new and max_group below the requests' own, and sizes far above them."""

@@ -25,7 +25,7 @@ def check_occupancy(entries):
 
 
 @pytest.mark.parametrize("name,many,few,rest", [
-    ("flowkv_window", 16, 8, 12), ("flowkv_prefix", 12, 12, 14),
+    ("flowkv_window", 16, 8, 12), ("flowkv_prefix", 20, 16, 20),
 ])
 def test_attention_kernels(tmp_path_factory, name, many, few, rest):
     asm = compiled(name, tmp_path_factory)

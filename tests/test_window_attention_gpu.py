@@ -113,6 +113,96 @@ def test_tiles_in_the_order_of_the_lengths(hk, d, G, n_req, top):
         check_span(b, 0, q, d ** -0.5, attend(b, 0, q, d ** -0.5, window, sinks), window, sinks)
 
 
+TAILS = [  # (KV heads, query heads per KV head, new tokens, tokens in all): from 256 tiles of 256 rows on
+    (8, 8, [1030], [4000]),                             # 33 tiles a head: one behind a round
+    (8, 8, [700, 40, 300, 1], [3000, 5000, 300, 2900]), (8, 8, [2040], [2600]),     # 64: no tail
+    (16, 4, [1500, 9], [1500, 8000]), (5, 16, [900, 0, 100], [2500, 9, 4000]),
+    (2, 40, [600, 333], [3100, 2400]), (8, 8, [200] * 9, [2000 + 300 * i for i in range(9)]),
+]
+
+
+def tail_bytes(tiles):
+    """Workspace of 256 pieces of 256 rows, and of the pieces before each tile slot."""
+    return (256 * 256 * 130 + tiles + 1) * 4
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("case", range(len(TAILS)))
+def test_whole_tiles_and_a_tail_in_pieces(case, dtype):
+    hk, G, new, total = TAILS[case]
+    b = Batch(Geometry("wintail", 1, hk, 128, 16, dtype), (BM, LM)[case % 2], new, total, 40 + case,
+              pad=(case % 3, 2 * case))
+    q = queries(b, hk * G, 40 + case)
+    for window, sinks in ((2**18, 3), (2300, 40)):
+        slots = b.n_tokens * G // 256 + len(new)
+        assert fk.flowkv_window_attention_workspace(b.n_tokens, len(new), hk * G, hk, 128, b.max_new,
+                                                    8000, window, sinks) == tail_bytes(slots)
+        say(f"tail {hk} x {G} new {new} of {total} window {window} + {sinks} {dtype}")
+        out = attend(b, 0, q, 128 ** -0.5, window, sinks, max_len=8000)
+        check_span(b, 0, q, 128 ** -0.5, out, window, sinks, max_seq=8000)
+        # rows that the host was not told of: whole tiles
+        out = attend(b, 0, q, 128 ** -0.5, window, sinks, max_len=8000, max_new=b.max_new - 9)
+        check_span(b, 0, q, 128 ** -0.5, out, window, sinks, max_seq=8000)
+
+
+def test_a_tail_keeps_the_rules():
+    """NaN and infinities that no row sees, missing blocks, rows that see nothing."""
+    b = Batch(Geometry("wintailodd", 1, 8, 128, 16, "bfloat16"), BM, [1030, 60], [4000, 40], 47)
+    q = queries(b, 64, 47)
+    window, sinks = 2500, 5
+    ref = attend(b, 0, q, 0.09, window, sinks, max_len=8000)
+    check_span(b, 0, q, 0.09, ref, window, sinks, max_seq=8000)
+    view, base = b.layer_view(0), 4000 - 1030
+    for p in range(sinks, base - window + 1):
+        view[:, int(b.tab[0, p // 16]), p % 16] = float("nan")
+    assert torch.equal(attend(b, 0, q, 0.09, window, sinks, max_len=8000), ref)
+    at = base - window + 300                    # (seen by the first 300 rows)
+    view[1, int(b.tab[0, at // 16]), at % 16, :, 7] = float("inf")
+    out = attend(b, 0, q, 0.09, window, sinks, max_len=8000)
+    assert (out[:300, :, 7].float() == float("inf")).all()
+    assert torch.equal(out[300:], ref[300:])
+    b.tab[0, 100:140] = -1
+    b.upload()
+    view[1][view[1] == float("inf")] = 0
+    check_span(b, 0, q, 0.09, attend(b, 0, q, 0.09, window, sinks, max_len=8000), window, sinks,
+               max_seq=8000)
+
+
+def test_a_tail_in_a_replayed_graph_and_on_two_streams():
+    b = Batch(Geometry("wintailgraph", 2, 8, 128, 16, "bfloat16"), BM, [1030, 60], [4000, 3000], 48)
+    q = queries(b, 64, 48)
+    ref = [attend(b, l, q, 0.09, 2500, 4, max_len=8000) for l in range(2)]
+    need = tail_bytes(1090 * 8 // 256 + 2)
+    out = [torch.zeros_like(r) for r in ref]
+    ws = [torch.full((need,), 255, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+
+    def call(l=1, stream=None):
+        fk.flowkv_window_attention(b.pool, l, q, *b.args(), 1090, 8000, 2500, 4, 0.09, out[l], ws[l],
+                                   stream=stream)
+    for i in range(5):
+        for l in range(2):
+            call(l, streams[l])
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], ref[0]) and torch.equal(out[1], ref[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for new, total in (([1030, 60], [4000, 3000]), ([0, 1024], [9, 4000]), ([545, 545], [700, 545]),
+                       ([3, 2], [3000, 3999])):
+        b.new, b.total = np.asarray(new), np.asarray(total)
+        b.off = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
+        b.offsets.copy_(torch.as_tensor(b.off))
+        b.lens.copy_(torch.as_tensor(b.total.astype(np.int32)))
+        out[1].fill_(float("nan"))
+        ws[1].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_span(b, 1, q, 0.09, out[1], 2500, 4, max_seq=8000)
+        assert torch.isnan(out[1][int(b.off[-1]):].float()).all()
+
+
 @pytest.mark.parametrize("split", [0, 64, 2048])
 @pytest.mark.parametrize("new,total", [([3], [700]), ([200, 1, 40], [700, 64, 300]),
                                        ([700], [700]), ([1] * 30, [50 * i + 1 for i in range(30)])])
