@@ -162,14 +162,15 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
     return std::max<int64_t>(tiles_of(n_tokens, units, group, most_new, rows) * kv_heads, 1);
   };
   const int64_t tiles32 = tiles_of(n_tokens, n_groups, group, max_group, 32);
-  const int64_t prefix_bytes = int64_t(max_prefix) * kv_heads * head_dim * 4;
+  // (in double: tiles of it pass 63 bits where max_prefix is set to the most there can be)
+  const double prefix_bytes = double(max_prefix) * kv_heads * head_dim * 4;
   out->shared = n_groups > 0 && max_prefix > 0 &&
                 (split_tokens > 0 ||
-                 (one <= 64 && (n_req * ((one + 31) / 32) - tiles32) * prefix_bytes >=
-                                   kLeastSaved));
+                 (one <= 64 && double(n_req * ((one + 31) / 32) - tiles32) * prefix_bytes >=
+                                   double(kLeastSaved)));
   // Tiles of 32 rows halve what a prefix is read, with two workgroups a CU instead of three.
   const bool many = split_tokens > kFewSplit ||
-                    (split_tokens == 0 && tiles32 * prefix_bytes >= kMostRead);
+                    (split_tokens == 0 && double(tiles32) * prefix_bytes >= double(kMostRead));
   out->few_rows = (many || int64_t(max_group) * group <= 16) && one <= 16 ? 16 : 32;
   out->many_rows = many ? 128 : 0;
   if (!out->shared) {

@@ -272,8 +272,8 @@ extern "C" int flowkv_append_rotated(
   if (q_heads < 0 || kv_heads < 1 || head_dim < 1)
     return fail(FLOWKV_EINVAL, "%d query heads, %d KV heads, head_dim %d", q_heads, kv_heads,
                 head_dim);
-  const int64_t e = dtype == FLOWKV_F32 ? 4 : 2, head = head_dim * e, slot = kv_heads * head;
-  if (head % 16 || pool->chunk_bytes % slot)
+  const int64_t e = dtype == FLOWKV_F32 ? 4 : 2, head = head_dim * e;
+  if (head % 16 || kv_heads > pool->chunk_bytes / head || pool->chunk_bytes % (kv_heads * head))
     return fail(FLOWKV_EINVAL,
                 "heads of %lld bytes: need a multiple of 16 whose %d KV heads divide chunk_bytes "
                 "%lld", (long long)head, kv_heads, (long long)pool->chunk_bytes);
@@ -307,7 +307,7 @@ extern "C" int flowkv_append_rotated(
   if (reinterpret_cast<uintptr_t>(cos_sin_dev) % 4)
     return fail(FLOWKV_EINVAL, "cosines not 4-byte aligned");
   const Variant variant = n_tokens * heads * per_head <= kRotateFew ? kOneHead
-                          : n_tokens * heads * head <= kRotatePast  ? kTwoHeads
+                          : n_tokens * heads <= kRotatePast / head  ? kTwoHeads
                                                                     : kTwoHeadsPast;
   const int64_t per = (variant == kOneHead ? heads : (heads + 1) / 2) * per_head;
   const int64_t items = n_tokens * per;
@@ -337,7 +337,7 @@ extern "C" int flowkv_append_rotated(
   a.n_req = n_req;
   a.max_blocks = max_blocks;
   a.pool_blocks = pool->num_blocks;
-  a.block_size = int32_t(pool->chunk_bytes / slot);
+  a.block_size = int32_t(pool->chunk_bytes / (kv_heads * head));
   a.q_heads = q_heads;
   a.kv_heads = kv_heads;
   a.pieces = int32_t(head / 16);

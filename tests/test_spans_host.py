@@ -39,6 +39,10 @@ def test_append_rotated_rejects_bad_arguments_without_touching_the_device():
               dict(table=(1 << 18) + 2), dict(hq=2**31 - 1), dict(n=2**31 - 1),
               dict(hk=4, ks=512, vs=512, d=192)):
         assert rotated(p, **c) == fk.EINVAL, c
+    # sizes whose products pass 64 bits
+    for c in (dict(hk=2**31 - 1, d=2**31 - 16), dict(hk=2**30, d=2**30, dtype=2),
+              dict(hk=1, ks=128, vs=128, n=2**31 - 1, hq=2**29, qs=2**36, qos=2**36)):
+        assert rotated(p, **c) == fk.EINVAL, c
     # 4-byte elements: a slot of 2 x 128 is twice as large, rotations come in 8 elements
     big = pool(chunk=16 * 2 * 128 * 4)
     assert rotated(big, dtype=2, n=0, rot=8) == fk.OK
@@ -156,6 +160,9 @@ def test_prefix_workspace_holds_every_record():
     ws = fk.flowkv_prefix_attention_workspace
     assert ws(4, 4, 8, 2, 128, 1, 1, 4, 20, 40, 64) == 4 * 8 * 2 * 130 * 4
     assert ws(4, 4, 8, 2, 128, 1, 1, 4, 65, 129, 64) == 4 * 8 * 5 * 130 * 4
+    # the library's rule with the most tokens of a prefix that there can be: shared, in long splits
+    # (the bytes that sharing saves, 2^24 requests' x 2^42, pass 63 bits)
+    assert ws(1 << 24, 1 << 24, 8, 8, 128, 1, 1, 1 << 24, 64, 1 << 30) <= (1 << 24) * 8 * 8 * 130 * 4
     # each by itself: as attention over all of it
     full = fk.flowkv_chunk_attention_workspace
     assert ws(700, 2, 8, 2, 128, 0, 600, 0, 3000, 0) == full(700, 2, 8, 2, 128, 600, 3000)
