@@ -562,7 +562,8 @@ int flowkv_chunk_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q_
    window >= 1 counts the token itself; sinks >= 0.  Tokens that no new token of a request sees
    are not looked up: their entries of the block list may hold anything (their blocks freed).
    dtype: FLOWKV_BF16 or FLOWKV_FP16, the type of q, the pool and out (weights enter the matrix
-   product rounded to it).  Split by split_tokens are the tokens that a workgroup's rows see
+   product rounded to it; in fp16 an output within 2^-10 of the type's largest value may become
+   infinite).  Split by split_tokens are the tokens that a workgroup's rows see
    between them, the first ones and those of its window.  The rest, single tokens of a decode
    step among it, is as for flowkv_chunk_attention: K and V of tokens that a row does not see,
    infinities and NaN among them, do not reach it, and a row that sees nothing gets zeros.
@@ -593,7 +594,7 @@ int flowkv_window_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q
    the group's first request is the one read for the prefix.  Every row sees all tokens up to
    its own position, those of the prefix and those behind it: the result is that of
    flowkv_chunk_attention, joined in another order.
-   dtype: FLOWKV_BF16 or FLOWKV_FP16, the type of q, the pool and out.
+   dtype: as for flowkv_window_attention.
    max_new: the most new tokens of a request, max_group: of a group; both size the launch, and
    rows past them are computed all the same.  max_prefix: the longest prefix; max_own: the most
    tokens of a request behind its prefix, or in all where it is in no group.  Where a prefix or
@@ -601,8 +602,8 @@ int flowkv_window_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q
    read).  max_prefix + max_own is at most 2^31 - 4097.
    split_tokens: cached tokens per workgroup at most, a multiple of 64 (over 2,048: of a prefix,
    in tiles of 128 rows); 0 takes the library's rule, which may also find that requests are done
-   sooner each by itself.  Up to three launches on hip_stream.  The rest is as for flowkv_chunk_attention.  EINVAL for bad shapes or
-   pointers, ECAP for a short workspace. */
+   sooner each by itself.  Up to three launches on hip_stream.  The rest is as for
+   flowkv_chunk_attention.  EINVAL for bad shapes or pointers, ECAP for a short workspace. */
 int flowkv_prefix_attention(const flowkv_pool* pool, int32_t layer, int32_t dtype,
                             const void* q_dev, int64_t q_stride, int32_t n_tokens, int32_t n_req,
                             int32_t q_heads, int32_t kv_heads, int32_t head_dim,

@@ -92,7 +92,7 @@ struct ChunkArgs {
   const int32_t* offsets;               // (n_req + 1)
   const int32_t* seq_lens;              // (n_req)
   const int32_t* tables;                // (n_req, max_blocks)
-  uint16_t* out;                        // (n_tokens, Hq, Dh) bf16
+  uint16_t* out;                        // (n_tokens, Hq, Dh), of q's type
   float* ws;                            // the splits' records
   uint32_t bunits, sunits;              // 128-byte units between blocks, slots
   uint32_t bs_magic, bs_shift;          // division by block_size,
@@ -168,7 +168,7 @@ struct Shared {
 
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// The requests of group g are groups_at(g) .. groups_at(g + 1), within the batch's whatever
+// The requests of group g are group_at(g) .. group_at(g + 1) - 1, within the batch's whatever
 // the caller's array holds.
 __device__ __forceinline__ int32_t group_at(const SpanArgs& a, int32_t g) {
   const int32_t r = a.groups[g];
@@ -187,46 +187,6 @@ __device__ __forceinline__ int64_t first_tile(const ChunkArgs& a, int32_t r) {
 // The token of a unit's row x (0 <= x < 2^31).
 __device__ __forceinline__ int32_t token_of(const ChunkArgs& a, int32_t x) {
   return int32_t((__umulhi(uint32_t(x), a.g_magic) + uint32_t(x)) >> a.g_shift);
-}
-
-// Item `want` of the tiles of all groups, each tile in splits of its group's prefix: which group,
-// which of its items (-1: there are fewer).  The lanes count 64 groups at a time, so that the
-// workgroups with something to do are the first of a launch, next to each other.  (Empty ones in
-// turn with them go to the same shader engines each time and leave those idle: one group of 128
-// rows in 26 splits took 37 us with a slot without rows beside each, 23 without.)
-struct Item {
-  int32_t unit;
-  int64_t at;
-};
-__device__ __forceinline__ int32_t group_at(const SpanArgs& a, int32_t g);
-__device__ __forceinline__ int32_t prefix_of(const SpanArgs& a, int32_t g);
-__device__ __forceinline__ Item find_item(const SpanArgs& a, int64_t want) {
-  const int ln = threadIdx.x & 63;
-  int64_t before = 0;
-  for (int32_t g0 = 0; g0 < a.n_groups; g0 += 64) {
-    const int32_t g = g0 + ln;
-    int64_t count = 0;
-    if (g < a.n_groups) {
-      const int64_t rows =
-          (int64_t(a.offsets[group_at(a, g + 1)]) - a.offsets[group_at(a, g)]) * a.group;
-      const int64_t tiles = rows > 0 ? (rows + (int64_t(1) << a.row_shift) - 1) >> a.row_shift : 0;
-      count = tiles * splits_of(prefix_of(a, g), a.prefix_split);
-    }
-    int64_t sum = count;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-      const int64_t y = __shfl_up(sum, off);
-      if (ln >= off) sum += y;
-    }
-    const uint64_t hit = __ballot(want < before + sum);
-    if (hit) {
-      const int l = __builtin_ctzll(hit);
-      const int64_t first = __shfl(sum - count, l);
-      return Item{g0 + l, want - before - first};
-    }
-    before += __shfl(sum, 63);
-  }
-  return Item{0, -1};
 }
 
 struct Request {
@@ -261,6 +221,44 @@ __device__ __forceinline__ int32_t prefix_before(const SpanArgs& a, int32_t r) {
   const int32_t g =
       flowkv::last_at_most(a.n_groups, r, [&](int32_t i) { return group_at(a, i); });
   return group_at(a, g) <= r && r < group_at(a, g + 1) ? prefix_of(a, g) : 0;
+}
+
+// Item `want` of the tiles of all groups, each tile in splits of its group's prefix: which group,
+// which of its items (-1: there are fewer).  The lanes count 64 groups at a time, so that the
+// workgroups with something to do are the first of a launch, next to each other.  (Empty ones in
+// turn with them go to the same shader engines each time and leave those idle: one group of 128
+// rows in 26 splits took 37 us with a slot without rows beside each, 23 without.)
+struct Item {
+  int32_t unit;
+  int64_t at;
+};
+__device__ __forceinline__ Item find_item(const SpanArgs& a, int64_t want) {
+  const int ln = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int32_t g0 = 0; g0 < a.n_groups; g0 += 64) {
+    const int32_t g = g0 + ln;
+    int64_t count = 0;
+    if (g < a.n_groups) {
+      const int64_t rows =
+          (int64_t(a.offsets[group_at(a, g + 1)]) - a.offsets[group_at(a, g)]) * a.group;
+      const int64_t tiles = rows > 0 ? (rows + (int64_t(1) << a.row_shift) - 1) >> a.row_shift : 0;
+      count = tiles * splits_of(prefix_of(a, g), a.prefix_split);
+    }
+    int64_t sum = count;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      const int64_t y = __shfl_up(sum, off);
+      if (ln >= off) sum += y;
+    }
+    const uint64_t hit = __ballot(want < before + sum);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      const int64_t first = __shfl(sum - count, l);
+      return Item{g0 + l, want - before - first};
+    }
+    before += __shfl(sum, 63);
+  }
+  return Item{0, -1};
 }
 
 // A group as a unit of rows: r is its first request, whose block list is read, and base the one
