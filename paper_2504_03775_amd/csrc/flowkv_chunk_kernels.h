@@ -228,51 +228,55 @@ __device__ __forceinline__ int32_t prefix_before(const SpanArgs& a, int32_t r) {
 // workgroups with something to do are the first of a launch, next to each other.  (Empty ones in
 // turn with them go to the same shader engines each time and leave those idle: one group of 128
 // rows in 26 splits took 37 us with a slot without rows beside each, 23 without.)
+// The group is a unit of rows: r is its first request, whose block list is read, base the one
+// behind its last, and limit its prefix.  (All of it from the lane that has counted it: read
+// again by the scalar unit it cost another chain of loads.)
 struct Item {
-  int32_t unit;
-  int64_t at;
+  Request unit;
+  int32_t at;
 };
-__device__ __forceinline__ Item find_item(const SpanArgs& a, int64_t want) {
+__device__ __forceinline__ Item find_item(const SpanArgs& a, uint32_t want) {
+  constexpr int32_t kMany = 1 << 24;             // (more than a launch has workgroups: `want`
+                                                 // is below, and 64 of them are below 2^31)
   const int ln = threadIdx.x & 63;
   int64_t before = 0;
   for (int32_t g0 = 0; g0 < a.n_groups; g0 += 64) {
     const int32_t g = g0 + ln;
-    int64_t count = 0;
+    int32_t count = 0, r = 0, base = 0, begin = 0, end = 0, limit = 0;
     if (g < a.n_groups) {
-      const int64_t rows =
-          (int64_t(a.offsets[group_at(a, g + 1)]) - a.offsets[group_at(a, g)]) * a.group;
+      r = group_at(a, g);
+      base = group_at(a, g + 1);
+      limit = prefix_of(a, g);
+      begin = a.offsets[r];
+      end = a.offsets[base];
+      const int64_t rows = (int64_t(end) - begin) * a.group;
       const int64_t tiles = rows > 0 ? (rows + (int64_t(1) << a.row_shift) - 1) >> a.row_shift : 0;
-      count = tiles * splits_of(prefix_of(a, g), a.prefix_split);
+      const int64_t items =
+          std::min<int64_t>(tiles, kMany) * splits_of(limit, a.prefix_split);
+      count = items < kMany ? int32_t(items) : kMany;
     }
-    int64_t sum = count;
-#pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-      const int64_t y = __shfl_up(sum, off);
+    int32_t sum = count;
+    for (int off = 1; off < 64 && off < a.n_groups - g0; off *= 2) {
+      const int32_t y = __shfl_up(sum, off);
       if (ln >= off) sum += y;
     }
     const uint64_t hit = __ballot(want < before + sum);
     if (hit) {
       const int l = __builtin_ctzll(hit);
-      const int64_t first = __shfl(sum - count, l);
-      return Item{g0 + l, want - before - first};
+      auto of = [&](int32_t x) { return __builtin_amdgcn_readlane(x, l); };
+      Request q;
+      q.r = of(r);
+      q.base = of(base);
+      q.begin = of(begin);
+      q.limit = of(limit);
+      const int64_t n = int64_t(of(end)) - q.begin;
+      q.n_new = q.r < q.base && q.begin >= 0 && n > 0 && q.begin + n <= a.n_tokens && q.limit > 0
+                    ? int32_t(n) : 0;
+      return Item{q, int32_t(want - before - of(sum - count))};
     }
-    before += __shfl(sum, 63);
+    before += __builtin_amdgcn_readlane(sum, 63);
   }
-  return Item{0, -1};
-}
-
-// A group as a unit of rows: r is its first request, whose block list is read, and base the one
-// behind its last.
-__device__ __forceinline__ Request group_unit(const SpanArgs& a, int32_t g) {
-  Request q;
-  q.r = group_at(a, g);
-  q.base = group_at(a, g + 1);
-  q.begin = a.offsets[q.r];
-  const int64_t n = int64_t(a.offsets[q.base]) - q.begin;
-  q.limit = prefix_of(a, g);
-  q.n_new = q.r < q.base && q.begin >= 0 && n > 0 && q.begin + n <= a.n_tokens && q.limit > 0
-                ? int32_t(n) : 0;
-  return q;
+  return Item{Request{}, -1};
 }
 
 // Item `at` of a group's: 8 splits of all tiles, tile by tile, then the next 8.  So the tiles of
@@ -293,27 +297,34 @@ __device__ __forceinline__ void place_item(const SpanArgs& a, const Request& q, 
   *split = int(8 * block + (rest - uint32_t(*tile) * wide));
 }
 
-// What new token i of a group sees of the prefix: all of it, unless the token lies in it.
-__device__ __forceinline__ int32_t seen_of_prefix(const SpanArgs& a, const Request& q, int32_t i) {
+// What new token i of a group sees of the prefix: all of it, unless the token lies in it.  Its
+// request is first looked for where it would be if all had as many.
+struct Guess {
+  int32_t r, from, to, len;              // of that request: first tokens, its own and the next's
+};
+__device__ __forceinline__ Guess guess_at(const SpanArgs& a, int32_t r) {
+  return Guess{r, a.offsets[r], a.offsets[r + 1], a.seq_lens[r]};
+}
+__device__ __forceinline__ int32_t likely(const Request& q, int32_t i) {
+  return std::min(q.r + int32_t(float(i) * float(q.base - q.r) / float(q.n_new)), q.base - 1);
+}
+__device__ __forceinline__ int32_t seen_of_prefix(const SpanArgs& a, const Request& q, int32_t i,
+                                                  Guess x) {
   const int32_t token = q.begin + i;
-  // its request: where it would be if all had as many, or between
-  int32_t r = q.r, hi = q.base;
-  const int32_t guess =
-      std::min(r + int32_t(float(i) * float(hi - r) / float(q.n_new)), hi - 1);
-  const int32_t from = a.offsets[guess], to = a.offsets[guess + 1];
-  if (from > token) {
-    hi = guess;
-  } else {
-    r = to > token ? guess : std::min(guess + 1, hi - 1);
-    if (to > token) hi = guess + 1;
+  if (x.from > token || x.to <= token) {
+    int32_t r = q.r, hi = q.base;
+    if (x.from > token) hi = x.r;
+    else r = std::min(x.r + 1, hi - 1);
+    while (hi - r > 1) {
+      const int32_t mid = r + (hi - r) / 2;
+      if (a.offsets[mid] <= token) r = mid;
+      else hi = mid;
+    }
+    x = guess_at(a, r);
   }
-  while (hi - r > 1) {
-    const int32_t mid = r + (hi - r) / 2;
-    if (a.offsets[mid] <= token) r = mid;
-    else hi = mid;
-  }
-  const Request one = request_at(a, r);
-  const int32_t n = one.base + (token - one.begin) + 1;
+  const int64_t count = int64_t(x.to) - x.from;
+  const int32_t n_new = x.from >= 0 && count > 0 && x.from + count <= a.n_tokens ? int32_t(count) : 0;
+  const int32_t n = (x.len > 0 ? x.len : 0) - n_new + (token - x.from) + 1;
   return n < 0 ? 0 : n < q.limit ? n : q.limit;
 }
 
@@ -371,7 +382,7 @@ struct Reach {
 template <class P>
 __device__ __forceinline__ int32_t end_of(const typename P::Args& a, const Request& rq,
                                           const Reach<P>& reach, int32_t i) {
-  if constexpr (P::kPrefix) return seen_of_prefix(a, rq, i);
+  if constexpr (P::kPrefix) return seen_of_prefix(a, rq, i, guess_at(a, likely(rq, i)));
   else return reach.below(seen(rq, i));
 }
 
@@ -954,8 +965,8 @@ __device__ __forceinline__ void attend_many(const typename P::Args& a) {
     if constexpr (P::kPrefix) {
       const Item item = find_item(a, rest);
       if (item.at < 0) return;
-      rq = group_unit(a, uniform(item.unit));
-      place_item(a, rq, uniform(int32_t(item.at)), &local, &split);
+      rq = item.unit;
+      place_item(a, rq, item.at, &local, &split);
     } else {
       split = int(rest / uint32_t(a.tiles));
       const int slot = a.tiles - 1 - int(rest % uint32_t(a.tiles));  // the longest first
@@ -1421,8 +1432,8 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
       const Item item = find_item(a, rest);
       if (item.at < 0) return;
       length = a.prefix_split;
-      rq = group_unit(a, uniform(item.unit));
-      place_item(a, rq, uniform(int32_t(item.at)), &local, &split);
+      rq = item.unit;
+      place_item(a, rq, item.at, &local, &split);
     }
   } else {
     uint32_t at = rest;
@@ -1451,63 +1462,21 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
   const int n_tiles = (s1 - s0 + kFewTile - 1) / kFewTile;
 
   __shared__ FewLds<kDh, kC> lds;
-  int32_t lim[kC], low[kC];
-  Vec qb[kC][kI];
-#pragma unroll
-  for (int c = 0; c < kC; ++c) {
-    const int32_t row = row0 + 16 * c + c16;
-    const bool live = row < rows;
-    const int32_t qi = live ? token_of(a, row) : 0;
-    const int32_t qh = live ? row - qi * a.group : 0;
-    if constexpr (P::kShared)
-      lim[c] = !live ? 0 : of_prefix ? seen_of_prefix(a, rq, qi) : end_of<P>(a, rq, reach, qi);
-    else
-      lim[c] = live ? end_of<P>(a, rq, reach, qi) : 0;
-    if (tid < 16) lds.lim[16 * c + tid] = lim[c];
-    if constexpr (P::kWindow) {
-      low[c] = reach.low(rq, qi);
-      if (tid < 16) lds.low[16 * c + tid] = low[c];
-    }
-    if (of_prefix) {
-      int32_t least = live ? lim[c] : rq.limit;
-#pragma unroll
-      for (int off = 1; off < 16; off *= 2) least = std::min(least, __shfl_xor(least, off));
-      tile_least = std::min(tile_least, uniform(least));
-    }
-#pragma unroll
-    for (int i = 0; i < kI; ++i) {
-      u32x4 x = {0, 0, 0, 0};
-      if (live)
-        x = *(cgvec4*)(a.q + (int64_t(rq.begin) + qi) * a.q_stride +
-                       (g * a.group + qh) * int64_t(kDh) + 32 * i + 8 * q4);
-      qb[c][i] = __builtin_bit_cast(Vec, x);
-    }
-  }
   const int32_t* table = a.tables + int64_t(rq.r) * a.max_blocks;
-  for (int x = tid; x < n_tiles * kFewTile; x += kFewThreads) {
+  auto entry_of = [&](int x, uint32_t* within) {
     const uint32_t t = reach.token(uint32_t(s0 + x));
     const uint32_t b = uint32_t((uint64_t(__umulhi(t, a.bs_magic)) + t) >> a.bs_shift);
-    const bool in = s0 + x < s1;
-    const int32_t blk = table[in ? b : 0];       // (s1 lies within the block list)
-    const bool good = in && blk >= 0 && blk < a.pool_blocks;
+    *within = t - b * uint32_t(a.block_size);
+    return s0 + x < s1 ? int32_t(b) : 0;         // (s1 lies within the block list)
+  };
+  auto place = [&](int x, int32_t blk, uint32_t within) {
+    const bool good = s0 + x < s1 && blk >= 0 && blk < a.pool_blocks;
     const uint64_t dead = __ballot(!good);
     lds.at[(x & -kFewTile) + (x & 3) * 8 + (x >> 2 & 7)] =
-        good ? uint32_t(blk) * a.bunits + (t - b * uint32_t(a.block_size)) * a.sunits : 0;
+        good ? uint32_t(blk) * a.bunits + within * a.sunits : 0;
     if (ln % kFewTile == 0) lds.dead[x / kFewTile] = uint32_t(dead >> ln);
-  }
+  };
   u32x4* const s_k = reinterpret_cast<u32x4*>(lds.area + wave * (kFewTile * kDh * 2));
-  f32x4 o[kC][kT];
-  float mref[kC], lsum[kC];                      // of the column's row; this lane's tokens
-#pragma unroll
-  for (int c = 0; c < kC; ++c) {
-    mref[c] = -INFINITY;
-    lsum[c] = 0.f;
-#pragma unroll
-    for (int t = 0; t < kT; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-  if (tid < 2) lds.odd[tid] = 0;
-  __syncthreads();
-
   u32x4 kw[kKL];
   VT vw[8];
   constexpr int kStride = 64 / kPc;              // tokens of one K load
@@ -1536,10 +1505,91 @@ __device__ __forceinline__ void attend_few(const typename P::Args& a) {
       else vw[e] = __builtin_nontemporal_load(at);
     }
   };
+  int32_t lim[kC], low[kC], qi[kC];
+  bool live[kC];
+  Vec qb[kC][kI];
+#pragma unroll
+  for (int c = 0; c < kC; ++c) {
+    const int32_t row = row0 + 16 * c + c16;
+    live[c] = row < rows;
+    qi[c] = live[c] ? token_of(a, row) : 0;
+  }
+  auto load_q = [&](int c) {
+    const int32_t qh = live[c] ? row0 + 16 * c + c16 - qi[c] * a.group : 0;
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+      u32x4 x = {0, 0, 0, 0};
+      // (kShared: a lane without a row has the first one's, which its column keeps to itself)
+      if (P::kShared || live[c])
+        x = *(cgvec4*)(a.q + (int64_t(rq.begin) + qi[c]) * a.q_stride +
+                       (g * a.group + qh) * int64_t(kDh) + 32 * i + 8 * q4);
+      qb[c][i] = __builtin_bit_cast(Vec, x);
+    }
+  };
+  auto limit = [&](int c, int32_t l) {
+    lim[c] = live[c] ? l : 0;
+    if (tid < 16) lds.lim[16 * c + tid] = lim[c];
+    if constexpr (P::kWindow) {
+      low[c] = reach.low(rq, qi[c]);
+      if (tid < 16) lds.low[16 * c + tid] = low[c];
+    }
+  };
+  if (tid < 2) lds.odd[tid] = 0;
+  if constexpr (P::kShared) {
+    // One link of loads before K and V: the block list, the rows' requests and the queries are
+    // under way together, so without branches between them.
+    constexpr int kPlaces = kFewSplit / kFewThreads;
+    int32_t blk[kPlaces];
+    uint32_t within[kPlaces];
+    const int32_t* const from = n_tiles > 0 ? table : a.offsets;   // (no list where none is seen)
+#pragma unroll
+    for (int e = 0; e < kPlaces; ++e) blk[e] = from[entry_of(tid + e * kFewThreads, &within[e])];
+    Guess one[kC];
+#pragma unroll
+    for (int c = 0; c < kC; ++c) one[c] = guess_at(a, of_prefix ? likely(rq, qi[c]) : rq.r);
+#pragma unroll
+    for (int c = 0; c < kC; ++c) load_q(c);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int e = 0; e < kPlaces; ++e) place(tid + e * kFewThreads, blk[e], within[e]);
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      limit(c, of_prefix ? seen_of_prefix(a, rq, qi[c], one[c]) : end_of<P>(a, rq, reach, qi[c]));
+      if (of_prefix) {
+        int32_t least = live[c] ? lim[c] : rq.limit;
+#pragma unroll
+        for (int off = 1; off < 16; off *= 2) least = std::min(least, __shfl_xor(least, off));
+        tile_least = std::min(tile_least, uniform(least));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      limit(c, end_of<P>(a, rq, reach, qi[c]));
+      load_q(c);
+    }
+    for (int x = tid; x < n_tiles * kFewTile; x += kFewThreads) {
+      uint32_t within;
+      const int32_t blk = table[entry_of(x, &within)];
+      place(x, blk, within);
+    }
+    __syncthreads();
+  }
   if (wave < n_tiles) {
     load_k(wave);
     load_v(wave);
   }
+  f32x4 o[kC][kT];
+  float mref[kC], lsum[kC];                      // of the column's row; this lane's tokens
+#pragma unroll
+  for (int c = 0; c < kC; ++c) {
+    mref[c] = -INFINITY;
+    lsum[c] = 0.f;
+#pragma unroll
+    for (int t = 0; t < kT; ++t) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
   for (int tile = wave; tile < n_tiles; tile += kFewWaves) {
     // (past the wave's last tile: its own again, so that as many loads are under way)
     const int next = tile + kFewWaves < n_tiles ? tile + kFewWaves : tile;
