@@ -29,8 +29,9 @@ using namespace flowkv::chunk;
 
 // Few rows: both in one launch.  A tile of 16 or 32 rows of a group reads the prefix through its
 // XCD's L2, which brings some 14 TB/s of it (all XCDs together).  32 single tokens behind 13,000,
-// 32 heads of 128 on 8: 28 us, of them 7 until the first loads (the group, its requests, the block
-// list, one after the other) and 17 for 52 steps of 32 tokens; 5 more of join.  Behind 4,000 and
+// 32 heads of 128 on 8: 27 us, of them 2 to find the group, 3 to look up its block list and rows
+// and 18 for 52 steps of 32 tokens (1.4 us for each of a wave's 13: memory's latency, which the
+// four tiles of a split meet together), 2 for its records; 4 more of join.  Behind 4,000 and
 // 100 to 2,500 of their own, 64 of them: 88 us, memory's 60 and the last workgroups' end.
 template <int kDh, int kC, class T>
 __global__ __launch_bounds__(kFewThreads, few_per_cu(kDh, kC))
