@@ -601,8 +601,9 @@ int flowkv_window_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q
    a request has more, its rows are of no meaning (nothing outside the pool and the lists is
    read).  max_prefix + max_own is at most 2^31 - 4097.
    split_tokens: cached tokens per workgroup at most, a multiple of 64 (over 2,048: of a prefix,
-   in tiles of 128 rows); 0 takes the library's rule, which may also find that requests are done
-   sooner each by itself.  Up to three launches on hip_stream.  The rest is as for
+   in tiles of 128 rows; with no group or a max_prefix of 0 as for flowkv_chunk_attention); 0
+   takes the library's rule, which may also find that requests are done sooner each by itself.
+   Up to three launches on hip_stream.  The rest is as for
    flowkv_chunk_attention.  EINVAL for bad shapes or pointers, ECAP for a short workspace. */
 int flowkv_prefix_attention(const flowkv_pool* pool, int32_t layer, int32_t dtype,
                             const void* q_dev, int64_t q_stride, int32_t n_tokens, int32_t n_req,

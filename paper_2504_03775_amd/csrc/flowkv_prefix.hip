@@ -150,9 +150,11 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
   if (longest > INT32_MAX - 4096)
     return fail(FLOWKV_EINVAL, "%lld tokens of a prefix and behind it: need at most 2^31 - 4097",
                 (long long)longest);
-  // (its checks of the sizes hold for either way)
+  const bool groups = n_groups > 0 && max_prefix > 0;
+  // (its checks of the sizes hold for either way; with split_tokens and groups the plan is shared)
   const int rc = plan_shape(alone(FLOWKV_BF16), n_tokens, n_req, q_heads, kv_heads, head_dim,
-                            max_new, Span{int32_t(longest)}, 0, true, &out->sh);
+                            max_new, Span{int32_t(longest)}, groups ? 0 : split_tokens, true,
+                            &out->sh);
   if (rc) return rc;
   if (split_tokens < 0 || split_tokens % kSplitUnit)
     return fail(FLOWKV_EINVAL, "split_tokens %d: need 0 or a multiple of %d", split_tokens,
@@ -165,7 +167,7 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
   const int64_t tiles32 = tiles_of(n_tokens, n_groups, group, max_group, 32);
   // (in double: tiles of it pass 63 bits where max_prefix is set to the most there can be)
   const double prefix_bytes = double(max_prefix) * kv_heads * head_dim * 4;
-  out->shared = n_groups > 0 && max_prefix > 0 &&
+  out->shared = groups &&
                 (split_tokens > 0 ||
                  (one <= 64 && double(n_req * ((one + 31) / 32) - tiles32) * prefix_bytes >=
                                    double(kLeastSaved)));
