@@ -587,11 +587,11 @@ int flowkv_window_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q
                                       int32_t split_tokens, int64_t* bytes);
 
 /* flowkv_chunk_attention for requests that share long prefixes, each prefix read once for all
-   of a group.  Group g is the requests groups[g] .. groups[g + 1] - 1 (n_groups + 1
-   non-decreasing int32 in device memory, requests outside of all groups allowed), whose first
-   prefix_lens[g] tokens are the same: their block lists name the same K and V there (blocks
-   shared by flowkv_share, a part-filled last one copied as flowkv_fork has it).  The list of
-   the group's first request is the one read for the prefix.  Every row sees all tokens up to
+   of a group where that is sooner (split_tokens).  Group g is the requests groups[g] ..
+   groups[g + 1] - 1 (n_groups + 1 non-decreasing int32 in device memory, requests outside of all
+   groups allowed), whose first prefix_lens[g] tokens are the same: their block lists name the
+   same K and V there (blocks shared by flowkv_share, a part-filled last one copied as flowkv_fork
+   has it).  The list of the group's first request is the one read for the prefix.  Every row sees all tokens up to
    its own position, those of the prefix and those behind it: the result is that of
    flowkv_chunk_attention, joined in another order.
    dtype: as for flowkv_window_attention.
@@ -602,9 +602,10 @@ int flowkv_window_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q
    read).  max_prefix + max_own is at most 2^31 - 4097.
    split_tokens: cached tokens per workgroup at most, a multiple of 64 (over 2,048: of a prefix,
    in tiles of 128 rows; with no group or a max_prefix of 0 as for flowkv_chunk_attention); 0
-   takes the library's rule, which may also find that requests are done sooner each by itself.
-   Up to three launches on hip_stream.  The rest is as for
-   flowkv_chunk_attention.  EINVAL for bad shapes or pointers, ECAP for a short workspace. */
+   takes the library's rule, by which all of a call's requests are done each by itself where they
+   bring more than 64 rows on average, a row being a (new token, query head of a KV head), or
+   sharing saves under some 24 MiB of reads.  Up to three launches on hip_stream.  The rest is as
+   for flowkv_chunk_attention.  EINVAL for bad shapes or pointers, ECAP for a short workspace. */
 int flowkv_prefix_attention(const flowkv_pool* pool, int32_t layer, int32_t dtype,
                             const void* q_dev, int64_t q_stride, int32_t n_tokens, int32_t n_req,
                             int32_t q_heads, int32_t kv_heads, int32_t head_dim,

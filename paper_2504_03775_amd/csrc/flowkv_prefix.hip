@@ -119,11 +119,22 @@ const Parts& parts(int32_t dtype) {
 }
 
 // Bytes of prefixes that tiles of 32 rows of a group read less than its requests would, each by
-// itself, from which on the join's launch is worth it.  (8 KV heads of 128: 2 requests behind
-// 8,000 tokens, 33 MB saved, 13.3 us shared and 12.8 by themselves; 16 behind 500, 29 MB, 12.7
-// and 13.6; 4 behind 8,000, 98 MB, 14.4 and 23.3; one KV head: 16 behind 2,000, 12 MB, 12.4 and
-// 10.9; 48, 37 MB, 13.5 and 14.2.)
+// itself, from which on the join's launch is worth it.  (In a graph, us shared and each by itself.
+// 8 KV heads of 128: 2 requests behind 5,000 tokens, 20 MiB saved, 12.7 and 12.7; behind 8,000,
+// 31 MiB, 14.4 and 15.9; 16 behind 500, 29 MiB, 13.7 and 12.5; behind 1,000, 59 MiB, 14.3 and
+// 15.4; 4 behind 8,000, 94 MiB, 14.7 and 29.3; one KV head: 16 behind 2,000, 15 MiB, 14.0 and
+// 11.4; 48 behind 1,500, 34 MiB, 14.3 and 14.1.  So up to some 50 MiB the one or the other may be
+// sooner, by 3 us at most: few long reads gain early, many short ones late.  Requests of no group
+// count as if they shared: the host does not know them.)
 constexpr int64_t kLeastSaved = int64_t(24) << 20;
+// Rows a request, on average, up to which it is: the tiles of all of them are then few beside
+// those of the requests, however long one of them is.  (us, each by itself and shared.  8 KV
+// heads of 128, groups of 4, behind 4,000: 63 single tokens beside one request of 17, 5 rows a
+// request, 169 and 36; beside one of 512, 36 rows, 221 and 113; beside one of 2,048, 132 rows, 351
+// and 381; 64 requests of 16, 64 rows, behind 8,000, 335 and 207; of 32, 128 rows, 359 and 390.
+// 15 beside one of 512, 132 rows, 90 and 101.  The 63 beside 512 behind 1,000: 80 and 67; behind
+// 500: 55 and 60.)
+constexpr int64_t kMostRows = 64;
 // Bytes that they read, through their L2s, from which on tiles of 128 rows in a launch of their
 // own are sooner done: they are bound by the matrix units, at less than half of the time.  (64
 // requests behind 13,000 tokens, 426 MB: 45.0 and 44.7 us; 128: 81 and 65; 250: 152 and 108; 250
@@ -160,17 +171,19 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
     return fail(FLOWKV_EINVAL, "split_tokens %d: need 0 or a multiple of %d", split_tokens,
                 kSplitUnit);
   const int group = q_heads / kv_heads;
-  const int64_t one = int64_t(max_new) * group;  // rows of a request
+  const int64_t one = int64_t(max_new) * group;  // rows of a request, at most
   auto tiles_at = [&](int64_t units, int64_t most_new, int rows) {
     return std::max<int64_t>(tiles_of(n_tokens, units, group, most_new, rows) * kv_heads, 1);
   };
+  const int64_t most_new = std::min(int64_t(n_tokens), int64_t(n_req) * max_new);   // no padding
   const int64_t tiles32 = tiles_of(n_tokens, n_groups, group, max_group, 32);
+  const int64_t alone32 = tiles_of(n_tokens, n_req, group, max_new, 32);
   // (in double: tiles of it pass 63 bits where max_prefix is set to the most there can be)
   const double prefix_bytes = double(max_prefix) * kv_heads * head_dim * 4;
   out->shared = groups &&
                 (split_tokens > 0 ||
-                 (one <= 64 && double(n_req * ((one + 31) / 32) - tiles32) * prefix_bytes >=
-                                   double(kLeastSaved)));
+                 (most_new * group <= kMostRows * n_req &&
+                  double(alone32 - tiles32) * prefix_bytes >= double(kLeastSaved)));
   // Tiles of 32 rows halve what a prefix is read, with two workgroups a CU instead of three.
   const bool many = split_tokens > kFewSplit ||
                     (split_tokens == 0 && double(tiles32) * prefix_bytes >= double(kMostRead));

@@ -18,3 +18,31 @@ def test_split_tokens_holds_where_there_is_nothing_to_share():
                 full(n, 4, 8, 2, 128, new, 5000, split)
     # no group: a prefix's tokens are as many more of the requests' own
     assert ws(4, 4, 8, 2, 128, 0, 1, 4, 200, 400, 64) == 4 * 8 * 10 * record
+
+
+def records(n_tokens, *rest):
+    """Records a row of a shared call, by the workspace; None: not one of a whole number of them
+    (work by the lengths: pieces), 0: none."""
+    bytes_ = ws(n_tokens, *rest)
+    row = n_tokens * rest[1] * (rest[3] + 2) * 4
+    return bytes_ // row if bytes_ % row == 0 else None
+
+
+def test_a_long_request_does_not_end_sharing_for_the_others():
+    """63 single tokens beside one request of more, behind one prefix (32 heads of 128 on 8, 8
+    of 128 on 1, 8 of 64 on 4): records of a prefix's splits and of the tokens behind it."""
+    for hq, hk, d in ((32, 8, 128), (8, 1, 128), (8, 4, 64)):
+        for prefix in (4000, 13000):
+            for new in (1, 16, 17, 64, 100, 300):
+                n = 63 + new
+                assert (records(n, 64, hq, hk, d, 1, new, n, 400, prefix) or 0) >= 2, (hq, new)
+    # where the requests bring many rows on average, whole tiles read a prefix once for many
+    for n, req, new in ((16 * 300, 16, 300), (16 * 64, 16, 64), (15 + 2000, 16, 2000)):
+        assert ws(n, req, 32, 8, 128, 1, new, n, 400, 4000) == \
+            ws(n, req, 32, 8, 128, 0, new, n, 400, 4000), (n, req)
+    # little saved: one prefix for one request, and for two requests of short ones
+    for n, req, prefix in ((100, 1, 9000), (2, 2, 300)):
+        assert ws(n, req, 32, 8, 128, 1, n // req, n, 400, prefix) == \
+            ws(n, req, 32, 8, 128, 0, n // req, n, 400, prefix)
+    # padding rows are nobody's: single tokens in a batch of 8,192 rows, as a captured call has them
+    assert records(8192, 64, 32, 8, 128, 1, 1, 64, 400, 4000) >= 2
