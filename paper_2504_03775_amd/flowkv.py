@@ -858,9 +858,9 @@ def flowkv_append_rotated(pool: KVPool, layer: int, k, v, cos_sin, q_offsets, bl
         raise ValueError(f"cos_sin: need contiguous (positions, rot_dim) float32 on {pool.device}, "
                          f"got {tuple(angles)} {cos_sin.dtype} on {cos_sin.device}")
     hq = qs = os_ = q_at = out_at = 0
+    if (q is None) != (q_out is None):
+        raise ValueError("q without q_out" if q_out is None else "q_out without q")
     if q is not None:
-        if q_out is None:
-            raise ValueError("q without q_out")
         hq = q.shape[1] if q.dim() == 3 else 0
         qs = _token_stride(q, q.shape, "q", hq, d, dtype, pool)
         os_ = _token_stride(q_out, q_out.shape, "q_out", hq, d, dtype, pool)
