@@ -80,10 +80,12 @@ inline int64_t tile_slots(int64_t n_tokens, int64_t n_req, int group, int rows) 
   return n_tokens * group / rows + n_req;
 }
 
-// Tiles of `rows` rows that the batch has at most.
+// Tiles of `rows` rows that the batch has at most.  (Where a request could have as many as there
+// are slots, no product: it may pass 63 bits.)
 inline int64_t tiles_of(int64_t n_tokens, int64_t n_req, int group, int64_t max_new, int rows) {
-  return std::min(n_req * ((max_new * group + rows - 1) / rows),
-                  tile_slots(n_tokens, n_req, group, rows));
+  const int64_t slots = tile_slots(n_tokens, n_req, group, rows);
+  const int64_t each = (max_new * group + rows - 1) / rows;
+  return n_req == 0 ? 0 : each >= slots ? slots : std::min(n_req * each, slots);
 }
 
 // The same without padding: of no more than max_new tokens a request.
