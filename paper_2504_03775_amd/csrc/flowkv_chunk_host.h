@@ -42,8 +42,18 @@ struct Kernels {
   const void* merge[2][2];                       // head_dim; a wave or four a row
 };
 constexpr int kSplitUnit = 64;
-constexpr int kTailRounds = 4;             // most rounds of tiles that have a tail,
-constexpr int kTailSteps = 32;             // and the least steps
+// Whole tiles and a tail in pieces (cut_tiles): 32 steps at least, so that a round not begun is
+// worth the search and the join; up to four rounds, and of the last one up to half in use, by the
+// tiles to be expected (a request's last one half full); and tiles about as long as each other,
+// 3 tokens cached for 5 new ones: the short ones under a prompt's diagonal fill the last round by
+// themselves.  (us, whole tiles and with a tail, 32 heads of 128 on 8, new tokens behind cached
+// ones.  Gains: 2,304 behind 4,000, 1.12 rounds, 272 and 224; 4,416, 2.16, 531 and 462; 8 of 320
+// behind 2,200, 39 steps, 155 and 135; 24 of 125 behind 10,606, 1.5 rounds, 702 and 604.  Losses:
+// 8 of 320 behind 700, 16 steps, 76 and 81; 4,096 behind 4,000, 2.0 rounds, 398 and 409; 8 of 960
+// behind 1,700, 3.75, 316 and 336; through a window of 2,100 with nothing cached, 4,416, 155 and
+// 165, 4 of 1,100, 71 and 87.)
+constexpr int kTailRounds = 4;
+constexpr int kTailSteps = 32;
 constexpr int kFewSteps = 8;               // of 32 tokens, a CU
 
 // x / d = (umulhi(x, m) + x) >> l with l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1.
@@ -228,11 +238,21 @@ inline int plan_shape(const Kernels& kernels, int32_t n_tokens, int32_t n_req, i
     out->kind = 2;
   }
   const Kind& kind = kKinds[out->kind];
+  // (the workspace of a tail is asked for wherever there might be one)
+  int64_t asked = 0;
   if (tail && rule && out->kind == cut_kind && head_dim == 128 && takes_lengths(cut_kind)) {
     const int64_t round = int64_t(kind.per_cu[1]) * kCus;
     if (t256 > round && t256 <= kTailRounds * round &&
-        length(cut_kind) >= int64_t(kTailSteps) * kind.step)
-      return by_pieces(cut_kind, true);
+        length(cut_kind) >= int64_t(kTailSteps) * kind.step) {
+      by_pieces(cut_kind, true);
+      const int64_t rows = std::min(int64_t(n_tokens), int64_t(n_req) * max_new) * group;
+      const int64_t half_full = (rows + (int64_t(n_req) + 2) * kind.rows / 2 - 1) / kind.rows;
+      const int64_t last = std::min(t256, half_full * kv_heads) % round;
+      const int64_t cached = span.max_seq_len - std::min(max_new, span.max_seq_len);
+      if (last > 0 && 2 * last <= round && 5 * cached >= 3 * int64_t(max_new)) return FLOWKV_OK;
+      out->tail = false;
+      asked = out->need;
+    }
   }
   if (rule && out->kind >= 2 && n_req > 1 && span.max_seq_len / 2 >= max_new &&
       (out->kind == 3 ? t256 : t128) > kCus && takes_lengths(out->kind)) {
@@ -240,7 +260,7 @@ inline int plan_shape(const Kernels& kernels, int32_t n_tokens, int32_t n_req, i
     out->split = 0;
     out->splits = 1;
     out->pieces = 0;
-    out->need = 0;
+    out->need = asked;
     return FLOWKV_OK;
   }
   if (rule) {
@@ -257,7 +277,7 @@ inline int plan_shape(const Kernels& kernels, int32_t n_tokens, int32_t n_req, i
   }
   out->split = split_tokens;
   const int64_t splits = splits_of(out->kind, split_tokens);
-  out->need = bytes_of(out->kind, split_tokens);
+  out->need = std::max(bytes_of(out->kind, split_tokens), asked);
   out->splits = int32_t(splits);
   out->pieces = 0;
   if (out->need == INT64_MAX)

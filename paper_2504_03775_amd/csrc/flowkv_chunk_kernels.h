@@ -715,8 +715,8 @@ struct Source {
 //     (Prompts with nothing cached gain nothing: the diagonal orders each of them.)
 // A third kind, where tiles are long and a few rounds of the CUs (kTail): as many whole tiles as
 // fill rounds, the longest first, and the rest of them in pieces, one round more.  (16 prompts of
-// 50 to 700 tokens behind 3,000 and 5,000, 20 heads of 128 on 4, 533 tiles on 256 CUs: 446 us in
-// whole tiles, three rounds.)
+// 50 to 700 tokens behind 3,000 and 5,000, 20 heads of 128 on 4, 560 tiles on 256 CUs: 403 us, in
+// whole tiles, three rounds, 465 on the same card.)
 constexpr int kPieceTiles = 512;           // most tile slots, and requests, of such a call
 constexpr int kPieceLeast = 2;             // steps
 constexpr int kCutSteps = 16;              // steps a CU, were all tiles the longest, from which on
