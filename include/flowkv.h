@@ -603,8 +603,8 @@ int flowkv_window_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q
    split_tokens: cached tokens per workgroup at most, a multiple of 64 (over 2,048: of a prefix,
    in tiles of 128 rows; with no group or a max_prefix of 0 as for flowkv_chunk_attention); 0
    takes the library's rule, by which all of a call's requests are done each by itself where they
-   bring more than 64 rows on average, a row being a (new token, query head of a KV head), or
-   sharing saves under some 24 MiB of reads.  Up to three launches on hip_stream.  The rest is as
+   bring more than 64 rows on average (112 where the longest brings four times as many), a row
+   being a (new token, query head of a KV head), or sharing saves under some 24 MiB of reads.  Up to three launches on hip_stream.  The rest is as
    for flowkv_chunk_attention.  EINVAL for bad shapes or pointers, ECAP for a short workspace. */
 int flowkv_prefix_attention(const flowkv_pool* pool, int32_t layer, int32_t dtype,
                             const void* q_dev, int64_t q_stride, int32_t n_tokens, int32_t n_req,

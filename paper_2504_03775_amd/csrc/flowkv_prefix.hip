@@ -28,11 +28,12 @@ using namespace flowkv::chunk;
 // ---- over a group's prefix, over what is behind it, and their join ----------------------
 
 // Few rows: both in one launch.  A tile of 16 or 32 rows of a group reads the prefix through its
-// XCD's L2, which brings some 14 TB/s of it (all XCDs together).  32 single tokens behind 13,000,
-// 32 heads of 128 on 8: 27 us, of them 2 to find the group, 3 to look up its block list and rows
-// and 18 for 52 steps of 32 tokens (1.4 us for each of a wave's 13: memory's latency, which the
-// four tiles of a split meet together), 2 for its records; 4 more of join.  Behind 4,000 and
-// 100 to 2,500 of their own, 64 of them: 88 us, memory's 60 and the last workgroups' end.
+// XCD's L2, so what its CU draws bounds it, some 45 bytes a nanosecond.  32 single tokens behind
+// 13,000, 32 heads of 128 on 8: 27 us, of them 2 to find the group, 3 to look up its block list and
+// rows and 18 for 52 steps of 32 tokens (four tiles of 32 rows draw 213 MB between them, 46 bytes a
+// nanosecond and CU; 1.4 us for each of a wave's 13 steps), 2 for its records; 4 more of join.
+// Behind 4,000 and 100 to 2,500 of their own, 64 of them: 88 us, memory's 60 and the last
+// workgroups' end.
 template <int kDh, int kC, class T>
 __global__ __launch_bounds__(kFewThreads, few_per_cu(kDh, kC))
 void prefix_attn_few(const SpanArgs a) {
@@ -121,20 +122,22 @@ const Parts& parts(int32_t dtype) {
 // Bytes of prefixes that tiles of 32 rows of a group read less than its requests would, each by
 // itself, from which on the join's launch is worth it.  (In a graph, us shared and each by itself.
 // 8 KV heads of 128: 2 requests behind 5,000 tokens, 20 MiB saved, 12.7 and 12.7; behind 8,000,
-// 31 MiB, 14.4 and 15.9; 16 behind 500, 29 MiB, 13.7 and 12.5; behind 1,000, 59 MiB, 14.3 and
-// 15.4; 4 behind 8,000, 94 MiB, 14.7 and 29.3; one KV head: 16 behind 2,000, 15 MiB, 14.0 and
-// 11.4; 48 behind 1,500, 34 MiB, 14.3 and 14.1.  So up to some 50 MiB the one or the other may be
-// sooner, by 3 us at most: few long reads gain early, many short ones late.  Requests of no group
+// 31 MiB, 14.4 and 15.9; 16 behind 500, 27 MiB, 13.7 and 12.5; behind 1,000, 55 MiB, 14.3 and
+// 15.4; 4 behind 8,000, 94 MiB, 14.7 and 29.3; one KV head: 16 behind 2,000, 12 MiB, 14.0 and
+// 11.4; 48 behind 1,500, 26 MiB, 14.3 and 14.1.  So up to some 50 MiB the one or the other may be
+// sooner, by up to 4 us: few long reads gain early, many short ones late.  Requests of no group
 // count as if they shared: the host does not know them.)
 constexpr int64_t kLeastSaved = int64_t(24) << 20;
 // Rows a request, on average, up to which it is: the tiles of all of them are then few beside
-// those of the requests, however long one of them is.  (us, each by itself and shared.  8 KV
-// heads of 128, groups of 4, behind 4,000: 63 single tokens beside one request of 17, 5 rows a
-// request, 169 and 36; beside one of 512, 36 rows, 221 and 113; beside one of 2,048, 132 rows, 351
-// and 381; 64 requests of 16, 64 rows, behind 8,000, 335 and 207; of 32, 128 rows, 359 and 390.
-// 15 beside one of 512, 132 rows, 90 and 101.  The 63 beside 512 behind 1,000: 80 and 67; behind
-// 500: 55 and 60.)
-constexpr int64_t kMostRows = 64;
+// those of the requests; and where the longest brings four times as many and more, so that most
+// bring few.  (us, each by itself and shared.  8 KV heads of 128, groups of 4, 64 requests of 16
+// tokens, 64 rows, behind 2,000, 111 and 102, behind 8,000, 335 and 207; of 17, 101 and 143, 310
+// and 277; of 32, 123 and 181, 359 and 390.  63 single tokens beside one of 17, 5 rows a request,
+// behind 4,000, 169 and 36; beside one of 512, 36 rows, 221 and 113, behind 1,000 80 and 67, behind
+// 500 55 and 60; beside one of 1,500, 98 rows, behind 2,000 183 and 192, behind 4,000 303 and 252;
+// beside one of 2,048, 132 rows, 351 and 381.  One KV head, groups of 8: the 63 beside one of 512,
+// 72 rows, 66 and 45, beside one of 850, 114 rows, 74 and 68.)
+constexpr int64_t kMostRows = 64, kMostRowsMixed = 112;
 // Bytes that they read, through their L2s, from which on tiles of 128 rows in a launch of their
 // own are sooner done: they are bound by the matrix units, at less than half of the time.  (64
 // requests behind 13,000 tokens, 426 MB: 45.0 and 44.7 us; 128: 81 and 65; 250: 152 and 108; 250
@@ -175,14 +178,16 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
   auto tiles_at = [&](int64_t units, int64_t most_new, int rows) {
     return std::max<int64_t>(tiles_of(n_tokens, units, group, most_new, rows) * kv_heads, 1);
   };
-  const int64_t most_new = std::min(int64_t(n_tokens), int64_t(n_req) * max_new);   // no padding
+  const int64_t rows =                           // of all requests, no padding; on average
+      std::min(int64_t(n_tokens), int64_t(n_req) * max_new) * group;
+  const int64_t each = rows / std::max(n_req, 1);
   const int64_t tiles32 = tiles_of(n_tokens, n_groups, group, max_group, 32);
   const int64_t alone32 = tiles_of(n_tokens, n_req, group, max_new, 32);
   // (in double: tiles of it pass 63 bits where max_prefix is set to the most there can be)
   const double prefix_bytes = double(max_prefix) * kv_heads * head_dim * 4;
   out->shared = groups &&
                 (split_tokens > 0 ||
-                 (most_new * group <= kMostRows * n_req &&
+                 (rows <= (one >= 4 * each ? kMostRowsMixed : kMostRows) * n_req &&
                   double(alone32 - tiles32) * prefix_bytes >= double(kLeastSaved)));
   // Tiles of 32 rows halve what a prefix is read, with two workgroups a CU instead of three.
   const bool many = split_tokens > kFewSplit ||

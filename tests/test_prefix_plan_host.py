@@ -33,11 +33,11 @@ def test_a_long_request_does_not_end_sharing_for_the_others():
     of 128 on 1, 8 of 64 on 4): records of a prefix's splits and of the tokens behind it."""
     for hq, hk, d in ((32, 8, 128), (8, 1, 128), (8, 4, 64)):
         for prefix in (4000, 13000):
-            for new in (1, 16, 17, 64, 100, 300):
+            for new in (1, 16, 17, 64, 100, 300, 512):
                 n = 63 + new
                 assert (records(n, 64, hq, hk, d, 1, new, n, 400, prefix) or 0) >= 2, (hq, new)
     # where the requests bring many rows on average, whole tiles read a prefix once for many
-    for n, req, new in ((16 * 300, 16, 300), (16 * 64, 16, 64), (15 + 2000, 16, 2000)):
+    for n, req, new in ((16 * 300, 16, 300), (64 * 17, 64, 17), (64 * 20, 64, 40), (15 + 2000, 16, 2000)):
         assert ws(n, req, 32, 8, 128, 1, new, n, 400, 4000) == \
             ws(n, req, 32, 8, 128, 0, new, n, 400, 4000), (n, req)
     # little saved: one prefix for one request, and for two requests of short ones
