@@ -227,7 +227,10 @@ __device__ __forceinline__ int32_t prefix_before(const SpanArgs& a, int32_t r) {
 // which of its items (-1: there are fewer).  The lanes count 64 groups at a time, so that the
 // workgroups with something to do are the first of a launch, next to each other.  (Empty ones in
 // turn with them go to the same shader engines each time and leave those idle: one group of 128
-// rows in 26 splits took 37 us with a slot without rows beside each, 23 without.)
+// rows in 26 splits took 37 us with a slot without rows beside each, 23 without.)  Past 64 groups
+// each 64 are one more chain of loads: with single tokens on one KV head of 128, 64 groups of 4
+// behind 1,000 take 22 us (each request by itself 35), 256 of 4 behind 500 49 (62), 512 of 2 59
+// (63), 1,024 of 2 behind 300 109 (76).
 // The group is a unit of rows: r is its first request, whose block list is read, base the one
 // behind its last, and limit its prefix.  (All of it from the lane that has counted it: read
 // again by the scalar unit it cost another chain of loads.)

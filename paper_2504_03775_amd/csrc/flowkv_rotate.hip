@@ -102,7 +102,8 @@ Divisor divisor(uint32_t d) {
 //
 // What bounds it: short calls, a launch and its chain of loads (offsets, length, angles; the rows'
 // own are under way meanwhile): 32 tokens of 48 heads of 128 3.3 us in a graph.  Long ones memory:
-// 17,679 tokens of 10 heads, 99.6 MB, 16.7 us, 5.9 TB/s.  (With divisions for the products, one
+// 17,679 tokens of 10 heads, 99.6 MB, 16.7 to 17.5 us by the card, 5.7 to 5.9 TB/s; in float32, 190
+// MB, 30.8 us, 6.2.  (With divisions for the products, one
 // head a lane and pairs of pieces next to each other 20.2.)
 constexpr int kThreads = 256;
 
@@ -236,8 +237,11 @@ __global__ __launch_bounds__(kThreads) void kv_rotate(const RotateArgs a) {
 }
 
 // Units up to which a lane takes one: they then are on the CUs at once.  And bytes written from
-// which on they go past the caches: 45 MB (17,679 tokens of 10 heads of 128) take 17.9 us past
-// them, 5.6 TB/s, and 20.8 through; 17 MB (8,484 tokens of 16 heads of 64) 11.9 and 10.5.
+// which on they go past the caches.  (us past them and through, in a graph: 10 heads of 128 in
+// blocks of 16, 10 MiB 5.5 and 6.2, 29 MiB 11.8 and 13.1, 146 MiB 54.6 and 59.8; 17,679 tokens of
+// them, 43 MiB, 17.5 and 18.2; 16 heads of 64 in blocks of 7, 17 MiB, 9.7 and 9.2.  With attention
+// through a window behind it, which then finds K, V and q in the L2s, 32 MiB together: 15 MiB 68.1
+// and 68.1, 29 MiB 96.6 and 95.1, 98.2 and 96.9, 38 MiB 94.4 and 93.8.)
 constexpr int64_t kRotateFew = 1 << 17;
 constexpr int64_t kRotatePast = int64_t(32) << 20;
 
