@@ -412,6 +412,24 @@ inline void fill(const Call& c, ChunkArgs* a) {
   a->scale_log2 = c.scale * kLog2e;
 }
 
+// Tile slots of a call's launch, workgroups of its merge, and whether their lanes are within 32
+// bits.
+struct Grid {
+  int64_t tiles, merge;
+  bool one, fits;                                // a merge's wave per (new token, query head), where
+};                                               // its lane groups hold all records at once
+inline Grid grid_of(const Kernels& kernels, const Shape& sh, int64_t n_tokens, int64_t n_req,
+                    int32_t q_heads, int32_t kv_heads, int head_dim) {
+  const Kind& kind = kernels.kind[sh.kind];
+  Grid g;
+  g.tiles = tile_slots(n_tokens, n_req, q_heads / kv_heads, kind.rows);
+  g.one = sh.splits <= kMergeChunk * 64 * 4 / head_dim;
+  g.merge = g.one ? (n_tokens * q_heads + 3) / 4 : n_tokens * q_heads;
+  g.fits = g.tiles * kv_heads <= UINT32_MAX / kind.threads / sh.splits &&
+           (sh.splits <= 1 || g.merge <= UINT32_MAX / kMergeThreads);
+  return g;
+}
+
 // Launches a call's kernels: its form's, and what joins its pieces or splits.  `args` begins
 // with a ChunkArgs that fill() has been through.
 template <class Args>
@@ -422,15 +440,9 @@ int launch(const Kernels& kernels, const Shape& sh, int32_t max_new, int head_di
   a.splits = sh.splits;
   a.row_shift = 0;
   while (1 << a.row_shift < kind.rows) ++a.row_shift;
-  const int64_t tiles = tile_slots(a.n_tokens, a.n_req, a.group, kind.rows);
-  const int64_t grid = tiles * a.kv_heads;
-  // a wave per (new token, query head) where its lane groups hold all records at once
-  const bool one = sh.splits <= kMergeChunk * 64 * 4 / head_dim;
-  const int64_t out_rows = int64_t(a.n_tokens) * a.q_heads,
-                merge = one ? (out_rows + 3) / 4 : out_rows;
-  // lanes of a launch in 32 bits
-  if (grid > UINT32_MAX / kind.threads / sh.splits ||
-      (sh.splits > 1 && merge > UINT32_MAX / kMergeThreads))
+  const Grid size = grid_of(kernels, sh, a.n_tokens, a.n_req, a.q_heads, a.kv_heads, head_dim);
+  const int64_t tiles = size.tiles, grid = tiles * a.kv_heads, merge = size.merge;
+  if (!size.fits)
     return fail(FLOWKV_EINVAL, "%lld tiles of queries x %d splits: too many for one call",
                 (long long)grid, sh.splits);
   a.tiles = int32_t(tiles);
@@ -451,7 +463,7 @@ int launch(const Kernels& kernels, const Shape& sh, int32_t max_new, int head_di
     e = hipLaunchKernel(kind.join[d128], dim3(unsigned(a.tiles * a.kv_heads * (kind.rows / 32))),
                         dim3(unsigned(2 * head_dim)), args, 0, stream);
   if (e == hipSuccess && sh.splits > 1)
-    e = hipLaunchKernel(kernels.merge[d128][!one], dim3(unsigned(merge)), dim3(kMergeThreads),
+    e = hipLaunchKernel(kernels.merge[d128][!size.one], dim3(unsigned(merge)), dim3(kMergeThreads),
                         args, 0, stream);
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess) return fail(FLOWKV_EHIP, "attention launch: %s", hipGetErrorString(e));

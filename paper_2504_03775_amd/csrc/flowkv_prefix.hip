@@ -151,6 +151,9 @@ struct Plan {
   int many_rows;               // of a tile over a prefix, in a launch of its own; 0: few_rows
   int32_t prefix_split, own_split;
   int64_t prefix_splits, own_splits;             // records of a row
+  int64_t prefix_items, own_tiles;               // tile slots of prefixes, and behind them
+  int64_t merge;                                 // workgroups of the join,
+  bool one, fits;                                // a wave a row; lanes of a launch in 32 bits
   int64_t need;
   int prefix_rows() const { return many_rows ? many_rows : few_rows; }
 };
@@ -194,10 +197,6 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
                     (split_tokens == 0 && double(tiles32) * prefix_bytes >= double(kMostRead));
   out->few_rows = (many || int64_t(max_group) * group <= 16) && one <= 16 ? 16 : 32;
   out->many_rows = many ? 128 : 0;
-  if (!out->shared) {
-    out->need = out->sh.need;
-    return FLOWKV_OK;
-  }
   constexpr int64_t kAll = INT32_MAX / kSplitUnit * kSplitUnit;
   auto split_of = [&](int64_t tiles, int32_t tokens, int64_t fixed, int64_t most) {
     if (split_tokens > 0) return int32_t(std::min<int64_t>(split_tokens, most));
@@ -212,11 +211,35 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
   };
   out->prefix_splits = splits_of(max_prefix, out->prefix_split);
   out->own_splits = splits_of(max_own, out->own_split);
-  if (__builtin_mul_overflow(int64_t(n_tokens) * q_heads,
-                             int64_t((head_dim + 2) * sizeof(float)), &out->need) ||
-      __builtin_mul_overflow(out->need, out->prefix_splits + out->own_splits, &out->need))
-    return fail(FLOWKV_EINVAL, "%lld splits: the workspace's size overflows",
-                (long long)(out->prefix_splits + out->own_splits));
+  const int64_t splits = out->prefix_splits + out->own_splits;
+  const int64_t out_rows = int64_t(n_tokens) * q_heads;
+  out->one = splits <= kMergeChunk * 64 * 4 / head_dim;
+  out->merge = out->one ? (out_rows + 3) / 4 : out_rows;
+  out->prefix_items = tile_slots(n_tokens, n_groups, group, out->prefix_rows());
+  out->own_tiles = tile_slots(n_tokens, n_req, group, out->few_rows);
+  // lanes of a launch in 32 bits: workgroups of prefixes and behind them, of a KV head
+  auto left = [&](int64_t most, int64_t items, int64_t each) {     // negative: too many
+    return each <= most && items <= most / each ? most - items * each : -1;
+  };
+  const int64_t most = UINT32_MAX / kFewThreads / kv_heads;
+  const int64_t behind =
+      many ? left(UINT32_MAX / 512 / kv_heads, out->prefix_items, out->prefix_splits) < 0 ? -1 : most
+           : left(most, out->prefix_items, out->prefix_splits);
+  out->fits = splits <= INT32_MAX && out->merge <= UINT32_MAX / kMergeThreads &&
+              left(behind, out->own_tiles, out->own_splits) >= 0;
+  const bool overflows = __builtin_mul_overflow(out_rows, int64_t((head_dim + 2) * sizeof(float)),
+                                                &out->need) ||
+                         __builtin_mul_overflow(out->need, splits, &out->need);
+  // (the rule takes no plan that is refused where the other is not)
+  if (split_tokens == 0 && (overflows || !out->fits) &&
+      grid_of(alone(FLOWKV_BF16), out->sh, n_tokens, n_req, q_heads, kv_heads, head_dim).fits)
+    out->shared = false;
+  if (!out->shared) {
+    out->need = out->sh.need;
+    return FLOWKV_OK;
+  }
+  if (overflows)
+    return fail(FLOWKV_EINVAL, "%lld splits: the workspace's size overflows", (long long)splits);
   return FLOWKV_OK;
 }
 
@@ -230,22 +253,11 @@ int launch_parts(int32_t dtype, const Plan& p, int head_dim, SpanArgs& a, hipStr
   const Parts& fn = parts(dtype);
   const int d128 = head_dim == 128, kv = a.kv_heads;
   const int64_t splits = p.prefix_splits + p.own_splits;
-  const int64_t out_rows = int64_t(a.n_tokens) * a.q_heads;
-  const bool one = splits <= kMergeChunk * 64 * 4 / head_dim;
-  const int64_t merge = one ? (out_rows + 3) / 4 : out_rows;
-  const int64_t prefix_items =
-      tile_slots(a.n_tokens, a.n_groups, a.group, p.prefix_rows());
-  const int64_t own_tiles = tile_slots(a.n_tokens, a.n_req, a.group, p.few_rows);
-  // lanes of a launch in 32 bits; workgroups of prefixes and behind them, of a KV head
-  auto fits = [&](int64_t items, int64_t each, int threads) {
-    return each <= UINT32_MAX / threads / kv && items <= UINT32_MAX / threads / kv / each;
-  };
-  if (splits > INT32_MAX || merge > UINT32_MAX / kMergeThreads ||
-      !fits(prefix_items, p.prefix_splits, 1024) || !fits(own_tiles, p.own_splits, 1024))
+  if (!p.fits)
     return fail(FLOWKV_EINVAL,
                 "%lld tiles of prefixes x %lld splits, %lld behind them x %lld: too many for one "
-                "call", (long long)prefix_items, (long long)p.prefix_splits, (long long)own_tiles,
-                (long long)p.own_splits);
+                "call", (long long)p.prefix_items, (long long)p.prefix_splits,
+                (long long)p.own_tiles, (long long)p.own_splits);
   a.splits = int32_t(splits);
   a.first_split = int32_t(p.prefix_splits);
   a.prefix_split = p.prefix_split;
@@ -255,19 +267,19 @@ int launch_parts(int32_t dtype, const Plan& p, int head_dim, SpanArgs& a, hipStr
     a.split_tokens = p.prefix_split;
     a.row_shift = row_shift(p.many_rows);
     e = hipLaunchKernel(fn.many[d128],
-                        dim3(unsigned(prefix_items * p.prefix_splits * kv)), dim3(512), args, 0,
+                        dim3(unsigned(p.prefix_items * p.prefix_splits * kv)), dim3(512), args, 0,
                         stream);
   }
-  a.prefix_items = p.many_rows ? 0 : uint32_t(prefix_items * p.prefix_splits);
+  a.prefix_items = p.many_rows ? 0 : uint32_t(p.prefix_items * p.prefix_splits);
   a.split_tokens = p.own_split;
   a.row_shift = row_shift(p.few_rows);
-  a.tiles = int32_t(own_tiles);
+  a.tiles = int32_t(p.own_tiles);
   if (e == hipSuccess)
     e = hipLaunchKernel(fn.few[p.few_rows == 32][d128],
-                        dim3(unsigned((a.prefix_items + own_tiles * p.own_splits) * kv)),
+                        dim3(unsigned((a.prefix_items + p.own_tiles * p.own_splits) * kv)),
                         dim3(kFewThreads), args, 0, stream);
   if (e == hipSuccess)
-    e = hipLaunchKernel(fn.merge[d128][!one], dim3(unsigned(merge)), dim3(kMergeThreads), args, 0,
+    e = hipLaunchKernel(fn.merge[d128][!p.one], dim3(unsigned(p.merge)), dim3(kMergeThreads), args, 0,
                         stream);
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess)

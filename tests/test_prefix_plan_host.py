@@ -46,3 +46,14 @@ def test_a_long_request_does_not_end_sharing_for_the_others():
             ws(n, req, 32, 8, 128, 0, n // req, n, 400, prefix)
     # padding rows are nobody's: single tokens in a batch of 8,192 rows, as a captured call has them
     assert records(8192, 64, 32, 8, 128, 1, 1, 64, 400, 4000) >= 2
+
+
+def test_the_rule_takes_no_plan_that_a_launch_cannot_hold():
+    """100,000 requests, one of 100 new tokens and 50,000 tokens of its own: a workgroup for every
+    split of every request's own would pass the lanes of a launch; whole tiles do not."""
+    n, req = 100_099, 100_000
+    assert ws(n, req, 32, 8, 128, 1, 100, n, 50_000, 13_000) == \
+        ws(n, req, 32, 8, 128, 0, 100, 0, 63_000, 0)
+    # where they fit
+    for n, own in ((20_000, 60_000), (60_000, 30_000), (100_000, 20_000)):
+        assert records(n, n, 32, 8, 128, 1, 1, n, own, 13_000) >= 2
