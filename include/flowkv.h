@@ -591,9 +591,9 @@ int flowkv_window_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q
    groups[g + 1] - 1 (n_groups + 1 non-decreasing int32 in device memory, requests outside of all
    groups allowed), whose first prefix_lens[g] tokens are the same: their block lists name the
    same K and V there (blocks shared by flowkv_share, a part-filled last one copied as flowkv_fork
-   has it).  The list of the group's first request is the one read for the prefix.  Every row sees all tokens up to
-   its own position, those of the prefix and those behind it: the result is that of
-   flowkv_chunk_attention, joined in another order.
+   has it).  The list of the group's first request is the one read for the prefix.  Every row sees
+   all tokens up to its own position, those of the prefix and those behind it: the result is that
+   of flowkv_chunk_attention, joined in another order.
    dtype: as for flowkv_window_attention.
    max_new: the most new tokens of a request, max_group: of a group; both size the launch, and
    rows past them are computed all the same.  max_prefix: the longest prefix; max_own: the most
@@ -604,8 +604,9 @@ int flowkv_window_attention_workspace(int32_t n_tokens, int32_t n_req, int32_t q
    in tiles of 128 rows; with no group or a max_prefix of 0 as for flowkv_chunk_attention); 0
    takes the library's rule, by which all of a call's requests are done each by itself where they
    bring more than 64 rows on average (112 where the longest brings four times as many), a row
-   being a (new token, query head of a KV head), or sharing saves under some 24 MiB of reads.  Up to three launches on hip_stream.  The rest is as
-   for flowkv_chunk_attention.  EINVAL for bad shapes or pointers, ECAP for a short workspace. */
+   being a (new token, query head of a KV head), or sharing saves under some 24 MiB of reads.  Up
+   to three launches on hip_stream.  The rest is as for flowkv_chunk_attention.  EINVAL for bad
+   shapes or pointers, ECAP for a short workspace. */
 int flowkv_prefix_attention(const flowkv_pool* pool, int32_t layer, int32_t dtype,
                             const void* q_dev, int64_t q_stride, int32_t n_tokens, int32_t n_req,
                             int32_t q_heads, int32_t kv_heads, int32_t head_dim,

@@ -412,12 +412,13 @@ inline void fill(const Call& c, ChunkArgs* a) {
   a->scale_log2 = c.scale * kLog2e;
 }
 
-// Tile slots of a call's launch, workgroups of its merge, and whether their lanes are within 32
+// Tile slots of a call's launch, workgroups of its merge (`one`: a wave per (new token, query
+// head), where its lane groups hold all records at once), and whether their lanes are within 32
 // bits.
 struct Grid {
   int64_t tiles, merge;
-  bool one, fits;                                // a merge's wave per (new token, query head), where
-};                                               // its lane groups hold all records at once
+  bool one, fits;
+};
 inline Grid grid_of(const Kernels& kernels, const Shape& sh, int64_t n_tokens, int64_t n_req,
                     int32_t q_heads, int32_t kv_heads, int head_dim) {
   const Kind& kind = kernels.kind[sh.kind];

@@ -222,11 +222,10 @@ int plan(int32_t n_tokens, int32_t n_req, int32_t q_heads, int32_t kv_heads, int
     return each <= most && items <= most / each ? most - items * each : -1;
   };
   const int64_t most = UINT32_MAX / kFewThreads / kv_heads;
-  const int64_t behind =
-      many ? left(UINT32_MAX / 512 / kv_heads, out->prefix_items, out->prefix_splits) < 0 ? -1 : most
-           : left(most, out->prefix_items, out->prefix_splits);
+  const int64_t room =
+      left(many ? UINT32_MAX / 512 / kv_heads : most, out->prefix_items, out->prefix_splits);
   out->fits = splits <= INT32_MAX && out->merge <= UINT32_MAX / kMergeThreads &&
-              left(behind, out->own_tiles, out->own_splits) >= 0;
+              left(many && room >= 0 ? most : room, out->own_tiles, out->own_splits) >= 0;
   const bool overflows = __builtin_mul_overflow(out_rows, int64_t((head_dim + 2) * sizeof(float)),
                                                 &out->need) ||
                          __builtin_mul_overflow(out->need, splits, &out->need);
@@ -279,8 +278,8 @@ int launch_parts(int32_t dtype, const Plan& p, int head_dim, SpanArgs& a, hipStr
                         dim3(unsigned((a.prefix_items + p.own_tiles * p.own_splits) * kv)),
                         dim3(kFewThreads), args, 0, stream);
   if (e == hipSuccess)
-    e = hipLaunchKernel(fn.merge[d128][!p.one], dim3(unsigned(p.merge)), dim3(kMergeThreads), args, 0,
-                        stream);
+    e = hipLaunchKernel(fn.merge[d128][!p.one], dim3(unsigned(p.merge)), dim3(kMergeThreads), args,
+                        0, stream);
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess)
     return fail(FLOWKV_EHIP, "prefix attention launch: %s", hipGetErrorString(e));
